@@ -265,6 +265,123 @@ moa_status moa_quantize_rows(const void *x, int32_t dtype, int64_t rows, int32_t
 moa_status moa_dequantize_rows(const int8_t *codes, const float *scales, int64_t rows, int32_t width, void *out,
                                int32_t dtype, void *stream);
 
+/* ---------------------------------------------------------------------------------------------------------------
+ * Serving operators around the drafter: a paged key / value cache with the attention of new rows over it, its eviction,
+ * and the rules between the LLM's logits and their verification. One cycle with a kept tree:
+ *   per LLM layer  moa_paged_attention (appends the tree's rows and attends), later moa_paged_commit (keeps the accepted path)
+ *   per cycle      moa_verify_greedy_rules on the logits, moa_token_record on the accepted tokens
+ *   now and then   moa_paged_evict
+ * and without drafting the same calls with one row per sequence. None of them needs a moa_ctx. They run on the current
+ * device, and `stream` has to belong to it. Lengths, tables and penalties are read on the device when a call's kernels run,
+ * so a captured call can be replayed while they change. Two calls that may overlap (different streams, two captured graphs)
+ * need workspaces of their own.
+ *
+ * A cache of one attention layer. Slot j of sequence b lies on page page_table[b][j / page_size], row j % page_size. Keys are
+ * stored as they enter the scores (already rotated). Slots 0 .. len[b]-1 are committed; len[b] < 0 marks a sequence that is
+ * not in use: no call reads, writes or advances anything of it, its rows of an output stay as they were. len and seen may be
+ * shared by the layers of a model; the calls take the new rows to lie behind len, and only moa_paged_commit with advance
+ * and moa_paged_evict with len_out move it. Positions on a page whose table entry is outside 0 .. n_pages-1 are left out,
+ * as are those behind the last slot, max_pages * page_size. The pages of a sequence must not be shared with another one
+ * where they are written. */
+typedef struct {
+  void *k, *v;               /* T [n_pages, page_size, hkv, head_dim]; page p starts page_stride * p elements in */
+  int64_t page_stride;       /* elements, >= page_size * hkv * head_dim, a multiple of 16 bytes (k and v may share blocks) */
+  const int32_t *page_table; /* device int32 [batch, max_pages] */
+  int32_t *len;              /* device int32 [batch] */
+  float *weight;             /* device [batch, hkv, max_pages * page_size]: accumulated attention weights, or NULL */
+  int32_t *pos;              /* device, the same shape: position that each slot's token had; NULL, or with weight and seen */
+  int32_t *seen;             /* device int32 [batch]: positions appended so far = the next row's position; or NULL */
+  int32_t batch;             /* <= MOA_MAX_BATCH */
+  int32_t max_pages, n_pages;
+  int32_t page_size;         /* a power of two <= 1024; max_pages * page_size <= 2^30 */
+  int32_t hkv, head_dim;     /* head_dim 64 or 128 */
+  int32_t dtype;             /* moa_dtype of k, v and of the rows */
+} moa_paged_cache;
+
+#define MOA_PAGED_MAX_ROWS 64 /* new rows per sequence: the slots that one packed mask word of moa_tree_attn_mask holds */
+
+/* Writes rows i < n_new[b] (all n when n_new is NULL; device int32 [batch]) of k_new, v_new T [batch, n, hkv, head_dim] to
+ * slots len[b] + i, without changing len. Rows lie row_stride elements apart (>= hkv * head_dim, a multiple of 16 bytes), so
+ * that they may be a part of a fused projection. With pos, the slots get positions seen[b] + i and weight 0. n is not
+ * bounded: a whole prompt may be appended. */
+moa_status moa_paged_append(const moa_paged_cache *cache, const void *k_new, const void *v_new, int64_t row_stride, int32_t n,
+                            const int32_t *n_new, void *stream);
+
+/* Attention of n new rows per sequence (n = 1: the next token; up to MOA_PAGED_MAX_ROWS: a kept tree):
+ *   out[b, i, h] = sum_j softmax_j(scale * q[b, i, h] . k_j) v_j
+ * over the slots j < len[b] and, when n_new = n, the rows' own slots len[b] + j' that row i sees: bit j' of mask[b, i]
+ * (device uint64 [batch, n], as moa_tree_attn_mask packs it for n <= 64), or j' <= i when mask is NULL. n_new = 0: the
+ * committed slots only, as in a cross-attention. A row whose mask word is 0 (an unused slot) sees nothing, and a row that
+ * sees nothing gives zeros. A new slot that no row sees is not read.
+ *   q           T [batch, n, hq, head_dim], rows q_stride elements apart; head h belongs to key / value head h / (hq / hkv)
+ *   k_new,v_new T [batch, n, hkv, head_dim], rows new_stride elements apart: appended by this call as moa_paged_append
+ *               would (slots that no row sees are not written), or NULL when the rows are in the pages already
+ *   scale       0 means 1 / sqrt(head_dim)
+ *   out         T [batch, n, hq, head_dim]
+ *   weight_out  device float [batch, hkv, max_pages * page_size], may be cache->weight, or NULL; n = 1 only: for every slot
+ *               that the row sees, cache->weight (0 for the new slot, or without it) + the sum over the group's query heads
+ *               of the softmax weights. Other entries stay as they were.
+ *   ws          device scratch of moa_paged_workspace_bytes bytes (its contents need not be kept or zeroed)
+ * Scores, statistics and sums are fp32. hq / hkv <= 128. */
+moa_status moa_paged_workspace_bytes(const moa_paged_cache *cache, int32_t n, int32_t hq, int32_t weights, size_t *bytes);
+moa_status moa_paged_attention(const moa_paged_cache *cache, const void *q, int64_t q_stride, const void *k_new, const void *v_new,
+                               int64_t new_stride, int32_t n, int32_t n_new, int32_t hq, const uint64_t *mask, float scale, void *out,
+                               float *weight_out, void *ws, size_t ws_bytes, void *stream);
+
+/* Ends a cycle for n uncommitted rows. With acc_slot (device int32 [batch, cap]) and acc_len (device int32 [batch]), as
+ * moa_verify_greedy writes them: the accepted rows' keys and values move to slots len[b] .. len[b] + acc_len[b] - 1, the
+ * others are given up (n <= MOA_PAGED_MAX_ROWS; the listed slots rise). advance != 0: len (and seen) grow by acc_len, or by
+ * n when acc_len is NULL. With several layers that share len: the layers' calls without advance, then one with it. */
+moa_status moa_paged_commit(const moa_paged_cache *cache, int32_t n, const int32_t *acc_slot, const int32_t *acc_len, int32_t cap,
+                            int32_t advance, void *stream);
+
+/* Eviction by accumulated attention weight. Of a sequence with len[b] > budget every key / value head keeps budget slots of
+ * its own: those of positions < sink and >= seen[b] - recent, and of the others the ones with the largest weight (a NaN
+ * after all numbers, equal weights by the lower slot). The kept slots behind the budget move to the freed slots before it,
+ * both in rising order; slots from the budget on are free afterwards. Needs cache->weight, pos and seen; sink + recent <=
+ * budget.
+ *   weight_out, pos_out  shaped as cache->weight and pos and may be them: entries of the slots in use afterwards
+ *   len_out     device int32 [batch], may be cache->len, or NULL: min(len, budget)
+ *   ws          device scratch of moa_paged_evict_workspace_bytes bytes */
+moa_status moa_paged_evict_workspace_bytes(const moa_paged_cache *cache, int32_t budget, size_t *bytes);
+moa_status moa_paged_evict(const moa_paged_cache *cache, int32_t budget, int32_t sink, int32_t recent, float *weight_out, int32_t *pos_out,
+                           int32_t *len_out, void *ws, size_t ws_bytes, void *stream);
+
+/* The record of the tokens that a sequence holds, for the penalties: counts device int32 [batch, vocab] and seen device
+ * uint32 [batch, ceil(vocab / 32)] (bit t % 32 of word t / 32), both zeroed by the caller for a new sequence. Adds tokens
+ * tok[b][0 .. n_tok[b]-1] (device int32 [batch, cap]; n_tok device int32 [batch], NULL: all cap): their bits in seen, and 1
+ * each in counts. A prompt, which only the repetition penalty counts, is added with counts NULL. Tokens outside
+ * 0 .. vocab-1 are left out, so acc_tok of moa_verify_greedy can be passed as it is. vocab <= 2^20. */
+moa_status moa_token_record(int32_t *counts, uint32_t *seen, int32_t batch, int32_t vocab, const int32_t *tok, const int32_t *n_tok, int32_t cap,
+                            void *stream);
+
+/* Rules for logits. Every pointer may be NULL (that rule is off). */
+typedef struct {
+  const int32_t *counts;     /* device int32 [batch, vocab]: times each token was generated */
+  const uint32_t *seen;      /* device uint32 [batch, ceil(vocab / 32)]: tokens of prompt and answer. With seen, counts are
+                                read where its bit is set only; without it, a token is in the context when its count > 0 */
+  const float *repetition;   /* device float [batch]: divides positive and multiplies other logits of the context's tokens */
+  const float *frequency;    /* device float [batch]: subtracted once per generation */
+  const float *presence;     /* device float [batch]: subtracted when generated at all */
+  const int32_t *bias_id;    /* device int32 [batch, n_bias]; ids outside 0 .. vocab-1 mark unused entries */
+  const float *bias_value;   /* device float [batch, n_bias]: added; the values of an id that is listed twice are summed in order */
+  const uint32_t *allow;     /* device uint32 [batch, n, ceil(vocab / 32)]: a token whose bit is 0 gets -inf, whatever its logit */
+  int32_t n_bias;            /* <= 1024 */
+} moa_logit_rule_set;
+
+/* Applies the rules to logits [batch, n, vocab] of logits_dtype, in the order of the struct, in fp32, each step rounded once;
+ * out (the logits' type, may be the logits themselves, or NULL) gets the result rounded once, choice (device int32 [batch, n]
+ * or NULL) the arg-max of the unrounded result: ties to the smallest id, NaN never, and 0 when nothing is above -inf.
+ * With tok and parent (device int32 [batch, n], a kept tree as moa_tree_expand writes it, n <= 256) the tokens on the path
+ * from the root to slot i, both included, count as generated for row i: the record holds the tokens before the root. The row
+ * of an unused slot has no path. batch * n <= 65535, vocab <= 2^20. */
+moa_status moa_logit_rules(const moa_logit_rule_set *rules, const int32_t *tok, const int32_t *parent, int32_t batch, int32_t n,
+                           const void *logits, int32_t logits_dtype, int32_t vocab, void *out, int32_t *choice, void *stream);
+/* moa_verify_greedy with the choices of moa_logit_rules; no adjusted logits are written. */
+moa_status moa_verify_greedy_rules(const moa_logit_rule_set *rules, const int32_t *tok, const int32_t *parent, int32_t batch, int32_t n,
+                                   const void *target_logits, int32_t logits_dtype, int32_t vocab, int32_t cap, int32_t *choice,
+                                   int32_t *acc_slot, int32_t *acc_tok, int32_t *acc_len, int32_t *next_tok, void *stream);
+
 /* Reads back the device status word kept in st->tree (0 = no device-side problem seen). Synchronises the stream. */
 moa_status moa_state_status(moa_ctx *ctx, moa_state *st, void *stream);
 

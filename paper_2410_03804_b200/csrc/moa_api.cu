@@ -4,6 +4,7 @@
 
 #include <stdio.h>
 #include <string.h>
+#include <atomic>
 #include <mutex>
 #include <new>
 
@@ -13,7 +14,10 @@
 #include "moa_attn_tc.cuh"
 #include "moa_basic.cuh"
 #include "moa_codec.cuh"
+#include "moa_evict.cuh"
+#include "moa_paged.cuh"
 #include "moa_phases.cuh"
+#include "moa_rules.cuh"
 #include "moa_tree.cuh"
 #include "moa_verify.cuh"
 #include "moa_wstream.cuh"
@@ -1791,3 +1795,5 @@ moa_status moa_state_status(moa_ctx* ctx, moa_state* st, void* stream) {
 }
 
 }  // extern "C"
+
+#include "moa_serving.inc"

@@ -21,7 +21,9 @@ MOA_OK = 0
 
 EXPORTS = ["moa_create", "moa_destroy", "moa_tli_configure", "moa_state_bytes", "moa_status_str", "moa_last_cuda_error",
            "moa_state_set_len", "moa_lsa_forward", "moa_sa_append", "moa_sa_append_static", "moa_drafter_prefill", "moa_tree_begin", "moa_draft_step",
-           "moa_tree_expand", "moa_tree_attn_mask", "moa_verify_greedy", "moa_pack_tree", "moa_unpack_tree", "moa_quantize_rows", "moa_dequantize_rows", "moa_state_status", "moa_profile_begin", "moa_profile_end", "moa_profile_phases",
+           "moa_tree_expand", "moa_tree_attn_mask", "moa_verify_greedy", "moa_pack_tree", "moa_unpack_tree", "moa_quantize_rows", "moa_dequantize_rows",
+           "moa_paged_workspace_bytes", "moa_paged_append", "moa_paged_attention", "moa_paged_commit", "moa_paged_evict_workspace_bytes",
+           "moa_paged_evict", "moa_token_record", "moa_logit_rules", "moa_verify_greedy_rules", "moa_state_status", "moa_profile_begin", "moa_profile_end", "moa_profile_phases",
            "moa_launch_count", "moa_trace_begin", "moa_trace_end"]
 
 
@@ -65,6 +67,17 @@ class MoaState(C.Structure):
     _fields_ = [("ca_k", C.c_void_p), ("ca_v", C.c_void_p), ("sa_k", C.c_void_p), ("sa_v", C.c_void_p),
                 ("ca_len", C.c_void_p), ("sa_len", C.c_void_p), ("tree", C.c_void_p),
                 ("ca_len_host", C.c_void_p), ("sa_len_host", C.c_void_p), ("step", C.c_int32)]
+
+
+class MoaPagedCache(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("page_stride", C.c_int64)] + [
+        (n, C.c_void_p) for n in ("page_table", "len", "weight", "pos", "seen")] + [
+        (n, C.c_int32) for n in ("batch", "max_pages", "n_pages", "page_size", "hkv", "head_dim", "dtype")]
+
+
+class MoaLogitRuleSet(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("counts", "seen", "repetition", "frequency", "presence", "bias_id", "bias_value",
+                                          "allow")] + [("n_bias", C.c_int32)]
 
 
 class MoaError(RuntimeError):
@@ -118,6 +131,15 @@ def load_library(rebuild_if_stale: bool = True) -> C.CDLL:
     lib.moa_unpack_tree.argtypes = [vp, C.c_int64, vp, vp, vp]
     lib.moa_quantize_rows.argtypes = [vp, i32, C.c_int64, i32, vp, vp, vp]
     lib.moa_dequantize_rows.argtypes = [vp, vp, C.c_int64, i32, vp, i32, vp]
+    lib.moa_paged_workspace_bytes.argtypes = [vp, i32, i32, i32, C.POINTER(sz)]
+    lib.moa_paged_append.argtypes = [vp, vp, vp, C.c_int64, i32, vp, vp]
+    lib.moa_paged_attention.argtypes = [vp, vp, C.c_int64, vp, vp, C.c_int64, i32, i32, i32, vp, C.c_float, vp, vp, vp, sz, vp]
+    lib.moa_paged_commit.argtypes = [vp, i32, vp, vp, i32, i32, vp]
+    lib.moa_paged_evict_workspace_bytes.argtypes = [vp, i32, C.POINTER(sz)]
+    lib.moa_paged_evict.argtypes = [vp, i32, i32, i32, vp, vp, vp, vp, sz, vp]
+    lib.moa_token_record.argtypes = [vp, vp, i32, i32, vp, vp, i32, vp]
+    lib.moa_logit_rules.argtypes = [vp, vp, vp, i32, i32, vp, i32, i32, vp, vp, vp]
+    lib.moa_verify_greedy_rules.argtypes = [vp, vp, vp, i32, i32, vp, i32, i32, i32, vp, vp, vp, vp, vp, vp]
     lib.moa_state_status.argtypes = [vp, C.POINTER(MoaState), vp]
     lib.moa_profile_begin.argtypes = [vp]
     lib.moa_profile_end.argtypes = [vp, C.POINTER(C.c_double), C.POINTER(i32)]
@@ -229,6 +251,260 @@ def moa_dequantize_rows(codes: torch.Tensor, scales: torch.Tensor, dtype=torch.f
     _check(load_library().moa_dequantize_rows(_ptr(codes), _ptr(scales), codes.shape[0], codes.shape[1], _ptr(out),
                                               0 if out.dtype == torch.float32 else 1, _stream(stream)), "moa_dequantize_rows")
     return out
+
+
+def _on(t: torch.Tensor, device) -> bool:
+    return t.is_cuda and t.device == device
+
+
+def _serving_call(device, stream, status_of, what: str):
+    """Runs a call of the serving operators with its tensors' device current, on the given or that device's current stream."""
+    if torch.cuda.current_device() == device.index:
+        _check(status_of(_stream(stream)), what)
+    else:
+        with torch.cuda.device(device):
+            _check(status_of(_stream(stream)), what)
+
+
+def _rows(t: torch.Tensor, batch: int, heads: int, head_dim: int, dtype, device, what: str):
+    """Checks rows [batch, n, heads, head_dim] whose heads are contiguous; returns (n, elements between two rows)."""
+    assert t.dim() == 4 and t.shape[0] == batch and t.shape[2] == heads and t.shape[3] == head_dim, what
+    assert t.dtype == dtype and _on(t, device), what
+    n = t.shape[1]
+    assert n >= 1 and t.stride(3) == 1 and t.stride(2) == head_dim, what + ": heads must be contiguous"
+    if n == 1:
+        step = t.stride(0) if batch > 1 else heads * head_dim
+    else:
+        step = t.stride(1)
+        assert batch == 1 or t.stride(0) == n * step, what + ": rows must be evenly spaced"
+    return n, step
+
+
+class PagedCache:
+    """The key / value cache of one attention layer in pages (moa_paged_cache of include/moa.h). k, v: cuda float32 /
+    bfloat16 [n_pages, page_size, hkv, head_dim], contiguous within a page (views of one block are fine); page_table: int32
+    [batch, max_pages]; length: int32 [batch], committed slots, < 0 for a sequence not in use; weight, pos: float32 / int32
+    [batch, hkv, max_pages * page_size] and seen: int32 [batch] for accumulated weights and eviction. The tensors are held,
+    not copied; the caller fills the table."""
+
+    def __init__(self, k, v, page_table, length, weight=None, pos=None, seen=None):
+        assert k.is_cuda and k.dim() == 4 and k.dtype in (torch.float32, torch.bfloat16), "k: cuda [n_pages, page_size, hkv, head_dim]"
+        dev, (n_pages, ps, hkv, dh) = k.device, k.shape
+        assert _on(v, dev) and v.shape == k.shape and v.dtype == k.dtype and v.stride() == k.stride(), "v must be laid out as k"
+        assert k.stride(3) == 1 and k.stride(2) == dh and (ps == 1 or k.stride(1) == hkv * dh), "a page must be contiguous"
+        i32 = lambda t: _on(t, dev) and t.dtype == torch.int32 and t.is_contiguous()  # noqa: E731
+        assert i32(page_table) and page_table.dim() == 2 and page_table.shape[1] >= 1, "page_table: int32 [batch, max_pages]"
+        batch, per = page_table.shape
+        assert i32(length) and length.shape == (batch,), "length: int32 [batch]"
+        full = (batch, hkv, per * ps)
+        assert weight is None or (_on(weight, dev) and weight.dtype == torch.float32 and weight.is_contiguous() and weight.shape == full), "weight"
+        assert pos is None or (i32(pos) and pos.shape == full), "pos"
+        assert seen is None or (i32(seen) and seen.shape == (batch,)), "seen"
+        self.k, self.v, self.page_table, self.len, self.weight, self.pos, self.seen = k, v, page_table, length, weight, pos, seen
+        self.device, self.dtype, self.batch, self.hkv, self.head_dim, self.slots = dev, k.dtype, batch, hkv, dh, per * ps
+        self.c = MoaPagedCache(k.data_ptr(), v.data_ptr(), k.stride(0) if n_pages > 1 else ps * hkv * dh, page_table.data_ptr(),
+                               length.data_ptr(), weight.data_ptr() if weight is not None else None,
+                               pos.data_ptr() if pos is not None else None, seen.data_ptr() if seen is not None else None, batch,
+                               per, n_pages, ps, hkv, dh, 0 if k.dtype == torch.float32 else 1)
+        self._ref = C.addressof(self.c)
+
+    def _scratch(self, status_of, what: str) -> int:
+        n = C.c_size_t()
+        with torch.cuda.device(self.device):
+            _check(status_of(C.byref(n)), what)
+        return n.value
+
+    def workspace(self, n: int, hq: int, weights: bool = False) -> torch.Tensor:
+        """Scratch for moa_paged_attention with n rows per sequence and hq query heads."""
+        lib = load_library()
+        return torch.empty(self._scratch(lambda b: lib.moa_paged_workspace_bytes(self._ref, n, hq, 1 if weights else 0, b),
+                                         "moa_paged_workspace_bytes"), dtype=torch.uint8, device=self.device)
+
+    def evict_workspace(self, budget: int) -> torch.Tensor:
+        """Scratch for moa_paged_evict."""
+        lib = load_library()
+        return torch.empty(self._scratch(lambda b: lib.moa_paged_evict_workspace_bytes(self._ref, budget, b),
+                                         "moa_paged_evict_workspace_bytes"), dtype=torch.uint8, device=self.device)
+
+    def _own_scratch(self, ws, make, stream):
+        if ws is None:
+            ws = make()
+            if stream is not None:
+                ws.record_stream(stream)
+        assert _on(ws, self.device) and ws.dtype == torch.uint8 and ws.is_contiguous(), "ws: cuda uint8, contiguous"
+        return ws
+
+
+def moa_paged_append(cache: PagedCache, k_new: torch.Tensor, v_new: torch.Tensor, n_new=None, stream=None):
+    """Writes rows [batch, n, hkv, head_dim] behind the committed slots (the first n_new[b] of each sequence), without
+    committing them."""
+    n, step = _rows(k_new, cache.batch, cache.hkv, cache.head_dim, cache.dtype, cache.device, "k_new")
+    assert _rows(v_new, cache.batch, cache.hkv, cache.head_dim, cache.dtype, cache.device, "v_new") == (n, step), "v_new must be laid out as k_new"
+    if n_new is not None:
+        assert _on(n_new, cache.device) and n_new.dtype == torch.int32 and n_new.shape == (cache.batch,) and n_new.is_contiguous()
+    lib = load_library()
+    _serving_call(cache.device, stream, lambda s: lib.moa_paged_append(cache._ref, k_new.data_ptr(), v_new.data_ptr(), step, n,
+                                                                       _ptr(n_new), s), "moa_paged_append")
+
+
+def moa_paged_attention(cache: PagedCache, q: torch.Tensor, k_new=None, v_new=None, mask=None, scale: float = 0.0,
+                        new_rows: bool = True, out=None, weight_out=None, ws=None, stream=None) -> torch.Tensor:
+    """Attention of q [batch, n, hq, head_dim] over the cache and the n new rows (k_new, v_new [batch, n, hkv, head_dim] are
+    appended by the call; without them the rows are in the pages already; new_rows=False: there are none). mask: int64
+    [batch, n] or [batch, n, 1], one packed word per row as moa_tree_attn_mask(packed=True) gives it; None: causal.
+    weight_out (n = 1): float32 [batch, hkv, slots], may be cache.weight. Returns out [batch, n, hq, head_dim]."""
+    dev, b, hkv, dh = cache.device, cache.batch, cache.hkv, cache.head_dim
+    assert q.dim() == 4, "q: [batch, n, hq, head_dim]"
+    hq = q.shape[2]
+    n, q_step = _rows(q, b, hq, dh, cache.dtype, dev, "q")
+    kp = vp = None
+    new_step = 0
+    if k_new is not None:
+        assert v_new is not None and new_rows, "k_new and v_new come together, as new rows"
+        m, new_step = _rows(k_new, b, hkv, dh, cache.dtype, dev, "k_new")
+        assert m == n and _rows(v_new, b, hkv, dh, cache.dtype, dev, "v_new") == (n, new_step), "v_new must be laid out as k_new"
+        kp, vp = k_new.data_ptr(), v_new.data_ptr()
+    else:
+        assert v_new is None, "k_new and v_new come together, as new rows"
+    mp = None
+    if mask is not None:
+        assert _on(mask, dev) and mask.dtype in (torch.int64, torch.uint64) and mask.is_contiguous() and mask.numel() == b * n, "mask: int64 [batch, n]"
+        mp = mask.data_ptr()
+    if out is None:
+        out = torch.empty((b, n, hq, dh), dtype=cache.dtype, device=dev)
+        if stream is not None:
+            out.record_stream(stream)
+    else:
+        assert _on(out, dev) and out.dtype == cache.dtype and out.shape == q.shape and out.is_contiguous(), "out"
+    wp = None
+    if weight_out is not None:
+        assert _on(weight_out, dev) and weight_out.dtype == torch.float32 and weight_out.is_contiguous(), "weight_out"
+        assert weight_out.shape == (b, hkv, cache.slots), "weight_out"
+        wp = weight_out.data_ptr()
+    ws = cache._own_scratch(ws, lambda: cache.workspace(n, hq, wp is not None), stream)
+    lib = load_library()
+    _serving_call(dev, stream, lambda s: lib.moa_paged_attention(cache._ref, q.data_ptr(), q_step, kp, vp, new_step, n, n if new_rows else 0,
+                                                                 hq, mp, float(scale), out.data_ptr(), wp, ws.data_ptr(), ws.numel(), s),
+                  "moa_paged_attention")
+    return out
+
+
+def moa_paged_commit(cache: PagedCache, n: int, acc_slot=None, acc_len=None, advance: bool = True, stream=None):
+    """Keeps the accepted path (acc_slot [batch, cap], acc_len [batch] of moa_verify_greedy) of n uncommitted rows, or all of
+    them, and advances cache.len (and cache.seen) when asked to."""
+    i32 = lambda t: _on(t, cache.device) and t.dtype == torch.int32 and t.is_contiguous()  # noqa: E731
+    assert acc_len is None or (i32(acc_len) and acc_len.shape == (cache.batch,)), "acc_len: int32 [batch]"
+    cap = 0
+    if acc_slot is not None:
+        assert acc_len is not None and i32(acc_slot) and acc_slot.dim() == 2 and acc_slot.shape[0] == cache.batch, "acc_slot: int32 [batch, cap]"
+        cap = acc_slot.shape[1]
+    lib = load_library()
+    _serving_call(cache.device, stream, lambda s: lib.moa_paged_commit(cache._ref, int(n), _ptr(acc_slot), _ptr(acc_len), cap,
+                                                                       1 if advance else 0, s), "moa_paged_commit")
+
+
+def moa_paged_evict(cache: PagedCache, budget: int, sink: int = 4, recent: int = 64, weight_out=None, pos_out=None, len_out=None,
+                    update_len: bool = True, ws=None, stream=None):
+    """Cuts every sequence's heads to `budget` slots (see include/moa.h). weight_out and pos_out default to the cache's own;
+    len_out to cache.len, or to nothing with update_len=False (layers that share len)."""
+    assert cache.weight is not None and cache.pos is not None and cache.seen is not None, "the cache needs weight, pos and seen"
+    w, p = cache.weight if weight_out is None else weight_out, cache.pos if pos_out is None else pos_out
+    assert _on(w, cache.device) and w.dtype == torch.float32 and w.is_contiguous() and w.shape == cache.weight.shape, "weight_out"
+    assert _on(p, cache.device) and p.dtype == torch.int32 and p.is_contiguous() and p.shape == cache.pos.shape, "pos_out"
+    n = len_out if len_out is not None else cache.len if update_len else None
+    assert n is None or (_on(n, cache.device) and n.dtype == torch.int32 and n.is_contiguous() and n.shape == cache.len.shape), "len_out"
+    ws = cache._own_scratch(ws, lambda: cache.evict_workspace(budget), stream)
+    lib = load_library()
+    _serving_call(cache.device, stream, lambda s: lib.moa_paged_evict(cache._ref, int(budget), int(sink), int(recent), w.data_ptr(), p.data_ptr(),
+                                                                      _ptr(n), ws.data_ptr(), ws.numel(), s), "moa_paged_evict")
+
+
+class LogitRules:
+    """The rules of a batch of sequences (moa_logit_rule_set of include/moa.h); every tensor may be None. vocab: V; counts:
+    int32 [batch, V]; seen: int32 [batch, ceil(V / 32)] bits; repetition, frequency, presence: float32 [batch]; bias_id,
+    bias_value: int32 / float32 [batch, n_bias]; allow: int32 [batch, n, ceil(V / 32)] bits. The tensors are held, not
+    copied: counts and seen may grow (moa_token_record) and penalties change between calls."""
+
+    def __init__(self, vocab: int, counts=None, seen=None, repetition=None, frequency=None, presence=None, bias_id=None,
+                 bias_value=None, allow=None):
+        words = (vocab + 31) // 32
+        given = [t for t in (counts, seen, repetition, frequency, presence, bias_id, bias_value, allow) if t is not None]
+        assert (bias_id is None) == (bias_value is None), "bias_id and bias_value come together"
+        self.device = given[0].device if given else None
+        self.batch = given[0].shape[0] if given else None
+        self.rows = None if allow is None else allow.shape[1]
+        n_bias = 0 if bias_id is None else bias_id.shape[1]
+        for t, dt, shape, what in ((counts, torch.int32, (self.batch, vocab), "counts"), (seen, torch.int32, (self.batch, words), "seen"),
+                                   (repetition, torch.float32, (self.batch,), "repetition"), (frequency, torch.float32, (self.batch,), "frequency"),
+                                   (presence, torch.float32, (self.batch,), "presence"), (bias_id, torch.int32, (self.batch, n_bias), "bias_id"),
+                                   (bias_value, torch.float32, (self.batch, n_bias), "bias_value"),
+                                   (allow, torch.int32, (self.batch, self.rows, words), "allow")):
+            assert t is None or (_on(t, self.device) and t.dtype == dt and t.is_contiguous() and t.shape == shape), what
+        self.vocab, self.counts, self.seen, self.held = vocab, counts, seen, given
+        p = lambda t: None if t is None or t.numel() == 0 else t.data_ptr()  # noqa: E731
+        self.c = MoaLogitRuleSet(p(counts), p(seen), p(repetition), p(frequency), p(presence), p(bias_id), p(bias_value), p(allow), n_bias)
+        self._ref = C.addressof(self.c)
+
+
+def moa_token_record(tok: torch.Tensor, vocab: int, counts=None, seen=None, n_tok=None, stream=None):
+    """Adds tokens tok int32 [batch, cap] (the first n_tok[b] of each sequence; ids outside 0..vocab-1 are left out) to the
+    record: bits in seen, and numbers in counts (None for a prompt)."""
+    assert tok.is_cuda and tok.dtype == torch.int32 and tok.dim() == 2 and tok.is_contiguous(), "tok: cuda int32 [batch, cap]"
+    b, cap = tok.shape
+    i32 = lambda t: _on(t, tok.device) and t.dtype == torch.int32 and t.is_contiguous()  # noqa: E731
+    assert counts is None or (i32(counts) and counts.shape == (b, vocab)), "counts: int32 [batch, vocab]"
+    assert seen is None or (i32(seen) and seen.shape == (b, (vocab + 31) // 32)), "seen: int32 [batch, ceil(vocab / 32)]"
+    assert n_tok is None or (i32(n_tok) and n_tok.shape == (b,)), "n_tok: int32 [batch]"
+    lib = load_library()
+    _serving_call(tok.device, stream, lambda s: lib.moa_token_record(_ptr(counts), _ptr(seen), b, vocab, _ptr(tok), _ptr(n_tok), cap, s),
+                  "moa_token_record")
+
+
+def _rule_rows(rules: LogitRules, logits: torch.Tensor, tok, parent):
+    assert logits.is_cuda and logits.is_contiguous() and logits.dim() == 3 and logits.dtype in (torch.float32, torch.bfloat16), "logits: [batch, n, V]"
+    b, n, v = logits.shape
+    assert v == rules.vocab and rules.batch in (None, b) and rules.rows in (None, n), "the rules are of another batch"
+    assert rules.device in (None, logits.device), "the rules are on another device"
+    assert (tok is None) == (parent is None), "tok and parent come together"
+    if tok is not None:
+        for t in (tok, parent):
+            assert _on(t, logits.device) and t.dtype == torch.int32 and t.is_contiguous() and t.shape == (b, n), "tok, parent: int32 [batch, n]"
+    return b, n, v, 0 if logits.dtype == torch.float32 else 1
+
+
+def moa_logit_rules(rules: LogitRules, logits: torch.Tensor, tok=None, parent=None, out=None, choice=None, stream=None):
+    """Applies the rules to logits [batch, n, V]; tok, parent int32 [batch, n]: the kept tree whose slots the rows are.
+    Returns (adjusted logits, arg-max int32 [batch, n]); out may be the logits themselves."""
+    b, n, v, dt = _rule_rows(rules, logits, tok, parent)
+    if out is None:
+        out = torch.empty_like(logits)
+    else:
+        assert _on(out, logits.device) and out.dtype == logits.dtype and out.shape == logits.shape and out.is_contiguous(), "out"
+    if choice is None:
+        choice = torch.empty((b, n), dtype=torch.int32, device=logits.device)
+    else:
+        assert _on(choice, logits.device) and choice.dtype == torch.int32 and choice.shape == (b, n) and choice.is_contiguous(), "choice"
+    lib = load_library()
+    _serving_call(logits.device, stream, lambda s: lib.moa_logit_rules(rules._ref, _ptr(tok), _ptr(parent), b, n, logits.data_ptr(), dt, v,
+                                                                       out.data_ptr(), choice.data_ptr(), s), "moa_logit_rules")
+    return out, choice
+
+
+def moa_verify_greedy_rules(rules: LogitRules, tok: torch.Tensor, parent: torch.Tensor, target_logits: torch.Tensor, cap: int, out=None,
+                            stream=None):
+    """moa_verify_greedy with the arg-max of the adjusted logits; none are written. Returns the same five tensors."""
+    assert tok is not None, "a verification needs the tree"
+    b, n, v, dt = _rule_rows(rules, target_logits, tok, parent)
+    dev, cap = target_logits.device, int(cap)
+    if out is None:
+        out = tuple(torch.empty(s, dtype=torch.int32, device=dev) for s in ((b, n), (b, cap), (b, cap), (b,), (b,)))
+    else:
+        for t, s in zip(out, ((b, n), (b, cap), (b, cap), (b,), (b,))):
+            assert _on(t, dev) and t.dtype == torch.int32 and t.is_contiguous() and t.shape == s, "out"
+    lib = load_library()
+    _serving_call(dev, stream, lambda s: lib.moa_verify_greedy_rules(rules._ref, tok.data_ptr(), parent.data_ptr(), b, n, target_logits.data_ptr(),
+                                                                     dt, v, cap, *(t.data_ptr() for t in out), s), "moa_verify_greedy_rules")
+    return tuple(out)
 
 
 class MoA:
