@@ -16,6 +16,7 @@
 #include "moa_codec.cuh"
 #include "moa_evict.cuh"
 #include "moa_paged.cuh"
+#include "moa_paged_tc.cuh"
 #include "moa_phases.cuh"
 #include "moa_rules.cuh"
 #include "moa_tree.cuh"

@@ -10,8 +10,9 @@
 // Work split (paged_rows_kernel): the (sequence, head, query tile) items are laid end to end as tiles of positions, and
 // the CTAs take equal consecutive stretches of that line, whatever the sequences' lengths are; the lengths are read on
 // the device, so a captured graph follows them. A stretch may end inside an item: such an item is left in pieces
-// (max, sum, unnormalised output), one per CTA, and paged_join_kernel adds them in the order of their positions, the same
-// order on every run. Piece number = CTA + item, unique because every step along the line changes one of the two.
+// (max, sum, unnormalised output) and paged_join_kernel adds them in the order of their positions, the same order on every
+// run. Only the first and the last item of a stretch can be cut, so a CTA has two places for pieces: the first for the item
+// its stretch begins in, the second for the one it ends in.
 //
 // Inside a CTA the four warps run on their own: each takes every fourth group of positions, keeps a three-stage ring of
 // its own in shared memory (cp.async, no barrier of the CTA in the loop), and its own running maximum, sum and output; the
@@ -55,7 +56,8 @@ struct PagedAttn {
   int n, n_new, hq, group, tiles;            // n_new: visible new slots (0 or n); tiles: query tiles per (sequence, head)
   float scale_log2;
   void* out;                                 // T [batch, n, hq, dh]
-  float *part_o, *part_ml;                   // [pieces][PG_ROWS][dh], [pieces][PG_ROWS][2]
+  float *part_o, *part_ml;                   // [2 * ctas][rows of an item][dh], the same [2]: pieces
+  float* whole_ml;                           // [items][PG_ROWS][2] of the items that were not cut, with score
   float* score; long long score_ld;          // [batch, hq, score_ld] scaled log2-domain scores, or null
   float* weight_out;                         // [batch, hkv, cap] or null
   int ctas;                                  // stretches the line is cut into at most
@@ -563,7 +565,8 @@ __global__ void __launch_bounds__(PG_THREADS, PG_WAVES) paged_rows_kernel(const 
     W.finish(so + warp * PG_ROWS * DH, sml + warp * PG_ROWS * 2);
     __syncthreads();
     const bool whole = t0 == 0 && t1 == T_b;
-    const long long piece = blockIdx.x + (long long)b * hm_n + hm;
+    const size_t piece = (size_t)blockIdx.x * 2 + (x == line_begin(L, blockIdx.x) ? 0 : 1);
+    float* const ml_at = whole ? (P.score ? P.whole_ml + ((size_t)b * hm_n + hm) * PG_ROWS * 2 : nullptr) : P.part_ml + piece * PG_ROWS * 2;
     for (int i = threadIdx.x; i < PG_ROWS * (DH / 4); i += PG_THREADS) {
       const int r = i / (DH / 4), c = i - r * (DH / 4);
       const int rr = mt * PG_ROWS + r;
@@ -590,12 +593,11 @@ __global__ void __launch_bounds__(PG_THREADS, PG_WAVES) paged_rows_kernel(const 
         else
           *reinterpret_cast<float4*>(dst) = make_float4(a.x * inv, a.y * inv, a.z * inv, a.w * inv);
       } else {
-        *reinterpret_cast<float4*>(P.part_o + ((size_t)piece * PG_ROWS + r) * DH + c * 4) = a;
+        *reinterpret_cast<float4*>(P.part_o + (piece * PG_ROWS + r) * DH + c * 4) = a;
       }
-      if (c == 0 && (!whole || P.score)) {
-        float* ml = P.part_ml + ((size_t)piece * PG_ROWS + r) * 2;
-        ml[0] = M;
-        ml[1] = S;
+      if (c == 0 && ml_at) {
+        ml_at[r * 2] = M;
+        ml_at[r * 2 + 1] = S;
       }
     }
     x += t1 - t0;
@@ -603,63 +605,90 @@ __global__ void __launch_bounds__(PG_THREADS, PG_WAVES) paged_rows_kernel(const 
   }
 }
 
+// The piece that CTA c holds of an item that begins at x0: its first place unless the item begins inside its stretch.
+__device__ __forceinline__ size_t piece_of(const PagedLine& L, int c, long long x0) { return (size_t)c * 2 + (line_begin(L, c) >= x0 ? 0 : 1); }
+
 // Joins the pieces of the items that a stretch's end cut, in the order of their positions; rows of sequences without any
-// position become zero. One CTA per query row at a time. Then the weights: weight_out = weight + sum over the group's heads of
-// exp2(score - max) / sum, slots 0 .. keys - 1, 256 slots per CTA at a time.
-template <typename T, int DH>
+// position become zero. Work: every end of a stretch times the rows of an item (ROWS), each for NW warps of a CTA that take
+// every NW-th piece and add their sums in warp order; an item that several ends cut belongs to the first of them. Then the
+// weights: weight_out = weight + sum over the group's heads of exp2(score - max) / sum, slots 0 .. keys - 1, 256 slots per CTA
+// at a time.
+template <typename T, int DH, int ROWS, int NW>
 __global__ void __launch_bounds__(128) paged_join_kernel(const PagedAttn P, int tile) {
   pdl_trigger();
   __shared__ PagedLine L;
-  __shared__ float s_m[128], s_l[128], red[40];
-  __shared__ float4 s_o[4][DH / 4];
+  __shared__ float s_m[128], s_l[128];
+  __shared__ float s_o[4][DH + 1];
   pdl_wait(KID_ATTN_MERGE);
   paged_line(L, P, tile);
   const int hm_n = P.c.hkv * P.tiles, R = P.n * P.group;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int n_rows = P.c.batch * P.c.hkv * R;
-  for (int w = blockIdx.x; w < n_rows; w += gridDim.x) {
-    const int b = w / (P.c.hkv * R), h = w / R % P.c.hkv, rr = w % R;
-    if (L.len[b] < 0) continue;
-    T* dst = (T*)P.out + (((size_t)b * P.n + rr / P.group) * P.hq + h * P.group + rr % P.group) * DH;
-    const long long T_b = L.pre[b + 1] - L.pre[b];
-    if (T_b == 0) {
-      for (int d = threadIdx.x; d < DH; d += 128) dst[d] = from_f<T>(0.f);
-      continue;
+  constexpr int DL = DH / 32, UNITS = 4 / NW;              // rows that a CTA joins side by side
+  const int sub = warp / NW, wq = warp % NW;
+  const long long n_units = (long long)(L.total > 0 ? L.ctas - 1 : 0) * ROWS;
+  for (long long w0 = (long long)blockIdx.x * UNITS; w0 < n_units; w0 += (long long)gridDim.x * UNITS) {
+    const long long w = w0 + sub;
+    const int c = (int)(w / ROWS) + 1, r = (int)(w % ROWS);
+    const long long x = w < n_units ? line_begin(L, c) : 0;
+    int b = 0, hm = 0;
+    long long x0 = 0, T_b = 1;
+    bool todo = w < n_units;
+    if (todo) {
+      int hi = PG_MAX_SEQ;                                 // the sequence that holds tile x: pre[b] * hm_n <= x < pre[b + 1] * hm_n
+      while (hi - b > 1) {
+        const int mid = (b + hi) >> 1;
+        if (L.pre[mid] * hm_n <= x) b = mid; else hi = mid;
+      }
+      T_b = L.pre[b + 1] - L.pre[b];
+      hm = (int)((x - L.pre[b] * hm_n) / T_b);
+      x0 = L.pre[b] * hm_n + hm * T_b;
+      todo = x != x0 && line_owner(L, x0) == c - 1 && hm % P.tiles * ROWS + r < R;
     }
-    const int hm = h * P.tiles + rr / PG_ROWS, r = rr % PG_ROWS;
-    const long long x0 = L.pre[b] * hm_n + (long long)hm * T_b;
-    const int c0 = line_owner(L, x0), c1 = line_owner(L, x0 + T_b - 1);
-    if (c0 == c1) continue;                                          // written whole
-    const size_t p0 = (size_t)c0 + (size_t)b * hm_n + hm;
-    const int np = c1 - c0 + 1;
-    float M = -INFINITY;
-    for (int i = threadIdx.x; i < np; i += 128) M = fmaxf(M, P.part_ml[((p0 + i) * PG_ROWS + r) * 2]);
-    M = block_max(M, red);
-    const float sub = M == -INFINITY ? 0.f : M;
-    // warp w takes pieces w, w + 4, ...; the four sums are added in warp order
-    float S = 0.f;
-    constexpr int DL = DH / 32;
-    float a[DL];
+    float S = 0.f, a[DL];
 #pragma unroll
     for (int d = 0; d < DL; ++d) a[d] = 0.f;
-    for (int i = warp; i < np; i += 4) {
-      const float* ml = P.part_ml + ((p0 + i) * PG_ROWS + r) * 2;
-      const float f = exp2f(ml[0] - sub);
-      S = fmaf(f, ml[1], S);
-      const float* o = P.part_o + ((p0 + i) * PG_ROWS + r) * DH + lane * DL;
+    if (todo) {
+      const int c1 = line_owner(L, x0 + T_b - 1);
+      float M = -INFINITY;
+      for (int i = c - 1 + lane; i <= c1; i += 32) M = fmaxf(M, P.part_ml[(piece_of(L, i, x0) * ROWS + r) * 2]);
+      M = warp_max(M);
+      const float ref = M == -INFINITY ? 0.f : M;
+      for (int i = c - 1 + wq; i <= c1; i += NW) {
+        const size_t at = piece_of(L, i, x0) * ROWS + r;
+        const float f = exp2f(P.part_ml[at * 2] - ref);
+        S = fmaf(f, P.part_ml[at * 2 + 1], S);
 #pragma unroll
-      for (int d = 0; d < DL; ++d) a[d] = fmaf(f, o[d], a[d]);
+        for (int d = 0; d < DL; ++d) a[d] = fmaf(f, P.part_o[at * DH + lane * DL + d], a[d]);
+      }
     }
-    float* so = reinterpret_cast<float*>(s_o);
+    if constexpr (NW > 1) {
+      __syncthreads();
+      if (wq > 0) {
 #pragma unroll
-    for (int d = 0; d < DL; ++d) so[warp * DH + lane * DL + d] = a[d];
-    if (lane == 0) s_l[warp] = S;
-    __syncthreads();
-    const float St = s_l[0] + s_l[1] + s_l[2] + s_l[3];
-    const float inv = St == 0.f ? 0.f : 1.f / St;
-    for (int d = threadIdx.x; d < DH; d += 128)
-      dst[d] = from_f<T>(St == 0.f ? 0.f : (so[d] + so[DH + d] + so[2 * DH + d] + so[3 * DH + d]) * inv);
-    __syncthreads();
+        for (int d = 0; d < DL; ++d) s_o[warp][lane * DL + d] = a[d];
+        if (lane == 0) s_o[warp][DH] = S;
+      }
+      __syncthreads();
+      if (wq == 0) {
+        for (int k = 1; k < NW; ++k) {
+#pragma unroll
+          for (int d = 0; d < DL; ++d) a[d] += s_o[warp + k][lane * DL + d];
+          S += s_o[warp + k][DH];
+        }
+      }
+    }
+    if (todo && wq == 0) {
+      const int rr = hm % P.tiles * ROWS + r;
+      T* dst = (T*)P.out + (((size_t)b * P.n + rr / P.group) * P.hq + hm / P.tiles * P.group + rr % P.group) * DH + lane * DL;
+      const float inv = S == 0.f ? 0.f : 1.f / S;
+#pragma unroll
+      for (int d = 0; d < DL; ++d) dst[d] = from_f<T>(S == 0.f ? 0.f : a[d] * inv);
+    }
+  }
+  for (int b = blockIdx.x; b < P.c.batch; b += gridDim.x) {
+    if (L.len[b] < 0 || L.pre[b + 1] != L.pre[b]) continue;
+    T* dst = (T*)P.out + (size_t)b * P.n * P.hq * DH;
+    for (int d = threadIdx.x; d < P.n * P.hq * DH; d += 128) dst[d] = from_f<T>(0.f);
   }
   if (!P.weight_out) return;
   // weights: chunks of 256 slots of every (sequence, head), counted along the lengths
@@ -684,12 +713,21 @@ __global__ void __launch_bounds__(128) paged_join_kernel(const PagedAttn P, int 
     for (int g = threadIdx.x; g < P.group; g += 128) {              // the heads' maximum and sum over their pieces
       const int hm = h * P.tiles + g / PG_ROWS, r = g % PG_ROWS;
       const long long x0 = L.pre[b] * hm_n + (long long)hm * T_b;
-      const int c0 = line_owner(L, x0), np = line_owner(L, x0 + T_b - 1) - c0 + 1;
-      const float* ml = P.part_ml + (((size_t)c0 + (size_t)b * hm_n + hm) * PG_ROWS + r) * 2;
-      float M = -INFINITY, S = 0.f;
-      for (int i = 0; i < np; ++i) M = fmaxf(M, ml[(size_t)i * PG_ROWS * 2]);
-      const float sub = M == -INFINITY ? 0.f : M;
-      for (int i = 0; i < np; ++i) S = fmaf(exp2f(ml[(size_t)i * PG_ROWS * 2] - sub), ml[(size_t)i * PG_ROWS * 2 + 1], S);
+      const int c0 = line_owner(L, x0), c1 = line_owner(L, x0 + T_b - 1);
+      float M = -INFINITY, S = 0.f, sub;
+      if (c0 == c1) {
+        const float* ml = P.whole_ml + (((size_t)b * hm_n + hm) * PG_ROWS + r) * 2;
+        M = ml[0];
+        S = ml[1];
+        sub = M == -INFINITY ? 0.f : M;
+      } else {
+        for (int i = c0; i <= c1; ++i) M = fmaxf(M, P.part_ml[(piece_of(L, i, x0) * PG_ROWS + r) * 2]);
+        sub = M == -INFINITY ? 0.f : M;
+        for (int i = c0; i <= c1; ++i) {
+          const float* ml = P.part_ml + (piece_of(L, i, x0) * PG_ROWS + r) * 2;
+          S = fmaf(exp2f(ml[0] - sub), ml[1], S);
+        }
+      }
       s_m[g] = sub;
       s_l[g] = S == 0.f ? 0.f : 1.f / S;
     }
@@ -705,11 +743,11 @@ __global__ void __launch_bounds__(128) paged_join_kernel(const PagedAttn P, int 
   }
 }
 
-// Writes rows i < n_new[b] of k_new / v_new [batch, n, hkv, dh] (row_stride elements apart) to slots len[b] + i.
-// 16 bytes per thread.
+// Writes rows i < n_new[b] of k_new / v_new [batch, n, hkv, dh] (row_stride elements apart) to slots len[b] + i; with mask
+// [batch, n] only those that some row sees. 16 bytes per thread.
 template <typename T>
 __global__ void __launch_bounds__(256) paged_append_kernel(PagedView C, const T* k_new, const T* v_new, long long row_stride, int n,
-                                                           const int* n_new, int dh) {
+                                                           const int* n_new, const unsigned long long* mask, int dh) {
   pdl_trigger();
   pdl_wait(KID_APPEND);
   constexpr int E = 16 / sizeof(T);
@@ -717,13 +755,18 @@ __global__ void __launch_bounds__(256) paged_append_kernel(PagedView C, const T*
   const int len = C.len[b];
   if (len < 0) return;
   const int rows = n_new ? min(n, n_new[b]) : n;
+  unsigned long long any = ~0ull;
+  if (mask) {                                                        // n <= 64
+    any = 0ull;
+    for (int i = 0; i < n; ++i) any |= __ldg(mask + (size_t)b * n + i);
+  }
   for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < (long long)rows * per; i += (long long)gridDim.x * blockDim.x) {
     const int r = (int)(i / per), c = (int)(i - (long long)r * per);
     const long long slot = (long long)len + r;
     if (slot >= C.cap()) continue;
     const long long o = C.row(b, slot, dh);
     const size_t src = (size_t)((long long)b * n + r) * (size_t)row_stride + (size_t)c * E;
-    if (o >= 0) {
+    if (o >= 0 && (!mask || ((any >> r) & 1ull))) {
       *reinterpret_cast<uint4*>((T*)C.k + o + (long long)c * E) = __ldg(reinterpret_cast<const uint4*>(k_new + src));
       *reinterpret_cast<uint4*>((T*)C.v + o + (long long)c * E) = __ldg(reinterpret_cast<const uint4*>(v_new + src));
     }
