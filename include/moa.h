@@ -321,8 +321,10 @@ moa_status moa_paged_append(const moa_paged_cache *cache, const void *k_new, con
  *   weight_out  device float [batch, hkv, max_pages * page_size], may be cache->weight, or NULL; n = 1 only: for every slot
  *               that the row sees, cache->weight (0 for the new slot, or without it) + the sum over the group's query heads
  *               of the softmax weights. Other entries stay as they were.
- *   ws          device scratch of moa_paged_workspace_bytes bytes (its contents need not be kept or zeroed)
- * Scores, statistics and sums are fp32. hq / hkv <= 128. */
+ *   ws          device scratch of moa_paged_workspace_bytes bytes. ZERO IT ONCE after allocating it: its first bytes count the
+ *               parts of the work that have been joined, and a call leaves them at zero again
+ * Scores, statistics and sums are fp32. hq / hkv <= 128; batch * hkv * (n * hq / hkv / 16, rounded up) * (max_pages * page_size
+ * / 64) <= 2^30. */
 moa_status moa_paged_workspace_bytes(const moa_paged_cache *cache, int32_t n, int32_t hq, int32_t weights, size_t *bytes);
 moa_status moa_paged_attention(const moa_paged_cache *cache, const void *q, int64_t q_stride, const void *k_new, const void *v_new,
                                int64_t new_stride, int32_t n, int32_t n_new, int32_t hq, const uint64_t *mask, float scale, void *out,

@@ -10,24 +10,24 @@
 // Work split (paged_rows_kernel): the (sequence, head, query tile) items are laid end to end as tiles of positions, and
 // the CTAs take equal consecutive stretches of that line, whatever the sequences' lengths are; the lengths are read on
 // the device, so a captured graph follows them. A stretch may end inside an item: such an item is left in pieces
-// (max, sum, unnormalised output) and paged_join_kernel adds them in the order of their positions, the same order on every
-// run. Only the first and the last item of a stretch can be cut, so a CTA has two places for pieces: the first for the item
-// its stretch begins in, the second for the one it ends in.
+// (max, sum, unnormalised output), and the CTA that delivers an item's last piece adds them all in the order of their
+// positions, the same order on every run. Only the first and the last item of a stretch can be cut, so a CTA has two places
+// for pieces: the first for the item its stretch begins in, the second for the one it ends in.
 //
-// Inside a CTA the four warps run on their own: each takes every fourth group of positions, keeps a three-stage ring of
-// its own in shared memory (cp.async, no barrier of the CTA in the loop), and its own running maximum, sum and output; the
-// four are merged once per item.
+// Inside a CTA (one per SM) the eight warps run on their own: each takes every eighth group of positions of the stretch and
+// keeps a three-stage ring of its own in shared memory (cp.async, no barrier of the CTA in the loop), with its own running
+// maximum, sum and output. The copies run two steps ahead, across the items' borders; at an item's end the warps' states
+// are merged through the ring stage that was read last, while the other two fill.
 #pragma once
 #include "moa_attn.cuh"
 
 namespace moa {
 
-constexpr int PG_WARPS = 4;
+constexpr int PG_WARPS = 8;
 constexpr int PG_THREADS = PG_WARPS * 32;
 constexpr int PG_STAGES = 3;
 constexpr int PG_ROWS = 16;                  // query rows per tile
 constexpr int PG_MAX_SEQ = 64;               // sequences per call
-constexpr int PG_WAVES = 2;                  // CTAs per SM
 
 // The cache of one layer as the kernels see it. T [n_pages, page_size, hkv, dh], pages page_stride elements apart.
 struct PagedView {
@@ -57,39 +57,41 @@ struct PagedAttn {
   float scale_log2;
   void* out;                                 // T [batch, n, hq, dh]
   float *part_o, *part_ml;                   // [2 * ctas][rows of an item][dh], the same [2]: pieces
-  float* whole_ml;                           // [items][PG_ROWS][2] of the items that were not cut, with score
+  float* item_ml;                            // [items][PG_ROWS][2]: max and sum of every item, with score
+  int* arrived;                              // [ctas]: pieces delivered of the item that is cut first at the end of a CTA's stretch; zero between calls
   float* score; long long score_ld;          // [batch, hq, score_ld] scaled log2-domain scores, or null
   float* weight_out;                         // [batch, hkv, cap] or null
   int ctas;                                  // stretches the line is cut into at most
   int min_tiles;                             // ... and the least tiles of one
 };
 
-// The line of work. tiles_of(b) position tiles per item of sequence b; pre[b] = items' tiles before sequence b, per item.
+// The line of work: item (b, hm) of sequence b, hm = head * tiles + query tile, has tiles_of(b) tiles of positions and begins
+// at pre[b] * hm_n + hm * tiles_of(b). The host keeps the whole line below 2^31 tiles.
 struct PagedLine {
-  long long pre[PG_MAX_SEQ + 1];
+  int pre[PG_MAX_SEQ + 1];                   // tiles per item, summed over the sequences before b
   int len[PG_MAX_SEQ];
-  long long total;                           // tiles of the whole line
-  int ctas;
+  int total, ctas, q, r;                     // tiles of the line; the first r of `ctas` stretches have q + 1 tiles, the others q
 };
 
 // Every thread of the CTA calls it; ends with a barrier.
 __device__ __forceinline__ void paged_line(PagedLine& L, const PagedAttn& P, int tile) {
   if (threadIdx.x < 32) {
     const int lane = threadIdx.x;
-    long long own[2], sum = 0;
+    int own[2], sum = 0;
+    const int cap = (int)P.c.cap();
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       const int b = lane * 2 + u;
-      const int len = b < P.c.batch ? P.c.len[b] : -1;
-      if (b < PG_MAX_SEQ) L.len[b] = (int)min((long long)len, P.c.cap());
-      const long long keys = len < 0 ? 0 : min((long long)len + P.n_new, P.c.cap());
+      const int len = b < P.c.batch ? min(P.c.len[b], cap) : -1;
+      L.len[b] = len;
+      const int keys = len < 0 ? 0 : min(len + P.n_new, cap);
       own[u] = (keys + tile - 1) / tile;
       sum += own[u];
     }
-    long long inc = sum;
+    int inc = sum;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-      const long long t = __shfl_up_sync(0xffffffffu, inc, o);
+      const int t = __shfl_up_sync(0xffffffffu, inc, o);
       if (lane >= o) inc += t;
     }
     L.pre[lane * 2] = inc - sum;
@@ -97,15 +99,49 @@ __device__ __forceinline__ void paged_line(PagedLine& L, const PagedAttn& P, int
     if (lane == 31) {
       L.pre[PG_MAX_SEQ] = inc;
       L.total = inc * P.c.hkv * P.tiles;
-      const long long most = (L.total + P.min_tiles - 1) / P.min_tiles;
-      L.ctas = (int)max(1ll, min((long long)P.ctas, most));
+      L.ctas = max(1, min(P.ctas, (L.total + P.min_tiles - 1) / P.min_tiles));
+      L.q = L.total / L.ctas;
+      L.r = L.total - L.q * L.ctas;
     }
   }
   __syncthreads();
 }
-__device__ __forceinline__ long long line_begin(const PagedLine& L, int cta) { return L.total * cta / L.ctas; }
-// the CTA whose stretch holds tile x: the i with total*i/ctas <= x < total*(i+1)/ctas (rounded down)
-__device__ __forceinline__ int line_owner(const PagedLine& L, long long x) { return (int)(((x + 1) * L.ctas - 1) / L.total); }
+__device__ __forceinline__ int line_begin(const PagedLine& L, int cta) { return L.q * cta + min(cta, L.r); }
+// the CTA whose stretch holds tile x < total
+__device__ __forceinline__ int line_owner(const PagedLine& L, int x) {
+  const int wide = L.r * (L.q + 1);
+  return x < wide ? x / (L.q + 1) : L.r + (x - wide) / L.q;
+}
+// The piece that CTA c holds of an item that begins at x0: its first place unless the item begins inside its stretch.
+__device__ __forceinline__ int piece_of(const PagedLine& L, int c, int x0) { return c * 2 + (line_begin(L, c) >= x0 ? 0 : 1); }
+
+// A place on the line: tile t of item (b, h, mt).
+struct PagedPlace {
+  int b, h, mt, t, T_b;
+  __device__ __forceinline__ void at(const PagedLine& L, const PagedAttn& P, int x) {
+    const int hm_n = P.c.hkv * P.tiles;
+    while (x >= L.pre[b + 1] * hm_n) ++b;
+    T_b = L.pre[b + 1] - L.pre[b];
+    const int in_b = x - L.pre[b] * hm_n, hm = in_b / T_b;
+    h = hm / P.tiles;
+    mt = hm - h * P.tiles;
+    t = in_b - hm * T_b;
+  }
+};
+
+// Which of the new slots some row sees: the others are not read at all (what lies there may be anything).
+__device__ __forceinline__ unsigned long long causal_word(int i) { return i >= 63 ? ~0ull : (2ull << i) - 1ull; }
+__device__ __forceinline__ unsigned long long any_word(const PagedAttn& P, int b) {          // a whole warp
+  if (!P.mask) return causal_word(P.n - 1);
+  const int lane = threadIdx.x & 31;
+  const unsigned long long* m = P.mask + (size_t)b * P.n;
+  unsigned long long a = lane < P.n ? __ldg(m + lane) : 0ull;
+  if (lane + 32 < P.n) a |= __ldg(m + lane + 32);
+  return ((unsigned long long)__reduce_or_sync(0xffffffffu, (unsigned)(a >> 32)) << 32) | __reduce_or_sync(0xffffffffu, (unsigned)a);
+}
+__device__ __forceinline__ unsigned long long row_word(const PagedAttn& P, int b, int i) {
+  return P.mask ? __ldg(P.mask + (size_t)b * P.n + i) : causal_word(i);
+}
 
 // One warp's running state over a 16-row query tile, merged over the CTA's warps at the end of an item.
 // (max in the log2 domain, sum, output) of row r, all in fp32.
@@ -150,11 +186,24 @@ struct PagedWarp<bf16, DH> {
     l[0] = l[1] = 0.f;
   }
 
-  // One step: 16 positions from `base` on, keys at sK, values at sV. live: bit per position that exists; see(u, j): whether
-  // row u of this thread sees position j of the step; plain: every row sees every position.
+  unsigned long long word[2];                // mask words of this thread's two rows
+  __device__ __forceinline__ bool words(const PagedAttn& P, int b, int mt, int R) {
+    bool full = true;
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const int rr = mt * PG_ROWS + gq + 8 * u;
+      word[u] = rr < R ? row_word(P, b, rr / P.group) : 0ull;
+      full = full && (rr >= R || word[u] != 0ull);
+    }
+    return __all_sync(0xffffffffu, full);
+  }
+
+  // One step: 16 positions, keys at K, values at V. see(w, j): whether a row with mask word w sees position j of the step;
+  // plain: every row sees every position. score: the tile's first row of scores, or null.
   template <typename See>
-  __device__ __forceinline__ void step(const PagedAttn& P, uint32_t sK, uint32_t sV, bool plain, See see, float* score0, float* score1) {
+  __device__ __forceinline__ void step(const PagedAttn& P, const uint8_t* K, const uint8_t* V, bool plain, See see, float* score, int, int mt, int R) {
     const int lane = threadIdx.x & 31;
+    const uint32_t sK = smem_u32(K), sV = smem_u32(V);
     float s[2][2][4];                        // [chain][8 positions][fragment]: two chains halve the products' latency
 #pragma unroll
     for (int c = 0; c < 2; ++c)
@@ -181,15 +230,16 @@ struct PagedWarp<bf16, DH> {
       for (int u = 0; u < 2; ++u)
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-          if (!see(u, (i >> 1) * 8 + 2 * tq + (i & 1))) z[u][i] = -INFINITY;
+          if (!see(word[u], (i >> 1) * 8 + 2 * tq + (i & 1))) z[u][i] = -INFINITY;
     }
-    if (score0) {                            // the row's scores, for the accumulated weights
-      *reinterpret_cast<float2*>(score0 + 2 * tq) = make_float2(z[0][0], z[0][1]);
-      *reinterpret_cast<float2*>(score0 + 8 + 2 * tq) = make_float2(z[0][2], z[0][3]);
-    }
-    if (score1) {
-      *reinterpret_cast<float2*>(score1 + 2 * tq) = make_float2(z[1][0], z[1][1]);
-      *reinterpret_cast<float2*>(score1 + 8 + 2 * tq) = make_float2(z[1][2], z[1][3]);
+    if (score) {                             // one token: row = head of the group; for the accumulated weights
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+        if (mt * PG_ROWS + gq + 8 * u < R) {
+          float* at = score + (gq + 8 * u) * P.score_ld + 2 * tq;
+          *reinterpret_cast<float2*>(at) = make_float2(z[u][0], z[u][1]);
+          *reinterpret_cast<float2*>(at + 8) = make_float2(z[u][2], z[u][3]);
+        }
     }
     float f[2];
 #pragma unroll
@@ -245,7 +295,6 @@ struct PagedWarp<bf16, DH> {
         *reinterpret_cast<float2*>(so + r * DH + i * 8 + 2 * tq) = make_float2(o[i][2 * u], o[i][2 * u + 1]);
     }
   }
-  __device__ __forceinline__ int row_of(int u) const { return gq + 8 * u; }
 };
 
 // ---------------------------------------------------------------------------------------------
@@ -258,9 +307,8 @@ struct PagedWarp<float, DH> {
   static constexpr int KW = 8;
   static constexpr int DL = DH / 32;         // output columns per lane
   float o[PG_ROWS][DL];
-  float m[PG_ROWS / 8], l[PG_ROWS / 8];      // lane's rows for the statistics: lane / 8 ... see step()
   float *sq, *sp;                            // queries [16][DH] of the CTA, this warp's probabilities [8][16]
-  int rows;
+  int rows;                                  // query rows of this tile
 
   // Shared memory behind the rings: queries of the item [16][DH], then per warp probabilities [KW][PG_ROWS] and factors [16].
   static constexpr int SMEM = (PG_ROWS * DH + PG_WARPS * (KW + 1) * PG_ROWS) * 4;
@@ -293,8 +341,13 @@ struct PagedWarp<float, DH> {
   // 16-byte chunk of a row, swizzled by the row
   static __device__ __forceinline__ uint32_t off(int row, int chunk) { return (uint32_t)(row * (DH * 4) + ((chunk ^ (row & 7)) << 4)); }
 
+  __device__ __forceinline__ bool words(const PagedAttn& P, int b, int mt, int R) {
+    const int rr = mt * PG_ROWS + (threadIdx.x & 15);
+    return __all_sync(0xffffffffu, rr >= R || row_word(P, b, rr / P.group) != 0ull);
+  }
+
   template <typename See>
-  __device__ __forceinline__ void step(const PagedAttn& P, const uint8_t* K, const uint8_t* V, bool plain, See see, float* score, long long score_ld) {
+  __device__ __forceinline__ void step(const PagedAttn& P, const uint8_t* K, const uint8_t* V, bool plain, See see, float* score, int b, int mt, int) {
     const int lane = threadIdx.x & 31;
     const int kk = lane & 7, quarter = lane >> 3;
     float acc[PG_ROWS];
@@ -319,7 +372,7 @@ struct PagedWarp<float, DH> {
       float t = acc[r];
       t += __shfl_xor_sync(0xffffffffu, t, 8);
       t += __shfl_xor_sync(0xffffffffu, t, 16);
-      if (quarter == (r & 3)) sp[kk * PG_ROWS + r] = (plain || see(r, kk)) ? t * P.scale_log2 : -INFINITY;
+      if (quarter == (r & 3)) sp[kk * PG_ROWS + r] = (plain || see(row_word(P, b, (mt * PG_ROWS + r) / P.group), kk)) ? t * P.scale_log2 : -INFINITY;
     }
     __syncwarp();
     // softmax statistics: lane r of each half-warp holds row r
@@ -333,7 +386,7 @@ struct PagedWarp<float, DH> {
       }
       if (score && lane < 16 && r < rows) {
 #pragma unroll
-        for (int k = 0; k < KW; k += 4) *reinterpret_cast<float4*>(score + r * score_ld + k) = make_float4(z[k], z[k + 1], z[k + 2], z[k + 3]);
+        for (int k = 0; k < KW; k += 4) *reinterpret_cast<float4*>(score + r * P.score_ld + k) = make_float4(z[k], z[k + 1], z[k + 2], z[k + 3]);
       }
       const float mn = fmaxf(mrow, mx);
       const float f = mn == mrow ? 1.f : exp2f(mrow - mn);
@@ -402,139 +455,128 @@ template <typename T, int DH> struct PagedCfg {
   static constexpr int CH = DH / E;                             // 16-byte chunks per row
   static constexpr int ROW_BYTES = DH * (int)sizeof(T);
   static constexpr int HALF = KW * ROW_BYTES;                   // a warp's keys (or values) of one stage
-  static constexpr int RING = PG_WARPS * PG_STAGES * 2 * HALF;
-  static constexpr int MERGE = PG_WARPS * PG_ROWS * (DH + 2) * 4;     // lies over the rings
-  static constexpr int EXTRA = sizeof(T) == 4 ? (PG_ROWS * DH + PG_WARPS * (8 + 1) * PG_ROWS) * 4 : 0;
-  static constexpr int SMEM = (RING > MERGE ? RING : MERGE) + EXTRA;
+  static constexpr int STAGE = 2 * HALF;
+  static constexpr int RING = PG_STAGES * STAGE;                // of one warp
+  static constexpr int EXTRA = sizeof(T) == 4 ? PagedWarp<float, DH>::SMEM : 0;
+  static constexpr int SMEM = PG_WARPS * RING + EXTRA;
+  static_assert(STAGE == PG_ROWS * DH * 4, "a warp's output takes one stage of its ring");
 };
 
-// Union of the rows' masks: a new slot that no row sees is not read at all (what lies there may be anything).
-__device__ __forceinline__ unsigned long long causal_word(int i) { return i >= 63 ? ~0ull : (2ull << i) - 1ull; }
+template <typename T>
+__device__ __forceinline__ void store4(T* dst, const float4 a) {
+  if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16(a.x, a.y), pack_bf16(a.z, a.w));
+  else *reinterpret_cast<float4*>(dst) = a;
+}
 
 template <typename T, int DH>
-__global__ void __launch_bounds__(PG_THREADS, PG_WAVES) paged_rows_kernel(const PagedAttn P) {
+__global__ void __launch_bounds__(PG_THREADS, 1) paged_rows_kernel(const PagedAttn P) {
   using C = PagedCfg<T, DH>;
   pdl_trigger();
   extern __shared__ __align__(128) uint8_t pg_smem[];
   __shared__ PagedLine L;
-  __shared__ unsigned long long row_mask[64];
   __shared__ unsigned int live_of[PG_WARPS][PG_STAGES];
+  __shared__ float sml[PG_WARPS][PG_ROWS][2];
+  __shared__ int s_last;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  uint8_t* const extra = pg_smem + (C::SMEM - C::EXTRA);
-  uint8_t* const ring = pg_smem + warp * (PG_STAGES * 2 * C::HALF);
+  uint8_t* const extra = pg_smem + PG_WARPS * C::RING;
+  uint8_t* const ring = pg_smem + warp * C::RING;
   const uint32_t ring_s = smem_u32(ring);
   pdl_wait(KID_ATTN);
   paged_line(L, P, C::TILE);
-  if ((int)blockIdx.x >= L.ctas || L.total == 0) return;
-  const long long x_end = line_begin(L, blockIdx.x + 1);
-  const int hm_n = P.c.hkv * P.tiles;
+  const int total = L.total;
+  if (total == 0 || (int)blockIdx.x >= L.ctas) return;
+  const int x_begin = line_begin(L, blockIdx.x), x_end = line_begin(L, blockIdx.x + 1);
   const int R = P.n * P.group;
-  PagedWarp<T, DH> W;
+  const int cap = (int)P.c.cap();
 
-  int b = 0;
-  for (long long x = line_begin(L, blockIdx.x); x < x_end;) {
-    while (x >= L.pre[b + 1] * hm_n) ++b;
-    const long long T_b = L.pre[b + 1] - L.pre[b];
-    const long long in_b = x - L.pre[b] * hm_n;
-    const int hm = (int)(in_b / T_b);
-    const int h = hm / P.tiles, mt = hm - h * P.tiles;
-    const long long t0 = in_b - hm * T_b, t1 = min(T_b, t0 + (x_end - x));
-    const int len = L.len[b];
-    const long long keys = min((long long)len + P.n_new, P.c.cap());
-
-    // masks of the sequence's rows; any: some row sees the slot
-    unsigned long long any = 0ull;
-    bool full_rows = true;                                           // every row sees the committed slots
-    if (P.mask) {
-      if (threadIdx.x < P.n) row_mask[threadIdx.x] = P.mask[(size_t)b * P.n + threadIdx.x];
-      __syncthreads();
-      for (int i = 0; i < P.n; ++i) { any |= row_mask[i]; full_rows = full_rows && row_mask[i] != 0ull; }
-    } else {
-      any = causal_word(P.n - 1);
+  // ---- copies: place of the next step that is asked for, two steps ahead of the one that is worked on ----
+  PagedPlace F;
+  F.b = 0;
+  F.at(L, P, x_begin);
+  int f_x = x_begin, f_len = L.len[F.b], f_keys = min(f_len + P.n_new, cap);
+  unsigned long long f_any = any_word(P, F.b);
+  const int ch = lane % C::CH, r_first = lane / C::CH;
+  constexpr int R_STEP = 32 / C::CH;
+  // A step's rows -> this warp's ring. A row that does not exist is zero-filled: zero times what lies there may not be zero.
+  auto issue = [&](int st) {
+    const int base = F.t * C::TILE + warp * C::KW, key = base + lane;
+    const uint32_t dK = ring_s + st * C::STAGE, dV = dK + C::HALF;
+    long long off = 0;
+    int src = 0;                                                   // 0: does not exist, 1: page, 2: new row
+    if (lane < C::KW && key < f_keys) {
+      if (key >= f_len && !((f_any >> (key - f_len)) & 1ull)) {
+        src = 0;
+      } else if (key >= f_len && P.k_new) {
+        src = 2;
+        off = ((long long)F.b * P.n + (key - f_len)) * P.new_stride + (long long)F.h * DH;
+      } else {
+        off = P.c.row(F.b, key, DH);
+        src = off >= 0 ? 1 : 0;
+        off += (long long)F.h * DH;
+      }
     }
-    W.start(P, b, h, mt, extra);
-
-    const int ch = lane % C::CH, r_first = lane / C::CH;
-    constexpr int R_STEP = 32 / C::CH;
-    // A step's rows -> this warp's ring. A row that does not exist is zero-filled: zero times what lies there may not be zero.
-    auto issue = [&](long long t, int st) {
-      const long long base = t * C::TILE + warp * C::KW;
-      const uint32_t dK = ring_s + st * 2 * C::HALF, dV = dK + C::HALF;
-      long long off = 0;
-      int src = 0;                                                   // 0: does not exist, 1: page, 2: new row
-      const long long key = base + lane;
-      if (lane < C::KW && key < keys) {
-        if (key >= len && !((any >> (key - len)) & 1ull)) {
-          src = 0;
-        } else if (key >= len && P.k_new) {
-          src = 2;
-          off = ((long long)b * P.n + (key - len)) * P.new_stride + (long long)h * DH;
-        } else {
-          off = P.c.row(b, key, DH);
-          src = off >= 0 ? 1 : 0;
-          off += (long long)h * DH;
-        }
-      }
-      const unsigned live = __ballot_sync(0xffffffffu, src != 0);
-      const unsigned fresh = __ballot_sync(0xffffffffu, src == 2);
-      if (lane == 0) live_of[warp][st] = live;
-      for (int r = r_first; r < C::KW; r += R_STEP) {
-        const long long o = __shfl_sync(0xffffffffu, off, r);
-        const bool ok = (live >> r) & 1u, nw = (fresh >> r) & 1u;
-        const T* kp = (const T*)(nw ? P.k_new : P.c.k) + (ok ? o : 0) + ch * C::E;
-        const T* vp = (const T*)(nw ? P.v_new : P.c.v) + (ok ? o : 0) + ch * C::E;
-        const uint32_t d = (uint32_t)(r * C::ROW_BYTES + ((ch ^ (r & 7)) << 4));
-        cp_async16(dK + d, kp, ok);
-        cp_async16(dV + d, vp, ok);
-      }
-    };
+    const unsigned live = __ballot_sync(0xffffffffu, src != 0), fresh = __ballot_sync(0xffffffffu, src == 2);
+    if (lane == 0) live_of[warp][st] = live;
 #pragma unroll
-    for (int st = 0; st < PG_STAGES - 1; ++st) {
-      if (t0 + st < t1) issue(t0 + st, st);
-      cp_async_commit();
+    for (int r0 = 0; r0 < C::KW; r0 += R_STEP) {
+      const int r = r0 + r_first;
+      const long long o = __shfl_sync(0xffffffffu, off, r);
+      const bool ok = (live >> r) & 1u, nw = (fresh >> r) & 1u;
+      const T* kp = (const T*)(nw ? P.k_new : P.c.k) + (ok ? o : 0) + ch * C::E;
+      const T* vp = (const T*)(nw ? P.v_new : P.c.v) + (ok ? o : 0) + ch * C::E;
+      const uint32_t d = (uint32_t)(r * C::ROW_BYTES + ((ch ^ (r & 7)) << 4));
+      cp_async16(dK + d, kp, ok);
+      cp_async16(dV + d, vp, ok);
     }
-    int st = 0;
-    for (long long t = t0; t < t1; ++t) {
-      {
-        const int nst = st == 0 ? PG_STAGES - 1 : st - 1;            // the stage of the step before this one
-        if (t + PG_STAGES - 1 < t1) issue(t + PG_STAGES - 1, nst);
-        cp_async_commit();
-      }
+    ++f_x;
+    if (++F.t == F.T_b && f_x < x_end) {
+      F.at(L, P, f_x);
+      f_len = L.len[F.b];
+      f_keys = min(f_len + P.n_new, cap);
+      f_any = any_word(P, F.b);
+    }
+  };
+#pragma unroll
+  for (int st = 0; st < PG_STAGES - 1; ++st) {
+    if (f_x < x_end) issue(st);
+    cp_async_commit();
+  }
+
+  PagedWarp<T, DH> W;
+  PagedPlace S;
+  S.b = 0;
+  int st = 0;
+  for (int x = x_begin; x < x_end;) {
+    S.at(L, P, x);
+    const int b = S.b, h = S.h, mt = S.mt, t0 = S.t, t1 = min(S.T_b, t0 + (x_end - x));
+    const int x0 = x - t0;                                           // the item's first tile on the line
+    const int len = L.len[b], keys = min(len + P.n_new, cap);
+    W.start(P, b, h, mt, extra);
+    const bool full_rows = W.words(P, b, mt, R);                     // every row of this warp's tile sees the committed slots
+    for (int t = t0; t < t1; ++t) {
+      if (f_x < x_end) issue(st == 0 ? PG_STAGES - 1 : st - 1);      // the stage of the step before this one
+      cp_async_commit();
       cp_async_wait<PG_STAGES - 1>();
       __syncwarp();
-      const long long base = t * C::TILE + warp * C::KW;
+      const int base = t * C::TILE + warp * C::KW;
       const unsigned live = live_of[warp][st];
       if (live != 0u) {
-        uint8_t* sK = ring + st * 2 * C::HALF;
+        uint8_t* sK = ring + st * C::STAGE;
         uint8_t* sV = sK + C::HALF;
-        constexpr unsigned ALL = C::KW == 32 ? 0xffffffffu : (1u << C::KW) - 1u;
+        constexpr unsigned ALL = (1u << C::KW) - 1u;
         const bool plain = live == ALL && base + C::KW <= len && full_rows;
-        // whether query row r of the tile sees position base + j
-        auto sees = [&](int r, int j) -> bool {
-          const int rr = mt * PG_ROWS + r;
-          if (rr >= R || !((live >> j) & 1u)) return false;
-          const int i = rr / P.group;
-          const unsigned long long w = P.mask ? row_mask[i] : causal_word(i);
-          const long long key = base + j;
+        // whether a row with mask word w sees position base + j
+        auto sees = [&](unsigned long long w, int j) -> bool {
+          if (!((live >> j) & 1u)) return false;
+          const int key = base + j;
           return key < len ? w != 0ull : ((w >> (key - len)) & 1ull) != 0ull;
         };
-        if constexpr (sizeof(T) == 2) {
-          float *s0 = nullptr, *s1 = nullptr;
-          if (P.score) {                                             // one token: row = head of the group
-            const int r0 = mt * PG_ROWS + W.row_of(0), r1 = mt * PG_ROWS + W.row_of(1);
-            float* at = P.score + ((long long)b * P.hq + h * P.group) * P.score_ld + base;
-            if (r0 < R) s0 = at + r0 * P.score_ld;
-            if (r1 < R) s1 = at + r1 * P.score_ld;
-          }
-          W.step(P, smem_u32(sK), smem_u32(sV), plain, [&](int u, int j) { return sees(W.row_of(u), j); }, s0, s1);
-        } else {
-          float* at = P.score ? P.score + ((long long)b * P.hq + h * P.group + mt * PG_ROWS) * P.score_ld + base : nullptr;
-          W.step(P, sK, sV, plain, sees, at, P.score_ld);
-        }
+        float* at = P.score ? P.score + ((long long)b * P.hq + h * P.group + mt * PG_ROWS) * P.score_ld + base : nullptr;
+        W.step(P, sK, sV, plain, sees, at, b, mt, R);
         // the item's first query tile writes the new rows it holds to their pages
         if (P.k_new && mt == 0 && base + C::KW > len) {
           for (int r = r_first; r < C::KW; r += R_STEP) {
-            const long long key = base + r;
+            const int key = base + r;
             if (key < len || key >= keys || !((live >> r) & 1u)) continue;
             const long long o = P.c.row(b, key, DH);
             if (o < 0) continue;
@@ -543,202 +585,152 @@ __global__ void __launch_bounds__(PG_THREADS, PG_WAVES) paged_rows_kernel(const 
             *reinterpret_cast<uint4*>((T*)P.c.v + o + (long long)h * DH + ch * C::E) = *reinterpret_cast<const uint4*>(sV + d);
           }
         }
-        __syncwarp();
-      } else if (P.score) {                                          // nothing there: the weights' pass reads -inf
+      } else if (P.score && base < keys) {                           // nothing there: the weights' pass reads -inf
         for (int i = lane; i < C::KW * min(PG_ROWS, R - mt * PG_ROWS); i += 32)
           P.score[((long long)b * P.hq + h * P.group + mt * PG_ROWS + i / C::KW) * P.score_ld + base + i % C::KW] = -INFINITY;
       }
       if (P.k_new && mt == 0 && P.c.pos && base + C::KW > len && lane < C::KW) {
-        const long long key = base + lane;
+        const int key = base + lane;
         if (key >= len && key < keys) {
-          const size_t at = ((size_t)b * P.c.hkv + h) * (size_t)P.c.cap() + (size_t)key;
-          P.c.pos[at] = P.c.seen[b] + (int)(key - len);
+          const size_t at = ((size_t)b * P.c.hkv + h) * (size_t)cap + (size_t)key;
+          P.c.pos[at] = P.c.seen[b] + (key - len);
           P.c.weight[at] = 0.f;
         }
       }
-      st = st == PG_STAGES - 1 ? 0 : st + 1;
+      __syncwarp();
+      if (t + 1 < t1) st = st == PG_STAGES - 1 ? 0 : st + 1;
     }
-    cp_async_wait<0>();
-    __syncthreads();                                                 // the rings are free: the merge lies over them
-    float* so = reinterpret_cast<float*>(pg_smem);                   // [warp][16][DH]
-    float* sml = so + PG_WARPS * PG_ROWS * DH;                       // [warp][16][2]
-    W.finish(so + warp * PG_ROWS * DH, sml + warp * PG_ROWS * 2);
+    // ---- merge of the warps, through the stage that was read last ----
+    W.finish(reinterpret_cast<float*>(ring + st * C::STAGE), &sml[warp][0][0]);
     __syncthreads();
-    const bool whole = t0 == 0 && t1 == T_b;
-    const size_t piece = (size_t)blockIdx.x * 2 + (x == line_begin(L, blockIdx.x) ? 0 : 1);
-    float* const ml_at = whole ? (P.score ? P.whole_ml + ((size_t)b * hm_n + hm) * PG_ROWS * 2 : nullptr) : P.part_ml + piece * PG_ROWS * 2;
+    const bool whole = t0 == 0 && t1 == S.T_b;
+    const int item = (b * P.c.hkv + h) * P.tiles + mt;
+    const int c0 = whole ? 0 : line_owner(L, x0), c1 = whole ? 0 : line_owner(L, x0 + S.T_b - 1);
+    const size_t prow = (size_t)piece_of(L, blockIdx.x, x0) * PG_ROWS;
     for (int i = threadIdx.x; i < PG_ROWS * (DH / 4); i += PG_THREADS) {
       const int r = i / (DH / 4), c = i - r * (DH / 4);
       const int rr = mt * PG_ROWS + r;
       if (rr >= R) break;
-      float mw[PG_WARPS], M = -INFINITY;
+      float M = -INFINITY;
 #pragma unroll
-      for (int w = 0; w < PG_WARPS; ++w) { mw[w] = sml[(w * PG_ROWS + r) * 2]; M = fmaxf(M, mw[w]); }
-      const float sub = M == -INFINITY ? 0.f : M;
-      float S = 0.f;
+      for (int w = 0; w < PG_WARPS; ++w) M = fmaxf(M, sml[w][r][0]);
+      const float ref = M == -INFINITY ? 0.f : M;
+      float Z = 0.f;
       float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
       for (int w = 0; w < PG_WARPS; ++w) {
-        const float f = exp2f(mw[w] - sub);
-        S = fmaf(f, sml[(w * PG_ROWS + r) * 2 + 1], S);
-        const float4 y = *reinterpret_cast<const float4*>(so + (w * PG_ROWS + r) * DH + c * 4);
+        const float f = exp2f(sml[w][r][0] - ref);
+        Z = fmaf(f, sml[w][r][1], Z);
+        const float4 y = *reinterpret_cast<const float4*>(pg_smem + w * C::RING + st * C::STAGE + (r * DH + c * 4) * 4);
         a.x = fmaf(f, y.x, a.x); a.y = fmaf(f, y.y, a.y); a.z = fmaf(f, y.z, a.z); a.w = fmaf(f, y.w, a.w);
       }
       if (whole) {
-        if (S == 0.f) a = make_float4(0.f, 0.f, 0.f, 0.f);           // the row sees nothing
-        const float inv = S == 0.f ? 0.f : 1.f / S;                  // a NaN stays one
-        T* dst = (T*)P.out + (((size_t)b * P.n + rr / P.group) * P.hq + h * P.group + rr % P.group) * DH + c * 4;
-        if constexpr (sizeof(T) == 2)
-          *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16(a.x * inv, a.y * inv), pack_bf16(a.z * inv, a.w * inv));
-        else
-          *reinterpret_cast<float4*>(dst) = make_float4(a.x * inv, a.y * inv, a.z * inv, a.w * inv);
+        const float inv = Z == 0.f ? 0.f : 1.f / Z;                  // a row that sees nothing; a NaN stays one
+        if (Z == 0.f) a = make_float4(0.f, 0.f, 0.f, 0.f);
+        store4((T*)P.out + (((size_t)b * P.n + rr / P.group) * P.hq + h * P.group + rr % P.group) * DH + c * 4,
+               make_float4(a.x * inv, a.y * inv, a.z * inv, a.w * inv));
+        if (c == 0 && P.score) { P.item_ml[((size_t)item * PG_ROWS + r) * 2] = M; P.item_ml[((size_t)item * PG_ROWS + r) * 2 + 1] = Z; }
       } else {
-        *reinterpret_cast<float4*>(P.part_o + (piece * PG_ROWS + r) * DH + c * 4) = a;
+        __stcg(reinterpret_cast<float4*>(P.part_o + (prow + r) * DH + c * 4), a);
+        if (c == 0) __stcg(reinterpret_cast<float2*>(P.part_ml + (prow + r) * 2), make_float2(M, Z));
       }
-      if (c == 0 && ml_at) {
-        ml_at[r * 2] = M;
-        ml_at[r * 2 + 1] = S;
+    }
+    if (!whole) {
+      // ---- join: the CTA that delivers the item's last piece adds all of them ----
+      __threadfence();
+      __syncthreads();
+      if (threadIdx.x == 0) {
+        s_last = atomicAdd(P.arrived + c0, 1) == c1 - c0;
+        if (s_last) P.arrived[c0] = 0;                               // as the next call expects it
+      }
+      __syncthreads();
+      if (s_last) {
+        __threadfence();
+        for (int i = threadIdx.x; i < PG_ROWS * (DH / 4); i += PG_THREADS) {
+          const int r = i / (DH / 4), c = i - r * (DH / 4);
+          const int rr = mt * PG_ROWS + r;
+          if (rr >= R) break;
+          float M = -INFINITY, Z = 0.f;
+          float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+          // pieces in order, eight loads under way at a time; the sums move to a new reference when the maximum grows
+          for (int p0 = c0; p0 <= c1; p0 += 8) {
+            float2 ml[8];
+            float4 o[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+              const size_t at = (size_t)piece_of(L, min(p0 + u, c1), x0) * PG_ROWS + r;
+              ml[u] = __ldcg(reinterpret_cast<const float2*>(P.part_ml + at * 2));
+              o[u] = __ldcg(reinterpret_cast<const float4*>(P.part_o + at * DH + c * 4));
+            }
+            float mx = M;
+#pragma unroll
+            for (int u = 0; u < 8; ++u) mx = fmaxf(mx, ml[u].x);
+            const float ref = mx == -INFINITY ? 0.f : mx, g = exp2f(M - ref);
+            Z *= g;
+            a.x *= g; a.y *= g; a.z *= g; a.w *= g;
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+              if (p0 + u > c1) continue;
+              const float f = exp2f(ml[u].x - ref);
+              Z = fmaf(f, ml[u].y, Z);
+              a.x = fmaf(f, o[u].x, a.x); a.y = fmaf(f, o[u].y, a.y); a.z = fmaf(f, o[u].z, a.z); a.w = fmaf(f, o[u].w, a.w);
+            }
+            M = mx;
+          }
+          const float inv = Z == 0.f ? 0.f : 1.f / Z;
+          if (Z == 0.f) a = make_float4(0.f, 0.f, 0.f, 0.f);
+          store4((T*)P.out + (((size_t)b * P.n + rr / P.group) * P.hq + h * P.group + rr % P.group) * DH + c * 4,
+                 make_float4(a.x * inv, a.y * inv, a.z * inv, a.w * inv));
+          if (c == 0 && P.score) { P.item_ml[((size_t)item * PG_ROWS + r) * 2] = M; P.item_ml[((size_t)item * PG_ROWS + r) * 2 + 1] = Z; }
+        }
       }
     }
     x += t1 - t0;
-    __syncthreads();                                                 // the merge is read before the rings fill again
+    st = st == PG_STAGES - 1 ? 0 : st + 1;
+    __syncthreads();                                                 // the merge is read before its stage fills again
   }
 }
 
-// The piece that CTA c holds of an item that begins at x0: its first place unless the item begins inside its stretch.
-__device__ __forceinline__ size_t piece_of(const PagedLine& L, int c, long long x0) { return (size_t)c * 2 + (line_begin(L, c) >= x0 ? 0 : 1); }
-
-// Joins the pieces of the items that a stretch's end cut, in the order of their positions; rows of sequences without any
-// position become zero. Work: every end of a stretch times the rows of an item (ROWS), each for NW warps of a CTA that take
-// every NW-th piece and add their sums in warp order; an item that several ends cut belongs to the first of them. Then the
-// weights: weight_out = weight + sum over the group's heads of exp2(score - max) / sum, slots 0 .. keys - 1, 256 slots per CTA
-// at a time.
-template <typename T, int DH, int ROWS, int NW>
-__global__ void __launch_bounds__(128) paged_join_kernel(const PagedAttn P, int tile) {
+// Rows of sequences in use that have no position at all: zeros. One CTA per sequence, only where that can happen.
+template <typename T>
+__global__ void __launch_bounds__(256) paged_empty_kernel(T* out, const int* len, int batch, int per_seq) {
   pdl_trigger();
+  pdl_wait();
+  const int b = blockIdx.x;
+  if (len[b] != 0) return;
+  for (int d = threadIdx.x; d < per_seq; d += 256) out[(size_t)b * per_seq + d] = from_f<T>(0.f);
+}
+
+// weight_out = weight + sum over the group's heads of exp2(score - max) / sum, slots 0 .. keys - 1 of every (sequence, head),
+// 512 slots per CTA at a time.
+__global__ void __launch_bounds__(256) paged_weights_kernel(const PagedAttn P) {
+  pdl_trigger();
+  constexpr int CHUNK = 512;
   __shared__ PagedLine L;
-  __shared__ float s_m[128], s_l[128];
-  __shared__ float s_o[4][DH + 1];
-  pdl_wait(KID_ATTN_MERGE);
-  paged_line(L, P, tile);
-  const int hm_n = P.c.hkv * P.tiles, R = P.n * P.group;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  constexpr int DL = DH / 32, UNITS = 4 / NW;              // rows that a CTA joins side by side
-  const int sub = warp / NW, wq = warp % NW;
-  const long long n_units = (long long)(L.total > 0 ? L.ctas - 1 : 0) * ROWS;
-  for (long long w0 = (long long)blockIdx.x * UNITS; w0 < n_units; w0 += (long long)gridDim.x * UNITS) {
-    const long long w = w0 + sub;
-    const int c = (int)(w / ROWS) + 1, r = (int)(w % ROWS);
-    const long long x = w < n_units ? line_begin(L, c) : 0;
-    int b = 0, hm = 0;
-    long long x0 = 0, T_b = 1;
-    bool todo = w < n_units;
-    if (todo) {
-      int hi = PG_MAX_SEQ;                                 // the sequence that holds tile x: pre[b] * hm_n <= x < pre[b + 1] * hm_n
-      while (hi - b > 1) {
-        const int mid = (b + hi) >> 1;
-        if (L.pre[mid] * hm_n <= x) b = mid; else hi = mid;
-      }
-      T_b = L.pre[b + 1] - L.pre[b];
-      hm = (int)((x - L.pre[b] * hm_n) / T_b);
-      x0 = L.pre[b] * hm_n + hm * T_b;
-      todo = x != x0 && line_owner(L, x0) == c - 1 && hm % P.tiles * ROWS + r < R;
-    }
-    float S = 0.f, a[DL];
+  pdl_wait();
+  paged_line(L, P, CHUNK);                   // here a tile is a chunk of slots
+  const int cap = (int)P.c.cap(), n_chunks = L.pre[PG_MAX_SEQ] * P.c.hkv;
+  int b = 0;
+  for (int w = blockIdx.x; w < n_chunks; w += gridDim.x) {
+    while (w >= L.pre[b + 1] * P.c.hkv) ++b;
+    const int per = L.pre[b + 1] - L.pre[b], in_b = w - L.pre[b] * P.c.hkv, h = in_b / per;
+    const int slot0 = (in_b - h * per) * CHUNK, keys = min(L.len[b] + P.n_new, cap);
+    const size_t at = ((size_t)b * P.c.hkv + h) * (size_t)cap;
+    const float* score = P.score + ((long long)b * P.hq + h * P.group) * P.score_ld;
+    const float* ml = P.item_ml + (size_t)(b * P.c.hkv + h) * P.tiles * PG_ROWS * 2;
 #pragma unroll
-    for (int d = 0; d < DL; ++d) a[d] = 0.f;
-    if (todo) {
-      const int c1 = line_owner(L, x0 + T_b - 1);
-      float M = -INFINITY;
-      for (int i = c - 1 + lane; i <= c1; i += 32) M = fmaxf(M, P.part_ml[(piece_of(L, i, x0) * ROWS + r) * 2]);
-      M = warp_max(M);
-      const float ref = M == -INFINITY ? 0.f : M;
-      for (int i = c - 1 + wq; i <= c1; i += NW) {
-        const size_t at = piece_of(L, i, x0) * ROWS + r;
-        const float f = exp2f(P.part_ml[at * 2] - ref);
-        S = fmaf(f, P.part_ml[at * 2 + 1], S);
-#pragma unroll
-        for (int d = 0; d < DL; ++d) a[d] = fmaf(f, P.part_o[at * DH + lane * DL + d], a[d]);
-      }
-    }
-    if constexpr (NW > 1) {
-      __syncthreads();
-      if (wq > 0) {
-#pragma unroll
-        for (int d = 0; d < DL; ++d) s_o[warp][lane * DL + d] = a[d];
-        if (lane == 0) s_o[warp][DH] = S;
-      }
-      __syncthreads();
-      if (wq == 0) {
-        for (int k = 1; k < NW; ++k) {
-#pragma unroll
-          for (int d = 0; d < DL; ++d) a[d] += s_o[warp + k][lane * DL + d];
-          S += s_o[warp + k][DH];
-        }
-      }
-    }
-    if (todo && wq == 0) {
-      const int rr = hm % P.tiles * ROWS + r;
-      T* dst = (T*)P.out + (((size_t)b * P.n + rr / P.group) * P.hq + hm / P.tiles * P.group + rr % P.group) * DH + lane * DL;
-      const float inv = S == 0.f ? 0.f : 1.f / S;
-#pragma unroll
-      for (int d = 0; d < DL; ++d) dst[d] = from_f<T>(S == 0.f ? 0.f : a[d] * inv);
-    }
-  }
-  for (int b = blockIdx.x; b < P.c.batch; b += gridDim.x) {
-    if (L.len[b] < 0 || L.pre[b + 1] != L.pre[b]) continue;
-    T* dst = (T*)P.out + (size_t)b * P.n * P.hq * DH;
-    for (int d = threadIdx.x; d < P.n * P.hq * DH; d += 128) dst[d] = from_f<T>(0.f);
-  }
-  if (!P.weight_out) return;
-  // weights: chunks of 256 slots of every (sequence, head), counted along the lengths
-  constexpr int CHUNK = 256;
-  long long n_chunks = 0;
-  for (int b = 0; b < P.c.batch; ++b)
-    if (L.len[b] >= 0) n_chunks += ((min((long long)L.len[b] + P.n_new, P.c.cap()) + CHUNK - 1) / CHUNK) * P.c.hkv;
-  long long base = 0;
-  int b = -1;
-  long long per = 0;
-  for (long long w = blockIdx.x; w < n_chunks; w += gridDim.x) {
-    while (b < 0 || w >= base + per * P.c.hkv) {
-      if (b >= 0) base += per * P.c.hkv;
-      ++b;
-      per = L.len[b] < 0 ? 0 : (min((long long)L.len[b] + P.n_new, P.c.cap()) + CHUNK - 1) / CHUNK;
-    }
-    const int h = (int)((w - base) / per);
-    const long long slot0 = (w - base - h * per) * CHUNK;
-    const long long keys = min((long long)L.len[b] + P.n_new, P.c.cap());
-    const long long T_b = L.pre[b + 1] - L.pre[b];
-    __syncthreads();
-    for (int g = threadIdx.x; g < P.group; g += 128) {              // the heads' maximum and sum over their pieces
-      const int hm = h * P.tiles + g / PG_ROWS, r = g % PG_ROWS;
-      const long long x0 = L.pre[b] * hm_n + (long long)hm * T_b;
-      const int c0 = line_owner(L, x0), c1 = line_owner(L, x0 + T_b - 1);
-      float M = -INFINITY, S = 0.f, sub;
-      if (c0 == c1) {
-        const float* ml = P.whole_ml + (((size_t)b * hm_n + hm) * PG_ROWS + r) * 2;
-        M = ml[0];
-        S = ml[1];
-        sub = M == -INFINITY ? 0.f : M;
-      } else {
-        for (int i = c0; i <= c1; ++i) M = fmaxf(M, P.part_ml[(piece_of(L, i, x0) * PG_ROWS + r) * 2]);
-        sub = M == -INFINITY ? 0.f : M;
-        for (int i = c0; i <= c1; ++i) {
-          const float* ml = P.part_ml + (piece_of(L, i, x0) * PG_ROWS + r) * 2;
-          S = fmaf(exp2f(ml[0] - sub), ml[1], S);
-        }
-      }
-      s_m[g] = sub;
-      s_l[g] = S == 0.f ? 0.f : 1.f / S;
-    }
-    __syncthreads();
-    for (long long slot = slot0 + threadIdx.x; slot < min(slot0 + CHUNK, keys); slot += 128) {
-      const size_t at = ((size_t)b * P.c.hkv + h) * (size_t)P.c.cap() + (size_t)slot;
+    for (int u = 0; u < CHUNK / 256; ++u) {
+      const int slot = slot0 + u * 256 + threadIdx.x;
+      if (slot >= keys) continue;
+      const float old = (P.c.weight && slot < L.len[b]) ? P.c.weight[at + slot] : 0.f;
       float sum = 0.f;
-      const float* s = P.score + ((long long)b * P.hq + h * P.group) * P.score_ld + slot;
-      for (int g = 0; g < P.group; ++g) sum = fmaf(exp2f(s[g * P.score_ld] - s_m[g]), s_l[g], sum);
-      const float old = (P.c.weight && slot < L.len[b]) ? P.c.weight[at] : 0.f;
-      P.weight_out[at] = old + sum;
+#pragma unroll 4
+      for (int g = 0; g < P.group; ++g) {
+        const float2 t = __ldg(reinterpret_cast<const float2*>(ml) + g);
+        const float z = __ldg(score + g * P.score_ld + slot);
+        sum = fmaf(exp2f(z - (t.x == -INFINITY ? 0.f : t.x)), t.y == 0.f ? 0.f : 1.f / t.y, sum);
+      }
+      P.weight_out[at + slot] = old + sum;
     }
   }
 }

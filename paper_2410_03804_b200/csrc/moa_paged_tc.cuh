@@ -79,32 +79,79 @@ __device__ __forceinline__ void tc_ld128(uint32_t taddr, float* v) {
       : "memory");
 }
 
+// Joins the pieces of the items that a stretch's end cut, in the order of their positions. Work: every end of a stretch times
+// the rows of an item, a warp each; an item that several ends cut belongs to the first of them.
+template <int DH, int ROWS>
+__global__ void __launch_bounds__(256) paged_join_kernel(const PagedAttn P, int tile) {
+  pdl_trigger();
+  __shared__ PagedLine L;
+  pdl_wait(KID_ATTN_MERGE);
+  paged_line(L, P, tile);
+  if (L.total == 0) return;
+  const int hm_n = P.c.hkv * P.tiles, R = P.n * P.group;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  constexpr int DL = DH / 32;
+  PagedPlace S;
+  S.b = 0;
+  // blockIdx.x: the end of a stretch, blockIdx.y: a part of the rows
+  const int c = blockIdx.x + 1;
+  if (c >= L.ctas) return;
+  const int x = line_begin(L, c);
+  S.at(L, P, x);
+  const int x0 = x - S.t;
+  if (S.t == 0 || line_owner(L, x0) != c - 1) return;
+  const int c1 = line_owner(L, x0 + S.T_b - 1), b = S.b, h = S.h;
+  (void)hm_n;
+  for (int r = blockIdx.y * 8 + warp; r < ROWS; r += gridDim.y * 8) {
+    const int rr = S.mt * ROWS + r;
+    if (rr >= R) break;
+    float M = -INFINITY, Z = 0.f, a[DL];
+#pragma unroll
+    for (int d = 0; d < DL; ++d) a[d] = 0.f;
+    for (int i = c - 1 + lane; i <= c1; i += 32) M = fmaxf(M, __ldg(P.part_ml + ((size_t)piece_of(L, i, x0) * ROWS + r) * 2));
+    M = warp_max(M);
+    const float ref = M == -INFINITY ? 0.f : M;
+#pragma unroll 4
+    for (int i = c - 1; i <= c1; ++i) {
+      const size_t at = (size_t)piece_of(L, i, x0) * ROWS + r;
+      const float f = exp2f(__ldg(P.part_ml + at * 2) - ref);
+      Z = fmaf(f, __ldg(P.part_ml + at * 2 + 1), Z);
+      if constexpr (DL == 4) {
+        const float4 o = __ldg(reinterpret_cast<const float4*>(P.part_o + at * DH) + lane);
+        a[0] = fmaf(f, o.x, a[0]); a[1] = fmaf(f, o.y, a[1]); a[2] = fmaf(f, o.z, a[2]); a[3] = fmaf(f, o.w, a[3]);
+      } else {
+        const float2 o = __ldg(reinterpret_cast<const float2*>(P.part_o + at * DH) + lane);
+        a[0] = fmaf(f, o.x, a[0]); a[1] = fmaf(f, o.y, a[1]);
+      }
+    }
+    const float inv = Z == 0.f ? 0.f : 1.f / Z;
+    bf16* dst = (bf16*)P.out + (((size_t)b * P.n + rr / P.group) * P.hq + h * P.group + rr % P.group) * DH + lane * DL;
+    uint32_t w[DL / 2];
+#pragma unroll
+    for (int d = 0; d < DL; d += 2) w[d / 2] = Z == 0.f ? 0u : pack_bf16(a[d] * inv, a[d + 1] * inv);
+    if constexpr (DL == 4) *reinterpret_cast<uint2*>(dst) = make_uint2(w[0], w[1]);
+    else *reinterpret_cast<uint32_t*>(dst) = w[0];
+  }
+}
+
 // One stretch of an item, as every role of the CTA walks through them.
 struct PtWalk {
-  long long x, x_end;
-  int b, hm_n;
+  int x, x_begin, x_end;
+  PagedPlace S;
   // the current segment
-  int h, pair, t0, nb;
-  bool whole, first;
-  __device__ __forceinline__ void begin(const PagedLine& L, const PagedAttn& P) {
-    hm_n = P.c.hkv * P.tiles;
-    x = line_begin(L, blockIdx.x);
+  int b, h, pair, t0, nb, x0;
+  bool whole;
+  __device__ __forceinline__ void begin(const PagedLine& L) {
+    x = x_begin = line_begin(L, blockIdx.x);
     x_end = line_begin(L, blockIdx.x + 1);
-    b = 0;
-    first = true;
+    S.b = 0;
   }
   __device__ __forceinline__ bool next(const PagedLine& L, const PagedAttn& P) {
     if (x >= x_end) return false;
-    first = x == line_begin(L, blockIdx.x);
-    while (x >= L.pre[b + 1] * hm_n) ++b;
-    const long long T_b = L.pre[b + 1] - L.pre[b];
-    const long long in_b = x - L.pre[b] * hm_n;
-    const int hm = (int)(in_b / T_b);
-    h = hm / P.tiles;
-    pair = hm - h * P.tiles;
-    t0 = (int)(in_b - hm * T_b);
-    nb = (int)min(T_b - t0, x_end - x);
-    whole = t0 == 0 && nb == T_b;
+    S.at(L, P, x);
+    b = S.b; h = S.h; pair = S.mt; t0 = S.t; x0 = x - t0;
+    nb = min(S.T_b - t0, x_end - x);
+    whole = nb == S.T_b;
     x += nb;
     return true;
   }
@@ -159,7 +206,7 @@ __global__ void __launch_bounds__(PT_THREADS, 1) paged_tree_kernel(const __grid_
   const uint32_t tmem = *tmem_slot;
   const bool idle = (int)blockIdx.x >= L.ctas || L.total == 0;
   PtWalk W;
-  if (!idle) W.begin(L, P);
+  if (!idle) W.begin(L);
 
   if (idle) {
   } else if (warp == 0) {
@@ -266,14 +313,8 @@ __global__ void __launch_bounds__(PT_THREADS, 1) paged_tree_kernel(const __grid_
         mbar_arrive(q_bar(i));
       }
       // ---- what the rows see ----
-      unsigned long long word = causal_word(qi), any = causal_word(P.n - 1);
-      if (P.mask) {
-        const unsigned long long* m = P.mask + (size_t)W.b * P.n;
-        word = m[qi];
-        unsigned long long a = lane < P.n ? m[lane] : 0ull;
-        if (lane + 32 < P.n) a |= m[lane + 32];
-        any = ((unsigned long long)__reduce_or_sync(0xffffffffu, (unsigned)(a >> 32)) << 32) | __reduce_or_sync(0xffffffffu, (unsigned)a);
-      }
+      const unsigned long long any = any_word(P, W.b);
+      unsigned long long word = row_word(P, W.b, qi);
       if (!valid) word = 0ull;
       const bool all_rows = __all_sync(0xffffffffu, word != 0ull || !valid);
       const int* table = P.c.table + (size_t)W.b * P.c.max_pages;
@@ -370,8 +411,7 @@ __global__ void __launch_bounds__(PT_THREADS, 1) paged_tree_kernel(const __grid_
       if (!dead) dead = __any_sync(0xffffffffu, !mbar_wait(o_bar(i), (c - 1u) & 1u, abort_flag));
       tc_fence_after();
       const float inv = dead ? __int_as_float(0x7fffffff) : l_run == 0.f ? 0.f : 1.f / l_run;
-      const size_t piece = (size_t)blockIdx.x * 2 + (W.first ? 0 : 1);
-      const size_t prow = piece * PT_ROWS + i * 128 + row;
+      const size_t prow = (size_t)piece_of(L, blockIdx.x, W.x0) * PT_ROWS + i * 128 + row;
       bf16* dst = (bf16*)P.out + (((size_t)W.b * P.n + qi) * P.hq + W.h * P.group + hd) * DH;
 #pragma unroll 1
       for (int d = 0; d < DH; d += 16) {

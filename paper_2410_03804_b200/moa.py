@@ -315,9 +315,9 @@ class PagedCache:
         return n.value
 
     def workspace(self, n: int, hq: int, weights: bool = False) -> torch.Tensor:
-        """Scratch for moa_paged_attention with n rows per sequence and hq query heads."""
+        """Scratch for moa_paged_attention with n rows per sequence and hq query heads (zeroed, as its first call needs it)."""
         lib = load_library()
-        return torch.empty(self._scratch(lambda b: lib.moa_paged_workspace_bytes(self._ref, n, hq, 1 if weights else 0, b),
+        return torch.zeros(self._scratch(lambda b: lib.moa_paged_workspace_bytes(self._ref, n, hq, 1 if weights else 0, b),
                                          "moa_paged_workspace_bytes"), dtype=torch.uint8, device=self.device)
 
     def evict_workspace(self, budget: int) -> torch.Tensor:
