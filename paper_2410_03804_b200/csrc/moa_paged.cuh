@@ -169,15 +169,13 @@ struct PagedWarp<bf16, DH> {
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       const int r = mt * PG_ROWS + gq + 8 * u;
-      const bool in = r < R;
-      const int rc = in ? r : 0;
+      const int rc = r < R ? r : 0;          // rows behind the last one are worked on and not written
       const uint32_t* src = reinterpret_cast<const uint32_t*>((const bf16*)P.q + ((long long)b * P.n + rc / P.group) * P.q_stride +
                                                               (long long)(h * P.group + rc % P.group) * DH);
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
-        const uint32_t x = __ldg(src + ks * 8 + tq), y = __ldg(src + ks * 8 + 4 + tq);
-        qf[ks][u] = in ? x : 0u;
-        qf[ks][2 + u] = in ? y : 0u;
+        qf[ks][u] = __ldg(src + ks * 8 + tq);
+        qf[ks][2 + u] = __ldg(src + ks * 8 + 4 + tq);
       }
     }
 #pragma unroll
@@ -536,22 +534,21 @@ __global__ void __launch_bounds__(PG_THREADS, 1) paged_rows_kernel(const PagedAt
       f_any = any_word(P, F.b);
     }
   };
+  PagedWarp<T, DH> W;
+  PagedPlace S = F;
+  W.start(P, S.b, S.h, S.mt, extra);                                 // the first queries are on their way before the copies
 #pragma unroll
   for (int st = 0; st < PG_STAGES - 1; ++st) {
     if (f_x < x_end) issue(st);
     cp_async_commit();
   }
-
-  PagedWarp<T, DH> W;
-  PagedPlace S;
-  S.b = 0;
   int st = 0;
   for (int x = x_begin; x < x_end;) {
     S.at(L, P, x);
     const int b = S.b, h = S.h, mt = S.mt, t0 = S.t, t1 = min(S.T_b, t0 + (x_end - x));
     const int x0 = x - t0;                                           // the item's first tile on the line
     const int len = L.len[b], keys = min(len + P.n_new, cap);
-    W.start(P, b, h, mt, extra);
+    if (x != x_begin) W.start(P, b, h, mt, extra);
     const bool full_rows = W.words(P, b, mt, R);                     // every row of this warp's tile sees the committed slots
     for (int t = t0; t < t1; ++t) {
       if (f_x < x_end) issue(st == 0 ? PG_STAGES - 1 : st - 1);      // the stage of the step before this one

@@ -17,6 +17,8 @@
 // Work split, pieces and join are those of the row kernel, with items of 256 query rows and one CTA per SM.
 // Every wait is bounded; a CTA whose wait ran out writes NaN to its rows.
 #pragma once
+#include <type_traits>
+
 #include "moa_attn_tc.cuh"
 #include "moa_paged.cuh"
 
@@ -27,6 +29,7 @@ constexpr int PT_ROWS = 256;                 // query rows per item: two tiles
 constexpr int PT_THREADS = 320;
 constexpr int PT_SLOTS = 5;
 constexpr uint32_t PT_TM_S = 0, PT_TM_O = 256;
+constexpr int PT_POLY = 4;                    // of every 16 exponentials, how many go to the multiply-add pipe (an even number)
 
 template <int DH> struct PtCfg {
   static constexpr int CK = DH / 64;                          // 64-column chunks of a row
@@ -34,6 +37,10 @@ template <int DH> struct PtCfg {
   static constexpr int SLOT = CK * CHUNK;
   static constexpr int SMEM = 2 * SLOT + PT_SLOTS * SLOT + 1024 + 256;
 };
+
+// 16-byte piece of a query row in its tile: 64-column chunks of 128-byte rows, 128-byte swizzle.
+template <int CHUNK>
+__device__ __forceinline__ int pt_q_off(int row, int piece) { return (piece >> 3) * CHUNK + row * 128 + (((piece & 7) ^ (row & 7)) << 4); }
 
 struct PagedTree {
   CUtensorMap tmK, tmV;                      // [n_pages, page_size, hkv * DH], box 64 columns x min(page_size, 128) rows
@@ -79,58 +86,56 @@ __device__ __forceinline__ void tc_ld128(uint32_t taddr, float* v) {
       : "memory");
 }
 
-// Joins the pieces of the items that a stretch's end cut, in the order of their positions. Work: every end of a stretch times
-// the rows of an item, a warp each; an item that several ends cut belongs to the first of them.
-template <int DH, int ROWS>
+// Joins the pieces of the items that a stretch's end cut, in the order of their positions; an item that several ends cut
+// belongs to the first of them. CTA (end of a stretch, quarter of the columns): a warp per 32 rows, a row per lane.
+template <int DH>
 __global__ void __launch_bounds__(256) paged_join_kernel(const PagedAttn P, int tile) {
   pdl_trigger();
   __shared__ PagedLine L;
   pdl_wait(KID_ATTN_MERGE);
   paged_line(L, P, tile);
-  if (L.total == 0) return;
-  const int hm_n = P.c.hkv * P.tiles, R = P.n * P.group;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  constexpr int DL = DH / 32;
+  const int c = blockIdx.x + 1;
+  if (L.total == 0 || c >= L.ctas) return;
   PagedPlace S;
   S.b = 0;
-  // blockIdx.x: the end of a stretch, blockIdx.y: a part of the rows
-  const int c = blockIdx.x + 1;
-  if (c >= L.ctas) return;
   const int x = line_begin(L, c);
   S.at(L, P, x);
   const int x0 = x - S.t;
   if (S.t == 0 || line_owner(L, x0) != c - 1) return;
-  const int c1 = line_owner(L, x0 + S.T_b - 1), b = S.b, h = S.h;
-  (void)hm_n;
-  for (int r = blockIdx.y * 8 + warp; r < ROWS; r += gridDim.y * 8) {
-    const int rr = S.mt * ROWS + r;
-    if (rr >= R) break;
-    float M = -INFINITY, Z = 0.f, a[DL];
-#pragma unroll
-    for (int d = 0; d < DL; ++d) a[d] = 0.f;
-    for (int i = c - 1 + lane; i <= c1; i += 32) M = fmaxf(M, __ldg(P.part_ml + ((size_t)piece_of(L, i, x0) * ROWS + r) * 2));
-    M = warp_max(M);
-    const float ref = M == -INFINITY ? 0.f : M;
+  const int c1 = line_owner(L, x0 + S.T_b - 1);
+  const int r = threadIdx.x, rr = S.mt * PT_ROWS + r;                // row of the item, of the (sequence, head)
+  const int R = P.n * P.group;
+  if ((rr & ~31) >= R) return;
+  float M = -INFINITY, Z = 0.f;
 #pragma unroll 4
-    for (int i = c - 1; i <= c1; ++i) {
-      const size_t at = (size_t)piece_of(L, i, x0) * ROWS + r;
-      const float f = exp2f(__ldg(P.part_ml + at * 2) - ref);
-      Z = fmaf(f, __ldg(P.part_ml + at * 2 + 1), Z);
-      if constexpr (DL == 4) {
-        const float4 o = __ldg(reinterpret_cast<const float4*>(P.part_o + at * DH) + lane);
-        a[0] = fmaf(f, o.x, a[0]); a[1] = fmaf(f, o.y, a[1]); a[2] = fmaf(f, o.z, a[2]); a[3] = fmaf(f, o.w, a[3]);
-      } else {
-        const float2 o = __ldg(reinterpret_cast<const float2*>(P.part_o + at * DH) + lane);
-        a[0] = fmaf(f, o.x, a[0]); a[1] = fmaf(f, o.y, a[1]);
-      }
-    }
-    const float inv = Z == 0.f ? 0.f : 1.f / Z;
-    bf16* dst = (bf16*)P.out + (((size_t)b * P.n + rr / P.group) * P.hq + h * P.group + rr % P.group) * DH + lane * DL;
-    uint32_t w[DL / 2];
+  for (int i = c - 1; i <= c1; ++i) M = fmaxf(M, __ldg(P.part_ml + ((size_t)piece_of(L, i, x0) * PT_ROWS + r) * 2));
+  const float ref = M == -INFINITY ? 0.f : M;
+  constexpr int N4 = DH / 16;                                        // 16-byte pieces of a row in a quarter
+  float4 a[N4];
 #pragma unroll
-    for (int d = 0; d < DL; d += 2) w[d / 2] = Z == 0.f ? 0u : pack_bf16(a[d] * inv, a[d + 1] * inv);
-    if constexpr (DL == 4) *reinterpret_cast<uint2*>(dst) = make_uint2(w[0], w[1]);
-    else *reinterpret_cast<uint32_t*>(dst) = w[0];
+  for (int d = 0; d < N4; ++d) a[d] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 2
+  for (int i = c - 1; i <= c1; ++i) {
+    const size_t piece = piece_of(L, i, x0);
+    const float2 ml = __ldg(reinterpret_cast<const float2*>(P.part_ml) + piece * PT_ROWS + r);
+    const float f = exp2f(ml.x - ref);
+    Z = fmaf(f, ml.y, Z);
+#pragma unroll
+    for (int d = 0; d < N4; ++d) {
+      const float4 o = __ldg(reinterpret_cast<const float4*>(P.part_o) + (piece * (DH / 4) + blockIdx.y * N4 + d) * PT_ROWS + r);
+      a[d].x = fmaf(f, o.x, a[d].x); a[d].y = fmaf(f, o.y, a[d].y); a[d].z = fmaf(f, o.z, a[d].z); a[d].w = fmaf(f, o.w, a[d].w);
+    }
+  }
+  if (rr >= R) return;
+  const float inv = Z == 0.f ? 0.f : 1.f / Z;
+  bf16* dst = (bf16*)P.out + (((size_t)S.b * P.n + rr / P.group) * P.hq + S.h * P.group + rr % P.group) * DH + blockIdx.y * (DH / 4);
+#pragma unroll
+  for (int d = 0; d < N4; d += 2) {
+    uint4 y = make_uint4(0u, 0u, 0u, 0u);
+    if (Z != 0.f)
+      y = make_uint4(pack_bf16(a[d].x * inv, a[d].y * inv), pack_bf16(a[d].z * inv, a[d].w * inv), pack_bf16(a[d + 1].x * inv, a[d + 1].y * inv),
+                     pack_bf16(a[d + 1].z * inv, a[d + 1].w * inv));
+    *reinterpret_cast<uint4*>(dst + d * 4) = y;
   }
 }
 
@@ -156,6 +161,48 @@ struct PtWalk {
     return true;
   }
 };
+
+// Two fp32 values side by side (packed fp32 instructions of sm_100).
+__device__ __forceinline__ uint64_t f2_pack(float lo, float hi) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+  return r;
+}
+__device__ __forceinline__ void f2_unpack(uint64_t v, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v)); }
+__device__ __forceinline__ uint64_t f2_fma(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ uint64_t f2_add(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ float max3_nan(float a, float b, float c) {      // NaN if one of them is
+  float r;
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+// 2^x of two values, -125 <= x <= 125, on the multiply-add pipe: x = n + f with n the nearest integer (by adding 1.5 * 2^23),
+// 2^f on [-1/2, 1/2] by the polynomial of degree 5 with the least relative error (7.5e-8, a Remez fit), n added to the
+// exponent. The special-function unit gives 16 exponentials a cycle and SM, which alone would take as long as both products.
+__device__ __forceinline__ void ex2_poly2(uint64_t x, float& lo, float& hi) {
+  const uint64_t magic = f2_pack(12582912.f, 12582912.f);
+  const uint64_t t = f2_add(x, magic);
+  const uint64_t n = f2_add(t, f2_pack(-12582912.f, -12582912.f));
+  const uint64_t f = f2_fma(n, f2_pack(-1.f, -1.f), x);
+  uint64_t y = f2_fma(f2_pack(0.0013276472454890609f, 0.0013276472454890609f), f, f2_pack(0.009675540961325169f, 0.009675540961325169f));
+  y = f2_fma(y, f, f2_pack(0.05550713092088699f, 0.05550713092088699f));
+  y = f2_fma(y, f, f2_pack(0.24022120237350464f, 0.24022120237350464f));
+  y = f2_fma(y, f, f2_pack(0.6931469440460205f, 0.6931469440460205f));
+  y = f2_fma(y, f, f2_pack(1.0000001192092896f, 1.0000001192092896f));
+  float tl, th, yl, yh;
+  f2_unpack(t, tl, th);
+  f2_unpack(y, yl, yh);
+  lo = __int_as_float(__float_as_int(yl) + (__float_as_int(tl) << 23));
+  hi = __int_as_float(__float_as_int(yh) + (__float_as_int(th) << 23));
+}
 
 // bits of positions base .. base + 63 that a row with mask word w sees: committed ones (if it sees anything) and its new slots
 __device__ __forceinline__ unsigned long long low_bits(long long n) { return n <= 0 ? 0ull : n >= 64 ? ~0ull : (1ull << n) - 1ull; }
@@ -302,12 +349,19 @@ __global__ void __launch_bounds__(PT_THREADS, 1) paged_tree_kernel(const __grid_
       const int len = L.len[W.b];
       const long long keys = min((long long)len + P.n_new, P.c.cap());
       // ---- queries into shared memory (the tile's last scores have been formed: this thread waited for them) ----
+      // coalesced: the warp's 32 rows, 32 * 8 / DH of them per instruction; rows behind the last one hold some real row and are
+      // worked on, but not written
+      constexpr int PIECES = DH / 8, RPI = 32 / PIECES;
+      const int piece = lane % PIECES;
       {
-        const uint4* src = reinterpret_cast<const uint4*>((const bf16*)P.q + ((long long)W.b * P.n + qi) * P.q_stride + (long long)(W.h * P.group + hd) * DH);
-        uint8_t* dst = bp + i * C::SLOT + row * 128;
+        const long long off = ((long long)W.b * P.n + qi) * P.q_stride + (long long)(W.h * P.group + hd) * DH;
+        uint4 x[PIECES];
 #pragma unroll
-        for (int p = 0; p < DH / 8; ++p)
-          *reinterpret_cast<uint4*>(dst + (p >> 3) * C::CHUNK + (((p & 7) ^ (row & 7)) << 4)) = valid ? __ldg(src + p) : make_uint4(0u, 0u, 0u, 0u);
+        for (int u = 0; u < PIECES; ++u)
+          x[u] = __ldg(reinterpret_cast<const uint4*>((const bf16*)P.q + __shfl_sync(0xffffffffu, off, u * RPI + lane / PIECES)) + piece);
+#pragma unroll
+        for (int u = 0; u < PIECES; ++u)
+          *reinterpret_cast<uint4*>(bp + i * C::SLOT + pt_q_off<C::CHUNK>(quad * 32 + u * RPI + lane / PIECES, piece)) = x[u];
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         tc_fence_before();
         mbar_arrive(q_bar(i));
@@ -335,7 +389,8 @@ __global__ void __launch_bounds__(PT_THREADS, 1) paged_tree_kernel(const __grid_
         float s[128];
         tc_ld128(tS, s);
         const long long k0 = (long long)(W.t0 + t) * PT_KB;
-        if (k0 + PT_KB > len || bad || !all_rows) {
+        const bool masked = k0 + PT_KB > len || bad || !all_rows;
+        if (masked) {
           unsigned long long vis[2] = {row_bits(word, k0, len, keys), row_bits(word, k0 + 64, len, keys)};
           unsigned long long live[2] = {row_bits(any, k0, len, keys), row_bits(any, k0 + 64, len, keys)};
           if (bad) {
@@ -365,8 +420,10 @@ __global__ void __launch_bounds__(PT_THREADS, 1) paged_tree_kernel(const __grid_
         }
         float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-        for (int e = 0; e < 128; ++e) m4[e & 3] = fmaxf(m4[e & 3], s[e]);
-        const float m_blk = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])) * P.scale_log2;
+        for (int e = 0; e < 128; e += 8)
+#pragma unroll
+          for (int u = 0; u < 4; ++u) m4[u] = max3_nan(m4[u], s[e + 2 * u], s[e + 2 * u + 1]);
+        const float m_blk = max3_nan(max3_nan(m4[0], m4[1], m4[2]), m4[3], m4[3]) * P.scale_log2;
         float f = 1.f;
         if (m_ref == -INFINITY) {
           m_ref = m_blk;                     // nothing has been added for this row yet
@@ -390,19 +447,40 @@ __global__ void __launch_bounds__(PT_THREADS, 1) paged_tree_kernel(const __grid_
           }
         }
         const float sub = m_ref == -INFINITY ? 0.f : m_ref;
-        float l4[4] = {0.f, 0.f, 0.f, 0.f};
+        const uint64_t scale2 = f2_pack(P.scale_log2, P.scale_log2), sub2 = f2_pack(-sub, -sub);
+        uint64_t l2[2] = {0ull, 0ull};
+        // scores that are not there (-inf) and NaN take the special-function unit: the polynomial knows neither
+        const bool poly = !masked && __all_sync(0xffffffffu, m_blk > -3.0e38f);
+        auto probabilities = [&](auto with_poly) {
 #pragma unroll
-        for (int e = 0; e < 128; e += 16) {
-          uint32_t w8[8];
+          for (int e = 0; e < 128; e += 16) {
+            uint32_t w8[8];
 #pragma unroll
-          for (int u = 0; u < 8; ++u) {
-            const float p0 = ex2_approx(fmaf(s[e + 2 * u], P.scale_log2, -sub)), p1 = ex2_approx(fmaf(s[e + 2 * u + 1], P.scale_log2, -sub));
-            l4[u & 3] += p0 + p1;
-            w8[u] = pack_bf16(p0, p1);
+            for (int u = 0; u < 8; ++u) {
+              const uint64_t x = f2_fma(f2_pack(s[e + 2 * u], s[e + 2 * u + 1]), scale2, sub2);
+              float p0, p1;
+              if (decltype(with_poly)::value && u * 2 >= 16 - PT_POLY) {
+                float x0, x1;
+                f2_unpack(x, x0, x1);
+                ex2_poly2(f2_pack(fmaxf(x0, -125.f), fmaxf(x1, -125.f)), p0, p1);
+              } else {
+                float x0, x1;
+                f2_unpack(x, x0, x1);
+                p0 = ex2_approx(x0);
+                p1 = ex2_approx(x1);
+              }
+              l2[u & 1] = f2_add(l2[u & 1], f2_pack(p0, p1));
+              w8[u] = pack_bf16(p0, p1);
+            }
+            tc_st8(tS + (uint32_t)(e / 2), w8);
           }
-          tc_st8(tS + (uint32_t)(e / 2), w8);
+        };
+        if (poly) probabilities(std::true_type{}); else probabilities(std::false_type{});
+        {
+          float a0, a1;
+          f2_unpack(f2_add(l2[0], l2[1]), a0, a1);
+          l_run += a0 + a1;
         }
-        l_run += (l4[0] + l4[1]) + (l4[2] + l4[3]);
         asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
         tc_fence_before();
         mbar_arrive(p_bar(i));
@@ -411,8 +489,8 @@ __global__ void __launch_bounds__(PT_THREADS, 1) paged_tree_kernel(const __grid_
       if (!dead) dead = __any_sync(0xffffffffu, !mbar_wait(o_bar(i), (c - 1u) & 1u, abort_flag));
       tc_fence_after();
       const float inv = dead ? __int_as_float(0x7fffffff) : l_run == 0.f ? 0.f : 1.f / l_run;
-      const size_t prow = (size_t)piece_of(L, blockIdx.x, W.x0) * PT_ROWS + i * 128 + row;
-      bf16* dst = (bf16*)P.out + (((size_t)W.b * P.n + qi) * P.hq + W.h * P.group + hd) * DH;
+      const size_t piece_at = (size_t)piece_of(L, blockIdx.x, W.x0), prow = piece_at * PT_ROWS + i * 128 + row;
+      const bool none = l_run == 0.f && !dead;                       // the row sees nothing
 #pragma unroll 1
       for (int d = 0; d < DH; d += 16) {
         float o[16];
@@ -422,18 +500,30 @@ __global__ void __launch_bounds__(PT_THREADS, 1) paged_tree_kernel(const __grid_
 #pragma unroll
           for (int e = 0; e < 16; ++e) o[e] = 0.f;
         }
-        if (!valid) continue;
-        if (W.whole) {
+        if (W.whole) {                       // staged over this thread's own query row, whose last scores have been formed
           uint32_t w8[8];
 #pragma unroll
-          for (int u = 0; u < 8; ++u) w8[u] = l_run == 0.f && !dead ? 0u : pack_bf16(o[2 * u] * inv, o[2 * u + 1] * inv);
-          *reinterpret_cast<uint4*>(dst + d) = make_uint4(w8[0], w8[1], w8[2], w8[3]);
-          *reinterpret_cast<uint4*>(dst + d + 8) = make_uint4(w8[4], w8[5], w8[6], w8[7]);
-        } else {
-          float* po = P.part_o + prow * DH + d;
+          for (int u = 0; u < 8; ++u) w8[u] = none ? 0u : pack_bf16(o[2 * u] * inv, o[2 * u + 1] * inv);
+          uint8_t* q = bp + i * C::SLOT;
+          *reinterpret_cast<uint4*>(q + pt_q_off<C::CHUNK>(row, d / 8)) = make_uint4(w8[0], w8[1], w8[2], w8[3]);
+          *reinterpret_cast<uint4*>(q + pt_q_off<C::CHUNK>(row, d / 8 + 1)) = make_uint4(w8[4], w8[5], w8[6], w8[7]);
+        } else {                             // columns outside, rows inside: neighbouring threads write neighbouring 16 bytes
 #pragma unroll
-          for (int e = 0; e < 16; e += 4) *reinterpret_cast<float4*>(po + e) = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+          for (int e = 0; e < 16; e += 4)
+            *reinterpret_cast<float4*>(P.part_o + ((piece_at * (DH / 4) + (d + e) / 4) * PT_ROWS + i * 128 + row) * 4) = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
         }
+      }
+      if (W.whole) {                         // coalesced, as the queries came
+        const long long off = valid ? (((long long)W.b * P.n + qi) * P.hq + W.h * P.group + hd) * DH : -1ll;
+        __syncwarp();
+#pragma unroll
+        for (int u = 0; u < PIECES; ++u) {
+          const long long o = __shfl_sync(0xffffffffu, off, u * RPI + lane / PIECES);
+          if (o >= 0)
+            *reinterpret_cast<uint4*>((bf16*)P.out + o + piece * 8) =
+                *reinterpret_cast<const uint4*>(bp + i * C::SLOT + pt_q_off<C::CHUNK>(quad * 32 + u * RPI + lane / PIECES, piece));
+        }
+        __syncwarp();
       }
       if (!W.whole && valid) {
         P.part_ml[prow * 2] = m_ref;

@@ -253,31 +253,37 @@ def moa_dequantize_rows(codes: torch.Tensor, scales: torch.Tensor, dtype=torch.f
     return out
 
 
-def _on(t: torch.Tensor, device) -> bool:
-    return t.is_cuda and t.device == device
+# The serving operators are called once per layer and token, so their checks read each attribute of a tensor once.
+_raw_stream = torch._C._cuda_getCurrentRawStream
 
 
-def _serving_call(device, stream, status_of, what: str):
-    """Runs a call of the serving operators with its tensors' device current, on the given or that device's current stream."""
-    if torch.cuda.current_device() == device.index:
-        _check(status_of(_stream(stream)), what)
+def _serving_call(index: int, stream, call, what: str, *args):
+    """Makes a call of the serving operators with its tensors' device current, on the given or that device's current stream."""
+    if torch._C._cuda_getDevice() == index:
+        status = call(*args, _raw_stream(index) if stream is None else stream.cuda_stream)
     else:
-        with torch.cuda.device(device):
-            _check(status_of(_stream(stream)), what)
+        with torch.cuda.device(index):
+            status = call(*args, _raw_stream(index) if stream is None else stream.cuda_stream)
+    if status != MOA_OK:
+        _check(status, what)
 
 
-def _rows(t: torch.Tensor, batch: int, heads: int, head_dim: int, dtype, device, what: str):
+def _is(t: torch.Tensor, dtype, index: int) -> bool:
+    """A contiguous tensor of a type on a device."""
+    return t.dtype is dtype and t.get_device() == index and t.is_contiguous()
+
+
+def _rows(t: torch.Tensor, batch: int, heads: int, head_dim: int, dtype, index: int, what: str):
     """Checks rows [batch, n, heads, head_dim] whose heads are contiguous; returns (n, elements between two rows)."""
-    assert t.dim() == 4 and t.shape[0] == batch and t.shape[2] == heads and t.shape[3] == head_dim, what
-    assert t.dtype == dtype and _on(t, device), what
-    n = t.shape[1]
-    assert n >= 1 and t.stride(3) == 1 and t.stride(2) == head_dim, what + ": heads must be contiguous"
+    assert t.dim() == 4 and t.dtype is dtype and t.get_device() == index, what
+    b, n, h, d = t.shape
+    s0, s1, s2, s3 = t.stride()
+    assert b == batch and h == heads and d == head_dim and n >= 1, what
+    assert s3 == 1 and (s2 == head_dim or heads == 1), what + ": heads must be contiguous"
     if n == 1:
-        step = t.stride(0) if batch > 1 else heads * head_dim
-    else:
-        step = t.stride(1)
-        assert batch == 1 or t.stride(0) == n * step, what + ": rows must be evenly spaced"
-    return n, step
+        return 1, s0 if batch > 1 else heads * head_dim
+    assert batch == 1 or s0 == n * s1, what + ": rows must be evenly spaced"
+    return n, s1
 
 
 class PagedCache:
@@ -290,18 +296,19 @@ class PagedCache:
     def __init__(self, k, v, page_table, length, weight=None, pos=None, seen=None):
         assert k.is_cuda and k.dim() == 4 and k.dtype in (torch.float32, torch.bfloat16), "k: cuda [n_pages, page_size, hkv, head_dim]"
         dev, (n_pages, ps, hkv, dh) = k.device, k.shape
-        assert _on(v, dev) and v.shape == k.shape and v.dtype == k.dtype and v.stride() == k.stride(), "v must be laid out as k"
-        assert k.stride(3) == 1 and k.stride(2) == dh and (ps == 1 or k.stride(1) == hkv * dh), "a page must be contiguous"
-        i32 = lambda t: _on(t, dev) and t.dtype == torch.int32 and t.is_contiguous()  # noqa: E731
-        assert i32(page_table) and page_table.dim() == 2 and page_table.shape[1] >= 1, "page_table: int32 [batch, max_pages]"
+        at = k.get_device()
+        assert v.get_device() == at and v.shape == k.shape and v.dtype == k.dtype and v.stride() == k.stride(), "v must be laid out as k"
+        assert k.stride(3) == 1 and (hkv == 1 or k.stride(2) == dh) and (ps == 1 or k.stride(1) == hkv * dh), "a page must be contiguous"
+        assert _is(page_table, torch.int32, at) and page_table.dim() == 2 and page_table.shape[1] >= 1, "page_table: int32 [batch, max_pages]"
         batch, per = page_table.shape
-        assert i32(length) and length.shape == (batch,), "length: int32 [batch]"
+        assert _is(length, torch.int32, at) and length.shape == (batch,), "length: int32 [batch]"
         full = (batch, hkv, per * ps)
-        assert weight is None or (_on(weight, dev) and weight.dtype == torch.float32 and weight.is_contiguous() and weight.shape == full), "weight"
-        assert pos is None or (i32(pos) and pos.shape == full), "pos"
-        assert seen is None or (i32(seen) and seen.shape == (batch,)), "seen"
+        assert weight is None or (_is(weight, torch.float32, at) and weight.shape == full), "weight: float32 [batch, hkv, slots]"
+        assert pos is None or (_is(pos, torch.int32, at) and pos.shape == full), "pos: int32 [batch, hkv, slots]"
+        assert seen is None or (_is(seen, torch.int32, at) and seen.shape == (batch,)), "seen: int32 [batch]"
         self.k, self.v, self.page_table, self.len, self.weight, self.pos, self.seen = k, v, page_table, length, weight, pos, seen
         self.device, self.dtype, self.batch, self.hkv, self.head_dim, self.slots = dev, k.dtype, batch, hkv, dh, per * ps
+        self.index, self._full = at, torch.Size(full)
         self.c = MoaPagedCache(k.data_ptr(), v.data_ptr(), k.stride(0) if n_pages > 1 else ps * hkv * dh, page_table.data_ptr(),
                                length.data_ptr(), weight.data_ptr() if weight is not None else None,
                                pos.data_ptr() if pos is not None else None, seen.data_ptr() if seen is not None else None, batch,
@@ -331,20 +338,19 @@ class PagedCache:
             ws = make()
             if stream is not None:
                 ws.record_stream(stream)
-        assert _on(ws, self.device) and ws.dtype == torch.uint8 and ws.is_contiguous(), "ws: cuda uint8, contiguous"
+        assert _is(ws, torch.uint8, self.index), "ws: cuda uint8, contiguous"
         return ws
 
 
 def moa_paged_append(cache: PagedCache, k_new: torch.Tensor, v_new: torch.Tensor, n_new=None, stream=None):
     """Writes rows [batch, n, hkv, head_dim] behind the committed slots (the first n_new[b] of each sequence), without
     committing them."""
-    n, step = _rows(k_new, cache.batch, cache.hkv, cache.head_dim, cache.dtype, cache.device, "k_new")
-    assert _rows(v_new, cache.batch, cache.hkv, cache.head_dim, cache.dtype, cache.device, "v_new") == (n, step), "v_new must be laid out as k_new"
-    if n_new is not None:
-        assert _on(n_new, cache.device) and n_new.dtype == torch.int32 and n_new.shape == (cache.batch,) and n_new.is_contiguous()
-    lib = load_library()
-    _serving_call(cache.device, stream, lambda s: lib.moa_paged_append(cache._ref, k_new.data_ptr(), v_new.data_ptr(), step, n,
-                                                                       _ptr(n_new), s), "moa_paged_append")
+    at, b, hkv, dh, dt = cache.index, cache.batch, cache.hkv, cache.head_dim, cache.dtype
+    n, step = _rows(k_new, b, hkv, dh, dt, at, "k_new")
+    assert _rows(v_new, b, hkv, dh, dt, at, "v_new") == (n, step), "v_new must be laid out as k_new"
+    assert n_new is None or (_is(n_new, torch.int32, at) and n_new.shape == (b,)), "n_new: int32 [batch]"
+    _serving_call(at, stream, load_library().moa_paged_append, "moa_paged_append", cache._ref, k_new.data_ptr(), v_new.data_ptr(), step, n,
+                  None if n_new is None else n_new.data_ptr())
 
 
 def moa_paged_attention(cache: PagedCache, q: torch.Tensor, k_new=None, v_new=None, mask=None, scale: float = 0.0,
@@ -353,54 +359,47 @@ def moa_paged_attention(cache: PagedCache, q: torch.Tensor, k_new=None, v_new=No
     appended by the call; without them the rows are in the pages already; new_rows=False: there are none). mask: int64
     [batch, n] or [batch, n, 1], one packed word per row as moa_tree_attn_mask(packed=True) gives it; None: causal.
     weight_out (n = 1): float32 [batch, hkv, slots], may be cache.weight. Returns out [batch, n, hq, head_dim]."""
-    dev, b, hkv, dh = cache.device, cache.batch, cache.hkv, cache.head_dim
+    at, b, hkv, dh, dt = cache.index, cache.batch, cache.hkv, cache.head_dim, cache.dtype
     assert q.dim() == 4, "q: [batch, n, hq, head_dim]"
     hq = q.shape[2]
-    n, q_step = _rows(q, b, hq, dh, cache.dtype, dev, "q")
-    kp = vp = None
+    n, q_step = _rows(q, b, hq, dh, dt, at, "q")
+    kp = vp = mp = wp = None
     new_step = 0
+    assert (k_new is None) == (v_new is None), "k_new and v_new come together"
     if k_new is not None:
-        assert v_new is not None and new_rows, "k_new and v_new come together, as new rows"
-        m, new_step = _rows(k_new, b, hkv, dh, cache.dtype, dev, "k_new")
-        assert m == n and _rows(v_new, b, hkv, dh, cache.dtype, dev, "v_new") == (n, new_step), "v_new must be laid out as k_new"
+        assert new_rows, "k_new and v_new are new rows"
+        m, new_step = _rows(k_new, b, hkv, dh, dt, at, "k_new")
+        assert m == n and _rows(v_new, b, hkv, dh, dt, at, "v_new") == (n, new_step), "v_new must be laid out as k_new, with q's rows"
         kp, vp = k_new.data_ptr(), v_new.data_ptr()
-    else:
-        assert v_new is None, "k_new and v_new come together, as new rows"
-    mp = None
     if mask is not None:
-        assert _on(mask, dev) and mask.dtype in (torch.int64, torch.uint64) and mask.is_contiguous() and mask.numel() == b * n, "mask: int64 [batch, n]"
+        assert (_is(mask, torch.int64, at) or _is(mask, torch.uint64, at)) and mask.numel() == b * n, "mask: int64 [batch, n]"
         mp = mask.data_ptr()
     if out is None:
-        out = torch.empty((b, n, hq, dh), dtype=cache.dtype, device=dev)
+        out = torch.empty((b, n, hq, dh), dtype=dt, device=cache.device)
         if stream is not None:
             out.record_stream(stream)
     else:
-        assert _on(out, dev) and out.dtype == cache.dtype and out.shape == q.shape and out.is_contiguous(), "out"
-    wp = None
+        assert _is(out, dt, at) and out.shape == q.shape, "out: [batch, n, hq, head_dim]"
     if weight_out is not None:
-        assert _on(weight_out, dev) and weight_out.dtype == torch.float32 and weight_out.is_contiguous(), "weight_out"
-        assert weight_out.shape == (b, hkv, cache.slots), "weight_out"
+        assert _is(weight_out, torch.float32, at) and weight_out.shape == cache._full, "weight_out: float32 [batch, hkv, slots]"
         wp = weight_out.data_ptr()
     ws = cache._own_scratch(ws, lambda: cache.workspace(n, hq, wp is not None), stream)
-    lib = load_library()
-    _serving_call(dev, stream, lambda s: lib.moa_paged_attention(cache._ref, q.data_ptr(), q_step, kp, vp, new_step, n, n if new_rows else 0,
-                                                                 hq, mp, float(scale), out.data_ptr(), wp, ws.data_ptr(), ws.numel(), s),
-                  "moa_paged_attention")
+    _serving_call(at, stream, load_library().moa_paged_attention, "moa_paged_attention", cache._ref, q.data_ptr(), q_step, kp, vp, new_step, n,
+                  n if new_rows else 0, hq, mp, scale, out.data_ptr(), wp, ws.data_ptr(), ws.numel())
     return out
 
 
 def moa_paged_commit(cache: PagedCache, n: int, acc_slot=None, acc_len=None, advance: bool = True, stream=None):
     """Keeps the accepted path (acc_slot [batch, cap], acc_len [batch] of moa_verify_greedy) of n uncommitted rows, or all of
     them, and advances cache.len (and cache.seen) when asked to."""
-    i32 = lambda t: _on(t, cache.device) and t.dtype == torch.int32 and t.is_contiguous()  # noqa: E731
-    assert acc_len is None or (i32(acc_len) and acc_len.shape == (cache.batch,)), "acc_len: int32 [batch]"
-    cap = 0
+    at, cap = cache.index, 0
+    assert acc_len is None or (_is(acc_len, torch.int32, at) and acc_len.shape == (cache.batch,)), "acc_len: int32 [batch]"
     if acc_slot is not None:
-        assert acc_len is not None and i32(acc_slot) and acc_slot.dim() == 2 and acc_slot.shape[0] == cache.batch, "acc_slot: int32 [batch, cap]"
-        cap = acc_slot.shape[1]
-    lib = load_library()
-    _serving_call(cache.device, stream, lambda s: lib.moa_paged_commit(cache._ref, int(n), _ptr(acc_slot), _ptr(acc_len), cap,
-                                                                       1 if advance else 0, s), "moa_paged_commit")
+        assert acc_len is not None and _is(acc_slot, torch.int32, at) and acc_slot.dim() == 2, "acc_slot: int32 [batch, cap]"
+        b, cap = acc_slot.shape
+        assert b == cache.batch, "acc_slot: int32 [batch, cap]"
+    _serving_call(at, stream, load_library().moa_paged_commit, "moa_paged_commit", cache._ref, n, None if acc_slot is None else acc_slot.data_ptr(),
+                  None if acc_len is None else acc_len.data_ptr(), cap, 1 if advance else 0)
 
 
 def moa_paged_evict(cache: PagedCache, budget: int, sink: int = 4, recent: int = 64, weight_out=None, pos_out=None, len_out=None,
@@ -408,15 +407,15 @@ def moa_paged_evict(cache: PagedCache, budget: int, sink: int = 4, recent: int =
     """Cuts every sequence's heads to `budget` slots (see include/moa.h). weight_out and pos_out default to the cache's own;
     len_out to cache.len, or to nothing with update_len=False (layers that share len)."""
     assert cache.weight is not None and cache.pos is not None and cache.seen is not None, "the cache needs weight, pos and seen"
+    at = cache.index
     w, p = cache.weight if weight_out is None else weight_out, cache.pos if pos_out is None else pos_out
-    assert _on(w, cache.device) and w.dtype == torch.float32 and w.is_contiguous() and w.shape == cache.weight.shape, "weight_out"
-    assert _on(p, cache.device) and p.dtype == torch.int32 and p.is_contiguous() and p.shape == cache.pos.shape, "pos_out"
+    assert _is(w, torch.float32, at) and w.shape == cache._full, "weight_out: float32 [batch, hkv, slots]"
+    assert _is(p, torch.int32, at) and p.shape == cache._full, "pos_out: int32 [batch, hkv, slots]"
     n = len_out if len_out is not None else cache.len if update_len else None
-    assert n is None or (_on(n, cache.device) and n.dtype == torch.int32 and n.is_contiguous() and n.shape == cache.len.shape), "len_out"
+    assert n is None or (_is(n, torch.int32, at) and n.shape == (cache.batch,)), "len_out: int32 [batch]"
     ws = cache._own_scratch(ws, lambda: cache.evict_workspace(budget), stream)
-    lib = load_library()
-    _serving_call(cache.device, stream, lambda s: lib.moa_paged_evict(cache._ref, int(budget), int(sink), int(recent), w.data_ptr(), p.data_ptr(),
-                                                                      _ptr(n), ws.data_ptr(), ws.numel(), s), "moa_paged_evict")
+    _serving_call(at, stream, load_library().moa_paged_evict, "moa_paged_evict", cache._ref, budget, sink, recent, w.data_ptr(), p.data_ptr(),
+                  None if n is None else n.data_ptr(), ws.data_ptr(), ws.numel())
 
 
 class LogitRules:
@@ -430,7 +429,7 @@ class LogitRules:
         words = (vocab + 31) // 32
         given = [t for t in (counts, seen, repetition, frequency, presence, bias_id, bias_value, allow) if t is not None]
         assert (bias_id is None) == (bias_value is None), "bias_id and bias_value come together"
-        self.device = given[0].device if given else None
+        self.index = given[0].get_device() if given else None
         self.batch = given[0].shape[0] if given else None
         self.rows = None if allow is None else allow.shape[1]
         n_bias = 0 if bias_id is None else bias_id.shape[1]
@@ -439,7 +438,7 @@ class LogitRules:
                                    (presence, torch.float32, (self.batch,), "presence"), (bias_id, torch.int32, (self.batch, n_bias), "bias_id"),
                                    (bias_value, torch.float32, (self.batch, n_bias), "bias_value"),
                                    (allow, torch.int32, (self.batch, self.rows, words), "allow")):
-            assert t is None or (_on(t, self.device) and t.dtype == dt and t.is_contiguous() and t.shape == shape), what
+            assert t is None or (t.is_cuda and _is(t, dt, self.index) and t.shape == shape), what
         self.vocab, self.counts, self.seen, self.held = vocab, counts, seen, given
         p = lambda t: None if t is None or t.numel() == 0 else t.data_ptr()  # noqa: E731
         self.c = MoaLogitRuleSet(p(counts), p(seen), p(repetition), p(frequency), p(presence), p(bias_id), p(bias_value), p(allow), n_bias)
@@ -451,42 +450,47 @@ def moa_token_record(tok: torch.Tensor, vocab: int, counts=None, seen=None, n_to
     record: bits in seen, and numbers in counts (None for a prompt)."""
     assert tok.is_cuda and tok.dtype == torch.int32 and tok.dim() == 2 and tok.is_contiguous(), "tok: cuda int32 [batch, cap]"
     b, cap = tok.shape
-    i32 = lambda t: _on(t, tok.device) and t.dtype == torch.int32 and t.is_contiguous()  # noqa: E731
-    assert counts is None or (i32(counts) and counts.shape == (b, vocab)), "counts: int32 [batch, vocab]"
-    assert seen is None or (i32(seen) and seen.shape == (b, (vocab + 31) // 32)), "seen: int32 [batch, ceil(vocab / 32)]"
-    assert n_tok is None or (i32(n_tok) and n_tok.shape == (b,)), "n_tok: int32 [batch]"
-    lib = load_library()
-    _serving_call(tok.device, stream, lambda s: lib.moa_token_record(_ptr(counts), _ptr(seen), b, vocab, _ptr(tok), _ptr(n_tok), cap, s),
-                  "moa_token_record")
+    at = tok.get_device()
+    assert counts is None or (_is(counts, torch.int32, at) and counts.shape == (b, vocab)), "counts: int32 [batch, vocab]"
+    assert seen is None or (_is(seen, torch.int32, at) and seen.shape == (b, (vocab + 31) // 32)), "seen: int32 [batch, ceil(vocab / 32)]"
+    assert n_tok is None or (_is(n_tok, torch.int32, at) and n_tok.shape == (b,)), "n_tok: int32 [batch]"
+    _serving_call(at, stream, load_library().moa_token_record, "moa_token_record", *(None if t is None else t.data_ptr() for t in (counts, seen)),
+                  b, vocab, tok.data_ptr(), None if n_tok is None else n_tok.data_ptr(), cap)
 
 
 def _rule_rows(rules: LogitRules, logits: torch.Tensor, tok, parent):
-    assert logits.is_cuda and logits.is_contiguous() and logits.dim() == 3 and logits.dtype in (torch.float32, torch.bfloat16), "logits: [batch, n, V]"
+    at, dt = logits.get_device(), logits.dtype
+    assert at >= 0 and logits.is_contiguous() and logits.dim() == 3 and dt in (torch.float32, torch.bfloat16), "logits: cuda [batch, n, V]"
     b, n, v = logits.shape
     assert v == rules.vocab and rules.batch in (None, b) and rules.rows in (None, n), "the rules are of another batch"
-    assert rules.device in (None, logits.device), "the rules are on another device"
+    assert rules.index in (None, at), "the rules are on another device"
     assert (tok is None) == (parent is None), "tok and parent come together"
     if tok is not None:
-        for t in (tok, parent):
-            assert _on(t, logits.device) and t.dtype == torch.int32 and t.is_contiguous() and t.shape == (b, n), "tok, parent: int32 [batch, n]"
-    return b, n, v, 0 if logits.dtype == torch.float32 else 1
+        assert _is(tok, torch.int32, at) and tok.shape == (b, n), "tok: int32 [batch, n]"
+        assert _is(parent, torch.int32, at) and parent.shape == (b, n), "parent: int32 [batch, n]"
+    return at, b, n, v, 0 if dt is torch.float32 else 1
+
+
+def _kept(t, stream):
+    if stream is not None:
+        t.record_stream(stream)
+    return t
 
 
 def moa_logit_rules(rules: LogitRules, logits: torch.Tensor, tok=None, parent=None, out=None, choice=None, stream=None):
     """Applies the rules to logits [batch, n, V]; tok, parent int32 [batch, n]: the kept tree whose slots the rows are.
     Returns (adjusted logits, arg-max int32 [batch, n]); out may be the logits themselves."""
-    b, n, v, dt = _rule_rows(rules, logits, tok, parent)
+    at, b, n, v, dt = _rule_rows(rules, logits, tok, parent)
     if out is None:
-        out = torch.empty_like(logits)
+        out = _kept(torch.empty_like(logits), stream)
     else:
-        assert _on(out, logits.device) and out.dtype == logits.dtype and out.shape == logits.shape and out.is_contiguous(), "out"
+        assert _is(out, logits.dtype, at) and out.shape == logits.shape, "out: as the logits"
     if choice is None:
-        choice = torch.empty((b, n), dtype=torch.int32, device=logits.device)
+        choice = _kept(torch.empty((b, n), dtype=torch.int32, device=logits.device), stream)
     else:
-        assert _on(choice, logits.device) and choice.dtype == torch.int32 and choice.shape == (b, n) and choice.is_contiguous(), "choice"
-    lib = load_library()
-    _serving_call(logits.device, stream, lambda s: lib.moa_logit_rules(rules._ref, _ptr(tok), _ptr(parent), b, n, logits.data_ptr(), dt, v,
-                                                                       out.data_ptr(), choice.data_ptr(), s), "moa_logit_rules")
+        assert _is(choice, torch.int32, at) and choice.shape == (b, n), "choice: int32 [batch, n]"
+    _serving_call(at, stream, load_library().moa_logit_rules, "moa_logit_rules", rules._ref, None if tok is None else tok.data_ptr(),
+                  None if parent is None else parent.data_ptr(), b, n, logits.data_ptr(), dt, v, out.data_ptr(), choice.data_ptr())
     return out, choice
 
 
@@ -494,17 +498,17 @@ def moa_verify_greedy_rules(rules: LogitRules, tok: torch.Tensor, parent: torch.
                             stream=None):
     """moa_verify_greedy with the arg-max of the adjusted logits; none are written. Returns the same five tensors."""
     assert tok is not None, "a verification needs the tree"
-    b, n, v, dt = _rule_rows(rules, target_logits, tok, parent)
-    dev, cap = target_logits.device, int(cap)
+    at, b, n, v, dt = _rule_rows(rules, target_logits, tok, parent)
     if out is None:
-        out = tuple(torch.empty(s, dtype=torch.int32, device=dev) for s in ((b, n), (b, cap), (b, cap), (b,), (b,)))
+        out = tuple(_kept(torch.empty(s, dtype=torch.int32, device=target_logits.device), stream)
+                    for s in ((b, n), (b, cap), (b, cap), (b,), (b,)))
     else:
         for t, s in zip(out, ((b, n), (b, cap), (b, cap), (b,), (b,))):
-            assert _on(t, dev) and t.dtype == torch.int32 and t.is_contiguous() and t.shape == s, "out"
-    lib = load_library()
-    _serving_call(dev, stream, lambda s: lib.moa_verify_greedy_rules(rules._ref, tok.data_ptr(), parent.data_ptr(), b, n, target_logits.data_ptr(),
-                                                                     dt, v, cap, *(t.data_ptr() for t in out), s), "moa_verify_greedy_rules")
-    return tuple(out)
+            assert _is(t, torch.int32, at) and t.shape == s, "out: int32 [batch, n], [batch, cap] twice, [batch] twice"
+    c, slot, acc, length, following = out
+    _serving_call(at, stream, load_library().moa_verify_greedy_rules, "moa_verify_greedy_rules", rules._ref, tok.data_ptr(), parent.data_ptr(), b, n,
+                  target_logits.data_ptr(), dt, v, cap, c.data_ptr(), slot.data_ptr(), acc.data_ptr(), length.data_ptr(), following.data_ptr())
+    return c, slot, acc, length, following
 
 
 class MoA:
