@@ -120,7 +120,12 @@ struct PagedPlace {
   int b, h, mt, t, T_b;
   __device__ __forceinline__ void at(const PagedLine& L, const PagedAttn& P, int x) {
     const int hm_n = P.c.hkv * P.tiles;
-    while (x >= L.pre[b + 1] * hm_n) ++b;
+    int hi = P.c.batch;                      // pre[b] * hm_n <= x < pre[hi] * hm_n
+    if (x < L.pre[b + 1] * hm_n) hi = b + 1;
+    while (hi - b > 1) {
+      const int mid = (b + hi) >> 1;
+      if (L.pre[mid] * hm_n <= x) b = mid; else hi = mid;
+    }
     T_b = L.pre[b + 1] - L.pre[b];
     const int in_b = x - L.pre[b] * hm_n, hm = in_b / T_b;
     h = hm / P.tiles;
