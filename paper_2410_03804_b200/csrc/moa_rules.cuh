@@ -11,11 +11,14 @@
 // leaves nothing above -inf chooses token 0.
 //
 // What bounds it: the logits, streamed once (and written once when adjusted logits are wanted). The rules are sparse: a
-// record knows a few thousand of 128256 tokens. A CTA first makes a bitmap of its slice in shared memory, of the tokens that
-// any rule but the mask touches (the record's bits, the path, the biases), with path and biases in a small hash table.
-// Pass 1 streams the logits and looks at bits only. Pass 2 takes the marked tokens, whose counts are scattered loads: side
-// by side over the CTA's threads. (Handled inside pass 1 they were one dependent load after the other for every warp that
-// met a marked token: 281 us for 976 rows of 128256 bf16 with 300 biases.)
+// record knows a few thousand of 128256 tokens. A CTA (or eight in a cluster) takes a row. It marks the allowed tokens of its
+// slice that any other rule touches (the record's, the path's, the biased ones) in a bitmap in shared memory, lists them, and
+// takes the listed ones side by side over its threads, so that their scattered loads (logit, count) are under way together;
+// path and biases are in a small hash table. The stream then looks at bits only: a masked or listed token counts as -inf,
+// four tokens of a table's byte selectors at a time, and the place of the best of 16 bytes is looked up once, at the end.
+// (976 rows of 128256 bf16 with 300 biases: 111 us, two waves of four CTAs per SM, of which the list costs 10 us each. Listed
+// tokens taken by the stream as it met them: 284 us. A second pass walking the bitmap: 115 us. A CTA walking the rows of a
+// sequence with one list for all, its copies ahead: 131 us, its rows' dependent steps no longer hidden by other CTAs.)
 #pragma once
 #include "moa_verify.cuh"
 
@@ -23,6 +26,7 @@ namespace moa {
 
 constexpr int RU_MAX_PATH = 256;             // tree slots per sequence
 constexpr int RU_MAX_BIAS = 1024;
+constexpr int RU_LIST = 1536;                // listed tokens of a slice; those behind them are taken one by one
 
 struct RulesArgs {
   const int* counts;                         // [batch, V] or null
@@ -40,16 +44,24 @@ struct RulesArgs {
 
 __device__ __forceinline__ unsigned ru_hash(int id, unsigned mask) { return ((unsigned)id * 2654435761u >> 12) & mask; }
 
+// Rises with the value, -0 as +0; 0 for -inf and NaN.
+__device__ __forceinline__ unsigned ru_key(float v) {
+  if (!(v > -INFINITY)) return 0u;
+  const unsigned u = __float_as_uint(v + 0.f);
+  return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
+}
+
 template <typename T, int CL, int NT>
 __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(NT) rules_kernel(const RulesArgs A) {
   pdl_trigger();
   extern __shared__ __align__(16) uint32_t ru_smem[];
-  __shared__ float sv[32];
-  __shared__ int si[32];
   __shared__ float cv[CL];
   __shared__ int ci[CL];
   __shared__ int s_path[RU_MAX_PATH], s_tok[RU_MAX_PATH], s_par[RU_MAX_PATH];
-  __shared__ int s_np;
+  __shared__ int s_np, s_listed;
+  __shared__ int list[RU_LIST];
+  __shared__ uint2 picks[256];                     // 16-bit types: byte selectors of four words for every byte of mask bits
+  __shared__ uint2 best[2][NT / 32];               // per warp: stream (key, first token of its 16 bytes), touched (key, token)
   const int rank = blockIdx.x, row = blockIdx.y, b = row / A.n, ti = row - b * A.n;
   const int tid = threadIdx.x;
   const int per_cta = ((A.V + CL - 1) / CL + 31) & ~31;
@@ -71,14 +83,35 @@ __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(NT) rules_kernel(co
   const unsigned* seen = A.seen ? A.seen + (size_t)b * A.words + (e0 >> 5) : nullptr;
   const unsigned* allow = A.allow ? A.allow + (size_t)row * A.words + (e0 >> 5) : nullptr;
   const bool dense = counts && !seen;        // counts without the record's bits: every count is read
+  if constexpr (sizeof(T) == 2) {                  // bit 2 q: the low half of word q, bit 2 q + 1: its high half; 0: from the other operand
+    auto pick = [](unsigned two) { return 0x7654u - (two & 1u) * 0x0044u - (two >> 1) * 0x4400u; };
+    if (tid < 256) picks[tid] = make_uint2(pick(tid & 3) | pick((tid >> 2) & 3) << 16, pick((tid >> 4) & 3) | pick((tid >> 6) & 3) << 16);
+  }
+  if (tid == 0) s_listed = 0;
   // ---- bitmap and hash table ----
+  const int size = e1 - e0;
+  auto in_slice = [&](int id) { return id >= e0 && id < e1; };
+  auto may = [&](int e) { return !allow || ((__ldg(allow + (e >> 5)) >> (e & 31)) & 1u) != 0u; };
   if (dense) {
-    for (int i = tid; i < ((e1 - e0 + 31) & ~31); i += NT) {          // whole warps
-      const unsigned m = __ballot_sync(0xffffffffu, e0 + i < e1 && counts[min(e0 + i, A.V - 1)] > 0);
-      if ((i & 31) == 0) mark[i >> 5] = m;
+    for (int i = tid; i < ((size + 31) & ~31); i += NT) {             // whole warps
+      const unsigned m = __ballot_sync(0xffffffffu, i < size && counts[e0 + min(i, size - 1)] > 0);
+      if ((i & 31) == 0) mark[i >> 5] = allow ? m & __ldg(allow + (i >> 5)) : m;
     }
   } else {
-    for (int i = tid; i < n_words; i += NT) mark[i] = seen ? __ldg(seen + i) : 0u;
+    for (int i0 = tid; i0 < n_words; i0 += 4 * NT) {
+      unsigned m[4], a[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int i = min(i0 + u * NT, n_words - 1);
+        m[u] = seen ? __ldg(seen + i) : 0u;
+        a[u] = allow && seen ? __ldg(allow + i) : ~0u;
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int i = i0 + u * NT, left = size - i * 32;              // no bits behind the vocabulary
+        if (i < n_words) mark[i] = m[u] & a[u] & (left >= 32 ? ~0u : (1u << left) - 1u);
+      }
+    }
   }
   if (A.table > 0) {
     for (int i = tid; i < A.table; i += NT) { h_id[i] = -1; h_cnt[i] = 0; h_n[i] = 0; h_first[i] = 0x7fffffff; }
@@ -108,7 +141,7 @@ __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(NT) rules_kernel(co
     const float* bval = A.bias_val + (size_t)b * A.n_bias;
     for (int i = tid; i < A.n_bias; i += NT) {
       const int id = __ldg(bid + i);
-      if (id < e0 || id >= e1) continue;
+      if (!in_slice(id) || !may(id - e0)) continue;
       const int s = slot_of(id);
       atomicAdd(&h_n[s], 1);
       atomicMin(&h_first[s], i);
@@ -118,7 +151,7 @@ __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(NT) rules_kernel(co
     const int np = s_np;
     for (int i = tid; i < np; i += NT) {
       const int id = s_path[i];
-      if (id < e0 || id >= e1) continue;
+      if (!in_slice(id) || !may(id - e0)) continue;
       atomicAdd(&h_cnt[slot_of(id)], 1);
       atomicOr(&mark[(id - e0) >> 5], 1u << ((id - e0) & 31));
     }
@@ -134,148 +167,205 @@ __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(NT) rules_kernel(co
   }
   __syncthreads();
 
-  // ---- pass 1: the stream; marked tokens are written as they are and left out of the arg-max ----
+  // ---- the list of the marked tokens, in no order ----
   const T* xr = (const T*)A.x + (size_t)row * A.V;
   T* orow = A.out ? (T*)A.out + (size_t)row * A.V : nullptr;
-  const uint8_t* mark8 = reinterpret_cast<const uint8_t*>(mark);
-  const uint8_t* allow8 = reinterpret_cast<const uint8_t*>(allow);
-  constexpr int PER = 16 / sizeof(T);
-  constexpr unsigned ALL = (1u << PER) - 1u;
-  float bv = -INFINITY;
-  int bi = 0x7fffffff;
-  const bool vec = ((reinterpret_cast<uintptr_t>(xr) | reinterpret_cast<uintptr_t>(orow)) & 15u) == 0;
-  const int nvec = vec ? (e1 - e0) / PER : 0;
-  constexpr int UN = 4;
-  for (int c0 = tid; c0 < nvec; c0 += UN * NT) {
-    uint4 raw[UN];
-    unsigned ba[UN];
-#pragma unroll
-    for (int u = 0; u < UN; ++u) {
-      const int c = c0 + u * NT;
-      const bool in = c < nvec;
-      raw[u] = in ? __ldcs(reinterpret_cast<const uint4*>(xr + e0) + c) : make_uint4(0u, 0u, 0u, 0u);
-      ba[u] = (in && allow8) ? (unsigned)__ldg(allow8 + (c * PER >> 3)) >> (PER == 4 ? (c * PER & 4) : 0) : ALL;
-    }
-#pragma unroll
-    for (int u = 0; u < UN; ++u) {
-      const int c = c0 + u * NT;
-      if (c >= nvec) continue;
-      const unsigned mk = ((unsigned)mark8[c * PER >> 3] >> (PER == 4 ? (c * PER & 4) : 0)) & ALL, al = ba[u] & ALL;
-      float x[PER];
-      if constexpr (sizeof(T) == 4) {
-        x[0] = __uint_as_float(raw[u].x); x[1] = __uint_as_float(raw[u].y);
-        x[2] = __uint_as_float(raw[u].z); x[3] = __uint_as_float(raw[u].w);
-      } else {
-        bf16x8_to_float(raw[u], x);
-      }
-      if (al != ALL) {
-#pragma unroll
-        for (int i = 0; i < PER; ++i)
-          if (!((al >> i) & 1u)) x[i] = -INFINITY;
-      }
-      if (orow) {
-        uint4 y;
-        if constexpr (sizeof(T) == 4) y = make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
-        else y = make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
-        __stcs(reinterpret_cast<uint4*>(orow + e0) + c, y);
-      }
-      if (mk != 0u) {
-#pragma unroll
-        for (int i = 0; i < PER; ++i)
-          if ((mk >> i) & 1u) x[i] = -INFINITY;
-      }
-      // a thread meets its elements in rising order, so "strictly greater" keeps the smallest id
-      float vm = x[0];
-#pragma unroll
-      for (int i = 1; i < PER; ++i) vm = fmaxf(vm, x[i]);
-      if (vm > bv) {
-        bv = vm;
-#pragma unroll
-        for (int i = PER - 1; i >= 0; --i)
-          if (x[i] == vm) bi = e0 + c * PER + i;
-      }
-    }
-  }
-  for (int i = nvec * PER + tid; i < e1 - e0; i += NT) {
-    const bool al = !allow8 || ((__ldg(allow8 + (i >> 3)) >> (i & 7)) & 1u);
-    const bool mk = (mark8[i >> 3] >> (i & 7)) & 1u;
-    const float x = al ? to_f(xr[e0 + i]) : -INFINITY;
-    if (orow) orow[e0 + i] = from_f<T>(x);
-    if (!mk && x > bv) { bv = x; bi = e0 + i; }
-  }
-  __syncthreads();                           // pass 2 writes single elements over the vectors of pass 1
-
-  // ---- pass 2: the marked tokens that are allowed ----
   const float rep = A.rep ? A.rep[b] : 1.f, freq = A.freq ? A.freq[b] : 0.f, pres = A.pres ? A.pres[b] : 0.f;
+  float tv = -INFINITY;                            // best of the touched tokens
+  int te = 0x7fffffff;
+  // one touched token of the slice
+  auto touch = [&](int e, float x, bool known, int c) {
+    bool biased = false;
+    float bias = 0.f;
+    if (A.table > 0) {
+      for (unsigned s = ru_hash(e0 + e, hmask);; s = (s + 1u) & hmask) {
+        const int id = h_id[s];
+        if (id == -1) break;
+        if (id == e0 + e) {
+          c += h_cnt[s];
+          known = known || h_cnt[s] > 0;
+          biased = h_n[s] > 0;
+          bias = h_val[s];
+          break;
+        }
+      }
+    }
+    known = known || c > 0;
+    if (known && A.rep) x = x > 0.f ? __fdiv_rn(x, rep) : __fmul_rn(x, rep);
+    if (c > 0) x = __fsub_rn(__fsub_rn(x, __fmul_rn(freq, (float)c)), pres);
+    if (biased) x = __fadd_rn(x, bias);
+    if (orow) orow[e0 + e] = from_f<T>(x);
+    best_of(x, e, tv, te);
+  };
+  auto in_record = [&](int e) { return seen && ((__ldg(seen + (e >> 5)) >> (e & 31)) & 1u); };
   for (int wi = tid; wi < n_words; wi += NT) {
     unsigned m = mark[wi];
     if (m == 0u) continue;
-    if (allow) m &= __ldg(allow + wi);
-    const unsigned in_record = seen ? __ldg(seen + wi) : 0u;
-    while (m != 0u) {
-      const int j = __ffs(m) - 1;
-      m &= m - 1u;
-      const int e = e0 + wi * 32 + j;
-      if (e >= e1) break;                    // bits behind the vocabulary
-      float x = to_f(xr[e]);
-      bool known = (in_record >> j) & 1u;
-      int c = 0;
-      if (counts && (known || dense)) { c = __ldg(counts + e); known = known || c > 0; }
-      bool biased = false;
-      float bias = 0.f;
-      if (A.table > 0) {
-        for (unsigned s = ru_hash(e, hmask);; s = (s + 1u) & hmask) {
-          const int id = h_id[s];
-          if (id == -1) break;
-          if (id == e) {
-            c += h_cnt[s];
-            known = known || h_cnt[s] > 0;
-            biased = h_n[s] > 0;
-            bias = h_val[s];
-            break;
-          }
+    int at = atomicAdd(&s_listed, __popc(m));
+    for (; m != 0u; m &= m - 1u, ++at) {
+      const int e = wi * 32 + __ffs(m) - 1;
+      if (at < RU_LIST) {
+        list[at] = e;
+      } else {                                     // (rare) no room
+        const bool known = in_record(e);
+        touch(e, to_f(xr[e0 + e]), known, counts && (known || dense) ? __ldg(counts + e0 + e) : 0);
+      }
+    }
+  }
+  __syncthreads();
+
+  // ---- the stream's first batch sets out, then the listed tokens ----
+  constexpr int PER = 16 / sizeof(T), UN = 4;
+  constexpr unsigned ALL = (1u << PER) - 1u;
+  const uint8_t* mark8 = reinterpret_cast<const uint8_t*>(mark);
+  const uint8_t* allow8 = reinterpret_cast<const uint8_t*>(allow);
+  // the row's 16-byte pieces start `head` tokens into the slice; with an output that does not lie alike, there are none
+  const T* xs = xr + e0;
+  T* os = orow ? orow + e0 : nullptr;
+  const int head = os && (((uintptr_t)xs ^ (uintptr_t)os) & 15u) ? size : min(size, (int)((16u - (unsigned)((uintptr_t)xs & 15u)) % 16u / sizeof(T)));
+  const int nvec = (size - head) / PER, tail = head + nvec * PER;
+  uint4 raw[UN];
+  unsigned al[UN];
+  auto load = [&](int c0) {
+#pragma unroll
+    for (int u = 0; u < UN; ++u) {
+      const int c = c0 + u * NT, e = head + c * PER;
+      if (c >= nvec) continue;
+      raw[u] = __ldcs(reinterpret_cast<const uint4*>(xs + head) + c);
+      if (allow8) {
+        al[u] = __ldg(allow8 + (e >> 3));
+        if ((e & 7) > 8 - PER) al[u] |= (unsigned)__ldg(allow8 + (e >> 3) + 1) << 8;
+      }
+    }
+  };
+  load(tid);
+  const int n_list = min(s_listed, RU_LIST);
+  for (int k0 = tid; k0 < n_list; k0 += 4 * NT) {
+    int e[4], c[4];
+    float x[4];
+    bool known[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      e[u] = k0 + u * NT < n_list ? list[k0 + u * NT] : -1;
+      if (e[u] < 0) continue;
+      x[u] = to_f(xs[e[u]]);
+      known[u] = in_record(e[u]);
+      c[u] = counts ? __ldg(counts + e0 + e[u]) : 0;         // without its bit it does not count
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+      if (e[u] >= 0) touch(e[u], x[u], known[u], known[u] || dense ? c[u] : 0);
+  }
+  // the few tokens before and behind the pieces
+  for (int k = tid; k < head + size - tail; k += NT) {
+    const int e = k < head ? k : tail + k - head;
+    if ((mark8[e >> 3] >> (e & 7)) & 1u) continue;
+    const float x = may(e) ? to_f(xs[e]) : -INFINITY;
+    if (os) os[e] = from_f<T>(x);
+    best_of(x, e, tv, te);
+  }
+  float bv = -INFINITY;                            // best of the stream
+  int be = 0x7fffffff;                             // the first token of the 16 bytes it is in
+  for (int c0 = tid; c0 - tid < nvec; c0 += UN * NT) {
+    if (c0 != tid) load(c0);
+    uint4 w[UN];
+    unsigned mk[UN], ok[UN];
+#pragma unroll
+    for (int u = 0; u < UN; ++u) {                 // a piece that does not exist has no allowed token
+      const int c = c0 + u * NT, e = min(head + c * PER, size - 1);
+      unsigned v = mark8[e >> 3];
+      if ((e & 7) > 8 - PER) v |= (unsigned)mark8[(e >> 3) + 1] << 8;
+      mk[u] = v >> (e & 7) & ALL;
+      ok[u] = allow8 ? al[u] >> (e & 7) & ALL : ALL;
+      if (c >= nvec) ok[u] = mk[u] = 0u;
+      const unsigned in = ok[u] & ~mk[u];
+      if constexpr (sizeof(T) == 4) {
+        w[u] = make_uint4(in & 1u ? raw[u].x : 0xff800000u, in & 2u ? raw[u].y : 0xff800000u, in & 4u ? raw[u].z : 0xff800000u,
+                          in & 8u ? raw[u].w : 0xff800000u);
+      } else {
+        const uint2 p = picks[in];
+        w[u] = make_uint4(__byte_perm(raw[u].x, 0xff80ff80u, p.x), __byte_perm(raw[u].y, 0xff80ff80u, p.x >> 16),
+                          __byte_perm(raw[u].z, 0xff80ff80u, p.y), __byte_perm(raw[u].w, 0xff80ff80u, p.y >> 16));
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < UN; ++u) {
+      float vm;
+      if constexpr (sizeof(T) == 4) {
+        vm = fmaxf(fmaxf(__uint_as_float(w[u].x), __uint_as_float(w[u].y)), fmaxf(__uint_as_float(w[u].z), __uint_as_float(w[u].w)));
+      } else {
+        auto two = [](uint32_t v) { return *reinterpret_cast<__nv_bfloat162*>(&v); };
+        const __nv_bfloat162 m = __hmax2(__hmax2(two(w[u].x), two(w[u].y)), __hmax2(two(w[u].z), two(w[u].w)));       // NaN only of NaNs
+        const uint32_t mw = *reinterpret_cast<const uint32_t*>(&m);
+        vm = fmaxf(__uint_as_float(mw << 16), __uint_as_float(mw & 0xffff0000u));
+      }
+      be = vm > bv ? head + (c0 + u * NT) * PER : be;        // rising tokens: the first of equals stays
+      bv = fmaxf(bv, vm);
+    }
+    if (os) {
+#pragma unroll
+      for (int u = 0; u < UN; ++u) {
+        const int c = c0 + u * NT, e = head + c * PER;
+        if (c >= nvec) continue;
+        const unsigned skip = mk[u];               // written above
+        if (skip == 0u) {
+          __stcs(reinterpret_cast<uint4*>(os + e), w[u]);
+        } else {
+#pragma unroll
+          for (int q = 0; q < PER; ++q)
+            if (!((skip >> q) & 1u)) {
+              const uint32_t v = sizeof(T) == 4 ? (q == 0 ? w[u].x : q == 1 ? w[u].y : q == 2 ? w[u].z : w[u].w)
+                                                : (q < 2 ? w[u].x : q < 4 ? w[u].y : q < 6 ? w[u].z : w[u].w);
+              if constexpr (sizeof(T) == 4) os[e + q] = __uint_as_float(v);
+              else os[e + q] = __ushort_as_bfloat16((unsigned short)(v >> (16 * (q & 1))));
+            }
         }
       }
-      if (known && A.rep) x = x > 0.f ? __fdiv_rn(x, rep) : __fmul_rn(x, rep);
-      if (c > 0) x = __fsub_rn(__fsub_rn(x, __fmul_rn(freq, (float)c)), pres);
-      if (biased) x = __fadd_rn(x, bias);
-      if (orow) orow[e] = from_f<T>(x);
-      best_of(x, e, bv, bi);
     }
   }
-  if (bv == -INFINITY) bi = 0x7fffffff;      // nothing above -inf: token 0, below
 
   if constexpr (CL > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-  if (!A.choice) return;                     // the same for the whole grid
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
-    const float ov = __shfl_xor_sync(0xffffffffu, bv, o);
-    const int oi = __shfl_xor_sync(0xffffffffu, bi, o);
-    best_of(ov, oi, bv, bi);
-  }
+  if (!A.choice) return;                           // the same for the whole grid
   const int lane = tid & 31, wid = tid >> 5;
-  if (lane == 0) { sv[wid] = bv; si[wid] = bi; }
+#pragma unroll
+  for (int kind = 0; kind < 2; ++kind) {
+    const unsigned key = ru_key(kind ? tv : bv);
+    const unsigned top = __reduce_max_sync(0xffffffffu, key);
+    const unsigned at = __reduce_min_sync(0xffffffffu, key == top ? (unsigned)(kind ? te : be) : 0x7fffffffu);
+    if (lane == 0) best[kind][wid] = make_uint2(top, at);
+  }
   __syncthreads();
   if (wid == 0) {
-    bv = lane < NT / 32 ? sv[lane] : -INFINITY;
-    bi = lane < NT / 32 ? si[lane] : 0x7fffffff;
+    unsigned key[2], at[2];
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-      const float ov = __shfl_xor_sync(0xffffffffu, bv, o);
-      const int oi = __shfl_xor_sync(0xffffffffu, bi, o);
-      best_of(ov, oi, bv, bi);
+    for (int kind = 0; kind < 2; ++kind) {
+      const uint2 t = lane < NT / 32 ? best[kind][lane] : make_uint2(0u, 0x7fffffffu);
+      key[kind] = __reduce_max_sync(0xffffffffu, t.x);
+      at[kind] = __reduce_min_sync(0xffffffffu, t.x == key[kind] ? t.y : 0x7fffffffu);
+    }
+    if (key[0] != 0u) {                            // which of the 16 bytes' tokens it was: a lane each
+      const int e = (int)at[0] + lane;
+      const bool in = lane < PER && !((mark8[e >> 3] >> (e & 7)) & 1u) && (!allow8 || ((__ldg(allow8 + (e >> 3)) >> (e & 7)) & 1u));
+      const unsigned hit = __ballot_sync(0xffffffffu, in && ru_key(to_f(xs[in ? e : 0])) == key[0]);
+      at[0] += __ffs(hit) - 1;
+    }
+    const bool stream = key[0] > key[1] || (key[0] == key[1] && at[0] < at[1]);
+    const unsigned top = stream ? key[0] : key[1];
+    const float v = top == 0u ? -INFINITY : __uint_as_float((top & 0x80000000u) ? top & 0x7fffffffu : ~top);
+    const int i = top == 0u ? 0x7fffffff : e0 + (int)(stream ? at[0] : at[1]);
+    if (lane == 0) {
+      if constexpr (CL == 1) {
+        A.choice[row] = i == 0x7fffffff ? 0 : i;
+      } else {                                     // the slice's result to the shared memory of the cluster's first CTA
+        uint32_t rv, ri;
+        asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(rv) : "r"(smem_u32(&cv[rank])), "r"(0));
+        asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(ri) : "r"(smem_u32(&ci[rank])), "r"(0));
+        asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(rv), "f"(v) : "memory");
+        asm volatile("st.shared::cluster.s32 [%0], %1;" ::"r"(ri), "r"(i) : "memory");
+      }
     }
   }
-  if constexpr (CL == 1) {
-    if (tid == 0) A.choice[row] = bi == 0x7fffffff ? 0 : bi;
-  } else {
-    if (tid == 0) {                          // the slice's result to the shared memory of the cluster's first CTA
-      uint32_t rv, ri;
-      asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(rv) : "r"(smem_u32(&cv[rank])), "r"(0));
-      asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(ri) : "r"(smem_u32(&ci[rank])), "r"(0));
-      asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(rv), "f"(bv) : "memory");
-      asm volatile("st.shared::cluster.s32 [%0], %1;" ::"r"(ri), "r"(bi) : "memory");
-    }
+  if constexpr (CL > 1) {
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
     if (rank == 0 && tid == 0) {
       float fv = -INFINITY;
