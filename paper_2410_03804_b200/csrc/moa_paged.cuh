@@ -65,12 +65,26 @@ struct PagedAttn {
   int min_tiles;                             // ... and the least tiles of one
 };
 
+struct PagedLine;
+// A place on the line: tile t of item (b, h, mt).
+struct PagedPlace {
+  int b, h, mt, t, T_b;
+  __device__ __forceinline__ void at(const PagedLine& L, const PagedAttn& P, int x);
+};
+
 // The line of work: item (b, hm) of sequence b, hm = head * tiles + query tile, has tiles_of(b) tiles of positions and begins
 // at pre[b] * hm_n + hm * tiles_of(b). The host keeps the whole line below 2^31 tiles.
 struct PagedLine {
   int pre[PG_MAX_SEQ + 1];                   // tiles per item, summed over the sequences before b
   int len[PG_MAX_SEQ];
-  int total, ctas, q, r;                     // tiles of the line; the first r of `ctas` stretches have q + 1 tiles, the others q
+  int total, ctas, hm_n;                     // tiles of the line, stretches, items per sequence
+  // Stretches of equal length wherever they end: the first r of them have q + 1 tiles, the others q. Or, when that costs
+  // little, stretches that end where items end: parts[b] of them per item of sequence b, cpre[b] before sequence b.
+  int q, r;
+  bool whole_items;
+  int parts[PG_MAX_SEQ], cpre[PG_MAX_SEQ + 1];
+  int x_begin, x_end;                        // this CTA's stretch, empty behind the last, and where it begins
+  PagedPlace first;
 };
 
 // Every thread of the CTA calls it; ends with a barrier.
@@ -78,7 +92,7 @@ __device__ __forceinline__ void paged_line(PagedLine& L, const PagedAttn& P, int
   if (threadIdx.x < 32) {
     const int lane = threadIdx.x;
     int own[2], sum = 0;
-    const int cap = (int)P.c.cap();
+    const int cap = (int)P.c.cap(), hm_n = P.c.hkv * P.tiles;
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       const int b = lane * 2 + u;
@@ -96,43 +110,120 @@ __device__ __forceinline__ void paged_line(PagedLine& L, const PagedAttn& P, int
     }
     L.pre[lane * 2] = inc - sum;
     L.pre[lane * 2 + 1] = inc - sum + own[0];
-    if (lane == 31) {
-      L.pre[PG_MAX_SEQ] = inc;
-      L.total = inc * P.c.hkv * P.tiles;
-      L.ctas = max(1, min(P.ctas, (L.total + P.min_tiles - 1) / P.min_tiles));
-      L.q = L.total / L.ctas;
-      L.r = L.total - L.q * L.ctas;
+    const int all = __shfl_sync(0xffffffffu, inc, 31), total = all * hm_n;
+    const int ctas = max(1, min(P.ctas, (total + P.min_tiles - 1) / P.min_tiles));
+    // Whole items: an item's share of the CTAs, rounded down. A stretch that ends inside an item costs its CTA a merge and a
+    // new start, about two tiles' time, so they are taken when the longest stretch is at most two tiles longer.
+    int n[2], count = 0, worst = 0;
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      n[u] = own[u] > 0 ? max(1, (int)((float)ctas * (float)own[u] / (float)total)) : 0;
+      count += n[u] * hm_n;
+      worst = max(worst, n[u] > 0 ? (own[u] + n[u] - 1) / n[u] : 0);
     }
+    worst = __reduce_max_sync(0xffffffffu, worst);
+    int cinc = count;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int t = __shfl_up_sync(0xffffffffu, cinc, o);
+      if (lane >= o) cinc += t;
+    }
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      L.parts[lane * 2 + u] = n[u];
+      L.cpre[lane * 2 + u] = cinc - count + (u ? n[0] * hm_n : 0);
+    }
+    const int q = total / ctas, r = total - q * ctas;
+    const int ccount = __shfl_sync(0xffffffffu, cinc, 31);
+    const bool whole_items = ccount <= ctas && worst <= q + 2;
+    if (lane == 31) {
+      L.pre[PG_MAX_SEQ] = all;
+      L.cpre[PG_MAX_SEQ] = ccount;
+      L.total = total;
+      L.hm_n = hm_n;
+      L.q = q;
+      L.r = r;
+      L.whole_items = whole_items;
+      L.ctas = whole_items ? max(1, ccount) : ctas;
+    }
+    __syncwarp();
+    // this CTA's stretch; its sequence is the last one that begins at or before it
+    const int cta = blockIdx.x;
+    int xb = 0, xe = 0;
+    if (total > 0 && cta < L.ctas) {
+      const int* pre = whole_items ? L.cpre : L.pre;
+      const int scale = whole_items ? 1 : hm_n;
+      xb = q * cta + min(cta, r);
+      xe = xb + q + (cta < r ? 1 : 0);
+      const int key = whole_items ? cta : xb;
+      const int b = __popc(__ballot_sync(0xffffffffu, pre[lane] * scale <= key)) + __popc(__ballot_sync(0xffffffffu, pre[lane + 32] * scale <= key)) - 1;
+      const int T_b = L.pre[b + 1] - L.pre[b];
+      int hm, t;
+      if (whole_items) {
+        const int np = L.parts[b], k = cta - L.cpre[b], j = k % np, pq = T_b / np, pr = T_b - pq * np;
+        hm = k / np;
+        t = pq * j + min(j, pr);
+        xb = L.pre[b] * hm_n + hm * T_b + t;
+        xe = xb + pq + (j < pr ? 1 : 0);
+      } else {
+        hm = (xb - L.pre[b] * hm_n) / T_b;
+        t = xb - L.pre[b] * hm_n - hm * T_b;
+      }
+      if (lane == 0) {
+        L.first.b = b;
+        L.first.h = hm / P.tiles;
+        L.first.mt = hm - hm / P.tiles * P.tiles;
+        L.first.t = t;
+        L.first.T_b = T_b;
+      }
+    }
+    if (lane == 0) { L.x_begin = xb; L.x_end = xe; }
   }
   __syncthreads();
 }
-__device__ __forceinline__ int line_begin(const PagedLine& L, int cta) { return L.q * cta + min(cta, L.r); }
+// the b with pre[b] * scale <= x < pre[b + 1] * scale
+__device__ __forceinline__ int line_seq(const int* pre, int scale, int x) {
+  int b = 0, hi = PG_MAX_SEQ;
+  while (hi - b > 1) {
+    const int mid = (b + hi) >> 1;
+    if (pre[mid] * scale <= x) b = mid; else hi = mid;
+  }
+  return b;
+}
+__device__ __forceinline__ int line_begin(const PagedLine& L, int cta) {
+  if (!L.whole_items) return L.q * cta + min(cta, L.r);
+  if (cta >= L.ctas) return L.total;
+  const int b = line_seq(L.cpre, 1, cta), n = L.parts[b], T_b = L.pre[b + 1] - L.pre[b];
+  const int k = cta - L.cpre[b], item = k / n, j = k - item * n, q = T_b / n;
+  return L.pre[b] * L.hm_n + item * T_b + q * j + min(j, T_b - q * n);
+}
 // the CTA whose stretch holds tile x < total
 __device__ __forceinline__ int line_owner(const PagedLine& L, int x) {
-  const int wide = L.r * (L.q + 1);
-  return x < wide ? x / (L.q + 1) : L.r + (x - wide) / L.q;
-}
-// The piece that CTA c holds of an item that begins at x0: its first place unless the item begins inside its stretch.
-__device__ __forceinline__ int piece_of(const PagedLine& L, int c, int x0) { return c * 2 + (line_begin(L, c) >= x0 ? 0 : 1); }
-
-// A place on the line: tile t of item (b, h, mt).
-struct PagedPlace {
-  int b, h, mt, t, T_b;
-  __device__ __forceinline__ void at(const PagedLine& L, const PagedAttn& P, int x) {
-    const int hm_n = P.c.hkv * P.tiles;
-    int hi = P.c.batch;                      // pre[b] * hm_n <= x < pre[hi] * hm_n
-    if (x < L.pre[b + 1] * hm_n) hi = b + 1;
-    while (hi - b > 1) {
-      const int mid = (b + hi) >> 1;
-      if (L.pre[mid] * hm_n <= x) b = mid; else hi = mid;
-    }
-    T_b = L.pre[b + 1] - L.pre[b];
-    const int in_b = x - L.pre[b] * hm_n, hm = in_b / T_b;
-    h = hm / P.tiles;
-    mt = hm - h * P.tiles;
-    t = in_b - hm * T_b;
+  int q = L.q, r = L.r, c = 0;
+  if (L.whole_items) {
+    const int b = line_seq(L.pre, L.hm_n, x), n = L.parts[b], T_b = L.pre[b + 1] - L.pre[b];
+    const int in_b = x - L.pre[b] * L.hm_n, item = in_b / T_b;
+    x = in_b - item * T_b;
+    c = L.cpre[b] + item * n;
+    q = T_b / n;
+    r = T_b - q * n;
   }
-};
+  const int wide = r * (q + 1);
+  return c + (x < wide ? x / (q + 1) : r + (x - wide) / q);
+}
+// The piece that CTA c holds of an item that begins at x0 and that CTA c0 is the first to hold: its first place, unless the
+// item begins inside its stretch, which is so for c0 at most. first_place: c0's.
+__device__ __forceinline__ int first_place(const PagedLine& L, int c0, int x0) { return line_begin(L, c0) >= x0 ? 0 : 1; }
+__device__ __forceinline__ int piece_of(int c, int c0, int first) { return c * 2 + (c == c0 ? first : 0); }
+
+__device__ __forceinline__ void PagedPlace::at(const PagedLine& L, const PagedAttn& P, int x) {
+  b = line_seq(L.pre, L.hm_n, x);
+  T_b = L.pre[b + 1] - L.pre[b];
+  const int in_b = x - L.pre[b] * L.hm_n, hm = in_b / T_b;
+  h = hm / P.tiles;
+  mt = hm - h * P.tiles;
+  t = in_b - hm * T_b;
+}
 
 // Which of the new slots some row sees: the others are not read at all (what lies there may be anything).
 __device__ __forceinline__ unsigned long long causal_word(int i) { return i >= 63 ? ~0ull : (2ull << i) - 1ull; }
@@ -158,6 +249,10 @@ __device__ __forceinline__ unsigned long long row_word(const PagedAttn& P, int b
 // ---------------------------------------------------------------------------------------------
 template <typename T, int DH> struct PagedWarp;
 
+// Place of columns d .. d + 7 (d a multiple of 4) of row r in a warp's output of [16][DH] floats.
+template <int DH>
+__device__ __forceinline__ int pg_at(int r, int d) { return r * DH + ((((d >> 3) ^ r) & (DH / 8 - 1)) << 3) + (d & 7); }
+
 template <int DH>
 struct PagedWarp<bf16, DH> {
   static constexpr int KW = 16;              // positions per warp step
@@ -167,7 +262,9 @@ struct PagedWarp<bf16, DH> {
   float m[2], l[2];
   int gq, tq;
 
-  __device__ __forceinline__ void start(const PagedAttn& P, int b, int h, int mt, uint8_t*) {
+  // The queries' loads may go out while the last item is merged; they are used by the next step.
+  static constexpr bool EARLY = true;
+  __device__ __forceinline__ void load(const PagedAttn& P, int b, int h, int mt, uint8_t*) {
     const int lane = threadIdx.x & 31;
     gq = lane >> 2; tq = lane & 3;
     const int R = P.n * P.group;
@@ -183,6 +280,8 @@ struct PagedWarp<bf16, DH> {
         qf[ks][2 + u] = __ldg(src + ks * 8 + 4 + tq);
       }
     }
+  }
+  __device__ __forceinline__ void clear() {
 #pragma unroll
     for (int i = 0; i < DH / 8; ++i) { o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f; }
     m[0] = m[1] = -INFINITY;
@@ -284,18 +383,20 @@ struct PagedWarp<bf16, DH> {
     }
   }
 
-  // Leaves (max, sum) and the output of this warp's 16 rows in shared memory: so [16][DH], sml [16][2].
-  __device__ __forceinline__ void finish(float* so, float* sml) {
+  // Leaves (max, sum) and the output of this warp's first `rows` rows in shared memory: so [16][DH] (8 columns of a row at the
+  // place pg_at gives, so that the 8 rows of a store meet different banks), sml [16][2].
+  __device__ __forceinline__ void finish(float* so, float* sml, int rows) {
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       float t = l[u];
       t += __shfl_xor_sync(0xffffffffu, t, 1);
       t += __shfl_xor_sync(0xffffffffu, t, 2);
       const int r = gq + 8 * u;
+      if (r >= rows) continue;
       if (tq == 0) { sml[r * 2] = m[u]; sml[r * 2 + 1] = t; }
 #pragma unroll
       for (int i = 0; i < DH / 8; ++i)
-        *reinterpret_cast<float2*>(so + r * DH + i * 8 + 2 * tq) = make_float2(o[i][2 * u], o[i][2 * u + 1]);
+        *reinterpret_cast<float2*>(so + pg_at<DH>(r, i * 8) + 2 * tq) = make_float2(o[i][2 * u], o[i][2 * u + 1]);
     }
   }
 };
@@ -318,7 +419,8 @@ struct PagedWarp<float, DH> {
 
   float mrow, lrow;                          // running max and sum of row (lane & 15); both half-warps hold the same
 
-  __device__ __forceinline__ void start(const PagedAttn& P, int b, int h, int mt, uint8_t* extra) {
+  static constexpr bool EARLY = false;       // the queries are shared by the warps
+  __device__ __forceinline__ void load(const PagedAttn& P, int b, int h, int mt, uint8_t* extra) {
     const int R = P.n * P.group;
     sq = reinterpret_cast<float*>(extra);
     sp = sq + PG_ROWS * DH + (threadIdx.x >> 5) * (KW + 1) * PG_ROWS;
@@ -332,13 +434,15 @@ struct PagedWarp<float, DH> {
                                                   (long long)(h * P.group + r % P.group) * DH) + c);
       reinterpret_cast<float4*>(sq)[i] = x;
     }
+    __syncthreads();
+  }
+  __device__ __forceinline__ void clear() {
 #pragma unroll
     for (int r = 0; r < PG_ROWS; ++r)
 #pragma unroll
       for (int d = 0; d < DL; ++d) o[r][d] = 0.f;
     mrow = -INFINITY;
     lrow = 0.f;
-    __syncthreads();
   }
 
   // 16-byte chunk of a row, swizzled by the row
@@ -441,13 +545,13 @@ struct PagedWarp<float, DH> {
     __syncwarp();
   }
 
-  __device__ __forceinline__ void finish(float* so, float* sml) {
+  __device__ __forceinline__ void finish(float* so, float* sml, int) {
     const int lane = threadIdx.x & 31;
     if (lane < 16) { sml[lane * 2] = mrow; sml[lane * 2 + 1] = lrow; }
 #pragma unroll
     for (int r = 0; r < PG_ROWS; ++r)
 #pragma unroll
-      for (int d = 0; d < DL; ++d) so[r * DH + lane * DL + d] = o[r][d];
+      for (int d = 0; d < DL; ++d) so[pg_at<DH>(r, lane * DL) + d] = o[r][d];
   }
 };
 
@@ -479,33 +583,34 @@ __global__ void __launch_bounds__(PG_THREADS, 1) paged_rows_kernel(const PagedAt
   __shared__ PagedLine L;
   __shared__ unsigned int live_of[PG_WARPS][PG_STAGES];
   __shared__ float sml[PG_WARPS][PG_ROWS][2];
-  __shared__ int s_last;
+  __shared__ int s_last[2], s_join[2][6];    // cut items of this CTA: whether it delivered the last piece; x0, b, h, mt, first and last CTA
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   uint8_t* const extra = pg_smem + PG_WARPS * C::RING;
   uint8_t* const ring = pg_smem + warp * C::RING;
   const uint32_t ring_s = smem_u32(ring);
   pdl_wait(KID_ATTN);
   paged_line(L, P, C::TILE);
-  const int total = L.total;
-  if (total == 0 || (int)blockIdx.x >= L.ctas) return;
-  const int x_begin = line_begin(L, blockIdx.x), x_end = line_begin(L, blockIdx.x + 1);
+  const int x_begin = L.x_begin, x_end = L.x_end;
+  if (x_begin == x_end) return;
+  if (threadIdx.x < 2) s_last[threadIdx.x] = 0;
   const int R = P.n * P.group;
   const int cap = (int)P.c.cap();
 
   // ---- copies: place of the next step that is asked for, two steps ahead of the one that is worked on ----
-  PagedPlace F;
-  F.b = 0;
-  F.at(L, P, x_begin);
+  PagedPlace F = L.first;
   int f_x = x_begin, f_len = L.len[F.b], f_keys = min(f_len + P.n_new, cap);
   unsigned long long f_any = any_word(P, F.b);
   const int ch = lane % C::CH, r_first = lane / C::CH;
   constexpr int R_STEP = 32 / C::CH;
   // A step's rows -> this warp's ring. A row that does not exist is zero-filled: zero times what lies there may not be zero.
-  auto issue = [&](int st) {
-    const int base = F.t * C::TILE + warp * C::KW, key = base + lane;
-    const uint32_t dK = ring_s + st * C::STAGE, dV = dK + C::HALF;
-    long long off = 0;
-    int src = 0;                                                   // 0: does not exist, 1: page, 2: new row
+  // look() finds the row of this lane's position of step F and moves F on; a step ahead of the copies that use it, so that they
+  // do not wait for the table.
+  long long off = 0;
+  int src = 0;                                // src 0: does not exist, 1: page, 2: new row
+  auto look = [&]() {
+    src = 0;
+    if (f_x >= x_end) return;
+    const int key = F.t * C::TILE + warp * C::KW + lane;
     if (lane < C::KW && key < f_keys) {
       if (key >= f_len && !((f_any >> (key - f_len)) & 1ull)) {
         src = 0;
@@ -518,6 +623,15 @@ __global__ void __launch_bounds__(PG_THREADS, 1) paged_rows_kernel(const PagedAt
         off += (long long)F.h * DH;
       }
     }
+    if (++F.t == F.T_b && f_x + 1 < x_end) {
+      F.at(L, P, f_x + 1);
+      f_len = L.len[F.b];
+      f_keys = min(f_len + P.n_new, cap);
+      f_any = any_word(P, F.b);
+    }
+  };
+  auto issue = [&](int st) {
+    const uint32_t dK = ring_s + st * C::STAGE, dV = dK + C::HALF;
     const unsigned live = __ballot_sync(0xffffffffu, src != 0), fresh = __ballot_sync(0xffffffffu, src == 2);
     if (lane == 0) live_of[warp][st] = live;
 #pragma unroll
@@ -532,16 +646,12 @@ __global__ void __launch_bounds__(PG_THREADS, 1) paged_rows_kernel(const PagedAt
       cp_async16(dV + d, vp, ok);
     }
     ++f_x;
-    if (++F.t == F.T_b && f_x < x_end) {
-      F.at(L, P, f_x);
-      f_len = L.len[F.b];
-      f_keys = min(f_len + P.n_new, cap);
-      f_any = any_word(P, F.b);
-    }
+    look();
   };
+  look();
   PagedWarp<T, DH> W;
-  PagedPlace S = F;
-  W.start(P, S.b, S.h, S.mt, extra);                                 // the first queries are on their way before the copies
+  PagedPlace S = L.first;
+  W.load(P, S.b, S.h, S.mt, extra);                                  // the first queries are on their way before the copies
 #pragma unroll
   for (int st = 0; st < PG_STAGES - 1; ++st) {
     if (f_x < x_end) issue(st);
@@ -549,12 +659,21 @@ __global__ void __launch_bounds__(PG_THREADS, 1) paged_rows_kernel(const PagedAt
   }
   int st = 0;
   for (int x = x_begin; x < x_end;) {
-    S.at(L, P, x);
+    if (x != x_begin) S.at(L, P, x);
     const int b = S.b, h = S.h, mt = S.mt, t0 = S.t, t1 = min(S.T_b, t0 + (x_end - x));
     const int x0 = x - t0;                                           // the item's first tile on the line
     const int len = L.len[b], keys = min(len + P.n_new, cap);
-    if (x != x_begin) W.start(P, b, h, mt, extra);
+    if (x != x_begin && !W.EARLY) W.load(P, b, h, mt, extra);
+    W.clear();
     const bool full_rows = W.words(P, b, mt, R);                     // every row of this warp's tile sees the committed slots
+    const bool whole = t0 == 0 && t1 == S.T_b;
+    const int place = x == x_begin ? 0 : 1;
+    if (!whole && threadIdx.x == PG_THREADS - 32) {                  // (while the first copies are on their way)
+      int* j = s_join[place];
+      j[0] = x0; j[1] = b; j[2] = h; j[3] = mt;
+      j[4] = place ? (int)blockIdx.x : line_owner(L, x0);
+      j[5] = line_owner(L, x0 + S.T_b - 1);
+    }
     for (int t = t0; t < t1; ++t) {
       if (f_x < x_end) issue(st == 0 ? PG_STAGES - 1 : st - 1);      // the stage of the step before this one
       cp_async_commit();
@@ -602,17 +721,19 @@ __global__ void __launch_bounds__(PG_THREADS, 1) paged_rows_kernel(const PagedAt
       __syncwarp();
       if (t + 1 < t1) st = st == PG_STAGES - 1 ? 0 : st + 1;
     }
-    // ---- merge of the warps, through the stage that was read last ----
-    W.finish(reinterpret_cast<float*>(ring + st * C::STAGE), &sml[warp][0][0]);
+    // ---- merge of the warps, through the stage that was read last; the next item's queries set out before ----
+    const int rows = min(PG_ROWS, R - mt * PG_ROWS), xn = x + (t1 - t0);
+    if (W.EARLY && xn < x_end) {
+      PagedPlace N = S;
+      N.at(L, P, xn);
+      W.load(P, N.b, N.h, N.mt, extra);
+    }
+    W.finish(reinterpret_cast<float*>(ring + st * C::STAGE), &sml[warp][0][0], rows);
     __syncthreads();
-    const bool whole = t0 == 0 && t1 == S.T_b;
     const int item = (b * P.c.hkv + h) * P.tiles + mt;
-    const int c0 = whole ? 0 : line_owner(L, x0), c1 = whole ? 0 : line_owner(L, x0 + S.T_b - 1);
-    const size_t prow = (size_t)piece_of(L, blockIdx.x, x0) * PG_ROWS;
-    for (int i = threadIdx.x; i < PG_ROWS * (DH / 4); i += PG_THREADS) {
-      const int r = i / (DH / 4), c = i - r * (DH / 4);
-      const int rr = mt * PG_ROWS + r;
-      if (rr >= R) break;
+    const size_t prow = ((size_t)blockIdx.x * 2 + place) * PG_ROWS;
+    for (int i = threadIdx.x; i < rows * (DH / 4); i += PG_THREADS) {
+      const int r = i / (DH / 4), c = i - r * (DH / 4), rr = mt * PG_ROWS + r;
       float M = -INFINITY;
 #pragma unroll
       for (int w = 0; w < PG_WARPS; ++w) M = fmaxf(M, sml[w][r][0]);
@@ -623,7 +744,7 @@ __global__ void __launch_bounds__(PG_THREADS, 1) paged_rows_kernel(const PagedAt
       for (int w = 0; w < PG_WARPS; ++w) {
         const float f = exp2f(sml[w][r][0] - ref);
         Z = fmaf(f, sml[w][r][1], Z);
-        const float4 y = *reinterpret_cast<const float4*>(pg_smem + w * C::RING + st * C::STAGE + (r * DH + c * 4) * 4);
+        const float4 y = *reinterpret_cast<const float4*>(pg_smem + w * C::RING + st * C::STAGE + pg_at<DH>(r, c * 4) * 4);
         a.x = fmaf(f, y.x, a.x); a.y = fmaf(f, y.y, a.y); a.z = fmaf(f, y.z, a.z); a.w = fmaf(f, y.w, a.w);
       }
       if (whole) {
@@ -637,59 +758,90 @@ __global__ void __launch_bounds__(PG_THREADS, 1) paged_rows_kernel(const PagedAt
         if (c == 0) __stcg(reinterpret_cast<float2*>(P.part_ml + (prow + r) * 2), make_float2(M, Z));
       }
     }
-    if (!whole) {
-      // ---- join: the CTA that delivers the item's last piece adds all of them ----
+    __syncthreads();                                                 // the merge is read before its stage fills again
+    if (!whole && threadIdx.x == 0) {
+      // The piece is delivered; who delivers an item's last one joins them, at the end, when nothing else waits for it. (The
+      // barrier and this thread's fence order the CTA's stores before the count.)
+      const int c0 = s_join[place][4], c1 = s_join[place][5];
       __threadfence();
-      __syncthreads();
-      if (threadIdx.x == 0) {
-        s_last = atomicAdd(P.arrived + c0, 1) == c1 - c0;
-        if (s_last) P.arrived[c0] = 0;                               // as the next call expects it
-      }
-      __syncthreads();
-      if (s_last) {
-        __threadfence();
-        for (int i = threadIdx.x; i < PG_ROWS * (DH / 4); i += PG_THREADS) {
-          const int r = i / (DH / 4), c = i - r * (DH / 4);
-          const int rr = mt * PG_ROWS + r;
-          if (rr >= R) break;
-          float M = -INFINITY, Z = 0.f;
-          float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
-          // pieces in order, eight loads under way at a time; the sums move to a new reference when the maximum grows
-          for (int p0 = c0; p0 <= c1; p0 += 8) {
-            float2 ml[8];
-            float4 o[8];
+      s_last[place] = atomicAdd(P.arrived + c0, 1) == c1 - c0;
+    }
+    x = xn;
+    st = st == PG_STAGES - 1 ? 0 : st + 1;
+  }
+
+  // ---- join: pieces in the order of their positions, a group of threads for every so many of them ----
+  __syncthreads();
+  for (int place = 0; place < 2; ++place) {
+    if (!s_last[place]) continue;                                    // the same for the whole CTA
+    const int x0 = s_join[place][0], b = s_join[place][1], h = s_join[place][2], mt = s_join[place][3], c0 = s_join[place][4], c1 = s_join[place][5];
+    if (threadIdx.x == 0) P.arrived[c0] = 0;                         // as the next call expects it
+    __threadfence();
+    const int rows = min(PG_ROWS, R - mt * PG_ROWS), units = rows * (DH / 4), np = c1 - c0 + 1;
+    const int fp = first_place(L, c0, x0);
+    const int subs = max(1, min(PG_THREADS / units, (np + 7) / 8)), each = (np + subs - 1) / subs;
+    float* sub_o = reinterpret_cast<float*>(pg_smem);                // [sub][unit][6]; the rings are empty
+    for (int u0 = 0; u0 < units; u0 += PG_THREADS) {
+      const int sub = threadIdx.x / units, unit = subs > 1 ? threadIdx.x - sub * units : u0 + threadIdx.x;
+      const bool work = sub < subs && unit < units;
+      const int r = unit / (DH / 4), c = unit - r * (DH / 4), rr = mt * PG_ROWS + r;
+      float M = -INFINITY, Z = 0.f;
+      float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+      auto add = [&](float m, float z, const float4& o, float ref) {
+        const float f = exp2f(m - ref);
+        Z = fmaf(f, z, Z);
+        a.x = fmaf(f, o.x, a.x); a.y = fmaf(f, o.y, a.y); a.z = fmaf(f, o.z, a.z); a.w = fmaf(f, o.w, a.w);
+      };
+      if (work) {
+        const int p_end = min(c1 + 1, c0 + (sub + 1) * each);
+        for (int p0 = c0 + sub * each; p0 < p_end; p0 += 8) {        // eight loads under way; the sums move to a new reference
+          float2 ml[8];
+          float4 o[8];
 #pragma unroll
-            for (int u = 0; u < 8; ++u) {
-              const size_t at = (size_t)piece_of(L, min(p0 + u, c1), x0) * PG_ROWS + r;
-              ml[u] = __ldcg(reinterpret_cast<const float2*>(P.part_ml + at * 2));
-              o[u] = __ldcg(reinterpret_cast<const float4*>(P.part_o + at * DH + c * 4));
-            }
-            float mx = M;
-#pragma unroll
-            for (int u = 0; u < 8; ++u) mx = fmaxf(mx, ml[u].x);
-            const float ref = mx == -INFINITY ? 0.f : mx, g = exp2f(M - ref);
-            Z *= g;
-            a.x *= g; a.y *= g; a.z *= g; a.w *= g;
-#pragma unroll
-            for (int u = 0; u < 8; ++u) {
-              if (p0 + u > c1) continue;
-              const float f = exp2f(ml[u].x - ref);
-              Z = fmaf(f, ml[u].y, Z);
-              a.x = fmaf(f, o[u].x, a.x); a.y = fmaf(f, o[u].y, a.y); a.z = fmaf(f, o[u].z, a.z); a.w = fmaf(f, o[u].w, a.w);
-            }
-            M = mx;
+          for (int u = 0; u < 8; ++u) {
+            const size_t at = (size_t)piece_of(min(p0 + u, p_end - 1), c0, fp) * PG_ROWS + r;
+            ml[u] = __ldcg(reinterpret_cast<const float2*>(P.part_ml + at * 2));
+            o[u] = __ldcg(reinterpret_cast<const float4*>(P.part_o + at * DH + c * 4));
           }
-          const float inv = Z == 0.f ? 0.f : 1.f / Z;
-          if (Z == 0.f) a = make_float4(0.f, 0.f, 0.f, 0.f);
-          store4((T*)P.out + (((size_t)b * P.n + rr / P.group) * P.hq + h * P.group + rr % P.group) * DH + c * 4,
-                 make_float4(a.x * inv, a.y * inv, a.z * inv, a.w * inv));
-          if (c == 0 && P.score) { P.item_ml[((size_t)item * PG_ROWS + r) * 2] = M; P.item_ml[((size_t)item * PG_ROWS + r) * 2 + 1] = Z; }
+          float mx = M;
+#pragma unroll
+          for (int u = 0; u < 8; ++u) mx = fmaxf(mx, ml[u].x);
+          const float ref = mx == -INFINITY ? 0.f : mx, g = exp2f(M - ref);
+          Z *= g;
+          a.x *= g; a.y *= g; a.z *= g; a.w *= g;
+#pragma unroll
+          for (int u = 0; u < 8; ++u)
+            if (p0 + u < p_end) add(ml[u].x, ml[u].y, o[u], ref);
+          M = mx;
         }
       }
+      if (subs > 1) {                                                // units <= the CTA's threads: one round
+        float* t = sub_o + (sub * units + unit) * 6;
+        if (work && sub > 0) { t[0] = M; t[1] = Z; t[2] = a.x; t[3] = a.y; t[4] = a.z; t[5] = a.w; }
+        __syncthreads();
+        if (work && sub == 0) {
+          float mx = M;
+          for (int q = 1; q < subs; ++q) mx = fmaxf(mx, sub_o[(q * units + unit) * 6]);
+          const float ref = mx == -INFINITY ? 0.f : mx, g = exp2f(M - ref);
+          Z *= g;
+          a.x *= g; a.y *= g; a.z *= g; a.w *= g;
+          for (int q = 1; q < subs; ++q) {
+            const float* y = sub_o + (q * units + unit) * 6;
+            add(y[0], y[1], make_float4(y[2], y[3], y[4], y[5]), ref);
+          }
+          M = mx;
+        }
+        __syncthreads();
+      }
+      if (work && sub == 0) {
+        const float inv = Z == 0.f ? 0.f : 1.f / Z;
+        if (Z == 0.f) a = make_float4(0.f, 0.f, 0.f, 0.f);
+        store4((T*)P.out + (((size_t)b * P.n + rr / P.group) * P.hq + h * P.group + rr % P.group) * DH + c * 4,
+               make_float4(a.x * inv, a.y * inv, a.z * inv, a.w * inv));
+        const int item = (b * P.c.hkv + h) * P.tiles + mt;
+        if (c == 0 && P.score) { P.item_ml[((size_t)item * PG_ROWS + r) * 2] = M; P.item_ml[((size_t)item * PG_ROWS + r) * 2 + 1] = Z; }
+      }
     }
-    x += t1 - t0;
-    st = st == PG_STAGES - 1 ? 0 : st + 1;
-    __syncthreads();                                                 // the merge is read before its stage fills again
   }
 }
 

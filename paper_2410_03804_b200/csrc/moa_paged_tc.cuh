@@ -62,18 +62,17 @@ __global__ void __launch_bounds__(256) paged_join_kernel(const PagedAttn P, int 
   const int c = blockIdx.x + 1;
   if (L.total == 0 || c >= L.ctas) return;
   PagedPlace S;
-  S.b = 0;
   const int x = line_begin(L, c);
   S.at(L, P, x);
   const int x0 = x - S.t;
   if (S.t == 0 || line_owner(L, x0) != c - 1) return;
-  const int c1 = line_owner(L, x0 + S.T_b - 1);
+  const int c1 = line_owner(L, x0 + S.T_b - 1), fp = first_place(L, c - 1, x0);
   const int r = threadIdx.x, rr = S.mt * PT_ROWS + r;                // row of the item, of the (sequence, head)
   const int R = P.n * P.group;
   if ((rr & ~31) >= R) return;
   float M = -INFINITY, Z = 0.f;
 #pragma unroll 4
-  for (int i = c - 1; i <= c1; ++i) M = fmaxf(M, __ldg(P.part_ml + ((size_t)piece_of(L, i, x0) * PT_ROWS + r) * 2));
+  for (int i = c - 1; i <= c1; ++i) M = fmaxf(M, __ldg(P.part_ml + ((size_t)piece_of(i, c - 1, fp) * PT_ROWS + r) * 2));
   const float ref = M == -INFINITY ? 0.f : M;
   constexpr int N4 = DH / 16;                                        // 16-byte pieces of a row in a quarter
   float4 a[N4];
@@ -81,7 +80,7 @@ __global__ void __launch_bounds__(256) paged_join_kernel(const PagedAttn P, int 
   for (int d = 0; d < N4; ++d) a[d] = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 2
   for (int i = c - 1; i <= c1; ++i) {
-    const size_t piece = piece_of(L, i, x0);
+    const size_t piece = piece_of(i, c - 1, fp);
     const float2 ml = __ldg(reinterpret_cast<const float2*>(P.part_ml) + piece * PT_ROWS + r);
     const float f = exp2f(ml.x - ref);
     Z = fmaf(f, ml.y, Z);
@@ -112,13 +111,13 @@ struct PtWalk {
   int b, h, pair, t0, nb, x0;
   bool whole;
   __device__ __forceinline__ void begin(const PagedLine& L) {
-    x = x_begin = line_begin(L, blockIdx.x);
-    x_end = line_begin(L, blockIdx.x + 1);
-    S.b = 0;
+    x = x_begin = L.x_begin;
+    x_end = L.x_end;
+    S = L.first;
   }
   __device__ __forceinline__ bool next(const PagedLine& L, const PagedAttn& P) {
     if (x >= x_end) return false;
-    S.at(L, P, x);
+    if (x != x_begin) S.at(L, P, x);
     b = S.b; h = S.h; pair = S.mt; t0 = S.t; x0 = x - t0;
     nb = min(S.T_b - t0, x_end - x);
     whole = nb == S.T_b;
@@ -206,7 +205,7 @@ __global__ void __launch_bounds__(PT_THREADS, 1) paged_tree_kernel(const __grid_
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
-  const bool idle = (int)blockIdx.x >= L.ctas || L.total == 0;
+  const bool idle = L.x_begin == L.x_end;
   PtWalk W;
   if (!idle) W.begin(L);
 
@@ -471,7 +470,7 @@ __global__ void __launch_bounds__(PT_THREADS, 1) paged_tree_kernel(const __grid_
       if (!dead) dead = __any_sync(0xffffffffu, !mbar_wait(o_bar(i), (c - 1u) & 1u, abort_flag));
       tc_fence_after();
       const float inv = dead ? __int_as_float(0x7fffffff) : l_run == 0.f ? 0.f : 1.f / l_run;
-      const size_t piece_at = (size_t)piece_of(L, blockIdx.x, W.x0), prow = piece_at * PT_ROWS + i * 128 + row;
+      const size_t piece_at = (size_t)blockIdx.x * 2 + (W.x0 > W.x_begin ? 1 : 0), prow = piece_at * PT_ROWS + i * 128 + row;
       const bool none = l_run == 0.f && !dead;                       // the row sees nothing
 #pragma unroll 1
       for (int d = 0; d < DH; d += 16) {
