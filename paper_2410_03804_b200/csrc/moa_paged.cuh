@@ -5,7 +5,7 @@
 //
 // What bounds it: one token reads every cached byte once for 4 * group multiply-adds per 4 bytes (bf16), so the cache
 // stream from HBM does. The layout follows from that: the queries that share a key / value head -- (rows of the sequence)
-// x (heads of the group) -- are stacked 16 to a tile, so a cached row is read once per 16 of them.
+// x (heads of the group) -- are stacked 8 to a tile, so a cached row is read once per 8 of them.
 //
 // Work split (paged_rows_kernel): the (sequence, head, query tile) items are laid end to end as tiles of positions, and
 // the CTAs take equal consecutive stretches of that line, whatever the sequences' lengths are; the lengths are read on
@@ -26,7 +26,7 @@ namespace moa {
 constexpr int PG_WARPS = 8;
 constexpr int PG_THREADS = PG_WARPS * 32;
 constexpr int PG_STAGES = 3;
-constexpr int PG_ROWS = 16;                  // query rows per tile
+constexpr int PG_ROWS = 8;                   // query rows per tile
 constexpr int PG_MAX_SEQ = 64;               // sequences per call
 
 // The cache of one layer as the kernels see it. T [n_pages, page_size, hkv, dh], pages page_stride elements apart.
@@ -239,27 +239,36 @@ __device__ __forceinline__ unsigned long long row_word(const PagedAttn& P, int b
   return P.mask ? __ldg(P.mask + (size_t)b * P.n + i) : causal_word(i);
 }
 
-// One warp's running state over a 16-row query tile, merged over the CTA's warps at the end of an item.
-// (max in the log2 domain, sum, output) of row r, all in fp32.
+// PagedWarp: one warp's running state over a query tile (maxima in the log2 domain, sums, outputs, all in fp32), merged over the
+// CTA's warps at the end of an item.
 
 // ---------------------------------------------------------------------------------------------
-// bf16: mma.sync m16n8k16, 16 positions per warp step. Scores and output accumulate in fp32. Probabilities enter the
-// second product as two bf16 terms (hi + lo, 16 bits of mantissa): rounding them once to 8 bits would put an error of up
-// to 2^-9 of every term into the output, and the tensor pipe has room (48 products per 8 KB of cache).
+// bf16: mma.sync m16n8k16, 16 positions per warp step, with the positions (then the columns of V) as the 16 rows of the left
+// operand and the queries as its 8 columns: S^T = K Q^T, O^T = V^T P^T. A group has 8 query heads at most as a rule, so with
+// the queries as the 16 rows half of every product was padding, and the products' issue rate kept 8 warps from getting ahead
+// of the cache's stream. Scores and output accumulate in fp32. Probabilities enter the second product as two bf16 terms
+// (hi + lo, 16 bits of mantissa): rounding them once to 8 bits would put an error of up to 2^-8 of every term into the output.
 // ---------------------------------------------------------------------------------------------
 template <typename T, int DH> struct PagedWarp;
 
-// Place of columns d .. d + 7 (d a multiple of 4) of row r in a warp's output of [16][DH] floats.
+// Place of columns d .. d + 7 (d a multiple of 4) of row r in a warp's output of [PG_ROWS][DH] floats.
 template <int DH>
 __device__ __forceinline__ int pg_at(int r, int d) { return r * DH + ((((d >> 3) ^ r) & (DH / 8 - 1)) << 3) + (d & 7); }
+
+__device__ __forceinline__ uint32_t mat8_trans(uint32_t v) {          // an 8 x 8 matrix of 16-bit values, two per lane, transposed
+  uint32_t r;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+  return r;
+}
 
 template <int DH>
 struct PagedWarp<bf16, DH> {
   static constexpr int KW = 16;              // positions per warp step
   static constexpr int KS = DH / 16;
-  uint32_t qf[KS][4];
-  float o[DH / 8][4];
-  float m[2], l[2];
+  uint32_t qf[KS][2];                        // query gq, columns 16 ks + 2 tq .. and + 8
+  float o[DH / 16][4];                       // columns 16 d + gq and + 8 of queries 2 tq and 2 tq + 1
+  float m[2], l[2];                          // queries 2 tq, 2 tq + 1; l: this lane's positions
+  unsigned long long word[2];                // their mask words
   int gq, tq;
 
   // The queries' loads may go out while the last item is merged; they are used by the next step.
@@ -267,33 +276,27 @@ struct PagedWarp<bf16, DH> {
   __device__ __forceinline__ void load(const PagedAttn& P, int b, int h, int mt, uint8_t*) {
     const int lane = threadIdx.x & 31;
     gq = lane >> 2; tq = lane & 3;
-    const int R = P.n * P.group;
+    const int R = P.n * P.group, r = mt * PG_ROWS + gq;
+    const int rc = r < R ? r : 0;            // queries behind the last one are worked on and not written
+    const uint32_t* src = reinterpret_cast<const uint32_t*>((const bf16*)P.q + ((long long)b * P.n + rc / P.group) * P.q_stride +
+                                                            (long long)(h * P.group + rc % P.group) * DH);
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      const int r = mt * PG_ROWS + gq + 8 * u;
-      const int rc = r < R ? r : 0;          // rows behind the last one are worked on and not written
-      const uint32_t* src = reinterpret_cast<const uint32_t*>((const bf16*)P.q + ((long long)b * P.n + rc / P.group) * P.q_stride +
-                                                              (long long)(h * P.group + rc % P.group) * DH);
-#pragma unroll
-      for (int ks = 0; ks < KS; ++ks) {
-        qf[ks][u] = __ldg(src + ks * 8 + tq);
-        qf[ks][2 + u] = __ldg(src + ks * 8 + 4 + tq);
-      }
+    for (int ks = 0; ks < KS; ++ks) {
+      qf[ks][0] = __ldg(src + ks * 8 + tq);
+      qf[ks][1] = __ldg(src + ks * 8 + 4 + tq);
     }
   }
   __device__ __forceinline__ void clear() {
 #pragma unroll
-    for (int i = 0; i < DH / 8; ++i) { o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f; }
+    for (int i = 0; i < DH / 16; ++i) { o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f; }
     m[0] = m[1] = -INFINITY;
     l[0] = l[1] = 0.f;
   }
-
-  unsigned long long word[2];                // mask words of this thread's two rows
   __device__ __forceinline__ bool words(const PagedAttn& P, int b, int mt, int R) {
     bool full = true;
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-      const int rr = mt * PG_ROWS + gq + 8 * u;
+      const int rr = mt * PG_ROWS + 2 * tq + u;
       word[u] = rr < R ? row_word(P, b, rr / P.group) : 0ull;
       full = full && (rr >= R || word[u] != 0ull);
     }
@@ -306,97 +309,84 @@ struct PagedWarp<bf16, DH> {
   __device__ __forceinline__ void step(const PagedAttn& P, const uint8_t* K, const uint8_t* V, bool plain, See see, float* score, int, int mt, int R) {
     const int lane = threadIdx.x & 31;
     const uint32_t sK = smem_u32(K), sV = smem_u32(V);
-    float s[2][2][4];                        // [chain][8 positions][fragment]: two chains halve the products' latency
+    float s[2][4];                           // two chains halve the products' latency
 #pragma unroll
-    for (int c = 0; c < 2; ++c)
+    for (int c = 0; c < 2; ++c) s[c][0] = s[c][1] = s[c][2] = s[c][3] = 0.f;
 #pragma unroll
-      for (int nt = 0; nt < 2; ++nt) s[c][nt][0] = s[c][nt][1] = s[c][nt][2] = s[c][nt][3] = 0.f;
-#pragma unroll
-    for (int ks2 = 0; ks2 < KS / 2; ++ks2) {
-      uint32_t kb[2][4];
-#pragma unroll
-      for (int nt = 0; nt < 2; ++nt)
-        ldsm_x4(sK + tile_off<DH>(nt * 8 + (lane & 7), ks2 * 4 + (lane >> 3)), kb[nt][0], kb[nt][1], kb[nt][2], kb[nt][3]);
-#pragma unroll
-      for (int nt = 0; nt < 2; ++nt) mma_bf16_16816(s[0][nt], qf[2 * ks2], kb[nt][0], kb[nt][1]);
-#pragma unroll
-      for (int nt = 0; nt < 2; ++nt) mma_bf16_16816(s[1][nt], qf[2 * ks2 + 1], kb[nt][2], kb[nt][3]);
+    for (int ks = 0; ks < KS; ++ks) {
+      uint32_t a[4];
+      ldsm_x4(sK + tile_off<DH>(lane & 15, ks * 2 + (lane >> 4)), a[0], a[1], a[2], a[3]);
+      mma_bf16_16816(s[ks & 1], a, qf[ks][0], qf[ks][1]);
     }
-    float z[2][4];                           // [row u][position nt*8 + 2*tq + e] = z[u][nt*2 + e]
+    float z[2][2];                           // [position gq, gq + 8][query 2 tq, 2 tq + 1]
 #pragma unroll
-    for (int nt = 0; nt < 2; ++nt)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) z[e >> 1][nt * 2 + (e & 1)] = (s[0][nt][e] + s[1][nt][e]) * P.scale_log2;
+    for (int e = 0; e < 4; ++e) z[e >> 1][e & 1] = (s[0][e] + s[1][e]) * P.scale_log2;
     if (!plain) {
 #pragma unroll
-      for (int u = 0; u < 2; ++u)
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (!see(word[u], (i >> 1) * 8 + 2 * tq + (i & 1))) z[u][i] = -INFINITY;
+      for (int e = 0; e < 4; ++e)
+        if (!see(word[e & 1], gq + 8 * (e >> 1))) z[e >> 1][e & 1] = -INFINITY;
     }
-    if (score) {                             // one token: row = head of the group; for the accumulated weights
+    if (score) {                             // one token: query = head of the group; for the accumulated weights
 #pragma unroll
-      for (int u = 0; u < 2; ++u)
-        if (mt * PG_ROWS + gq + 8 * u < R) {
-          float* at = score + (gq + 8 * u) * P.score_ld + 2 * tq;
-          *reinterpret_cast<float2*>(at) = make_float2(z[u][0], z[u][1]);
-          *reinterpret_cast<float2*>(at + 8) = make_float2(z[u][2], z[u][3]);
-        }
+      for (int e = 0; e < 4; ++e) {
+        const int r = 2 * tq + (e & 1);
+        if (mt * PG_ROWS + r < R) score[r * P.score_ld + gq + 8 * (e >> 1)] = z[e >> 1][e & 1];
+      }
     }
     float f[2];
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-      float mx = fmaxf(fmaxf(z[u][0], z[u][1]), fmaxf(z[u][2], z[u][3]));
-      mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
-      mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
+      float mx = fmaxf(z[0][u], z[1][u]);
+      mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
+      mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
+      mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
       const float mn = fmaxf(m[u], mx);
       f[u] = (mn == m[u]) ? 1.f : ex2_approx(m[u] - mn);          // m = -inf: 0
       m[u] = mn;
     }
     if (__any_sync(0xffffffffu, f[0] != 1.f || f[1] != 1.f)) {
 #pragma unroll
-      for (int i = 0; i < DH / 8; ++i) { o[i][0] *= f[0]; o[i][1] *= f[0]; o[i][2] *= f[1]; o[i][3] *= f[1]; }
+      for (int i = 0; i < DH / 16; ++i) { o[i][0] *= f[0]; o[i][1] *= f[1]; o[i][2] *= f[0]; o[i][3] *= f[1]; }
       l[0] *= f[0];
       l[1] *= f[1];
     }
-    uint32_t hi[4], lo[4];                   // A operand: rows gq, gq + 8 x positions 0..7, 8..15
+    const float sub0 = m[0] == -INFINITY ? 0.f : m[0], sub1 = m[1] == -INFINITY ? 0.f : m[1];       // seen nothing: exp2(-inf - 0) = 0
+    uint32_t hi[2], lo[2];                   // right operand: positions 0..7 and 8..15 x queries
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      const float sub = m[u] == -INFINITY ? 0.f : m[u];           // a row that has seen nothing: exp2(-inf - 0) = 0
-#pragma unroll
-      for (int nt = 0; nt < 2; ++nt) {
-        const float p0 = ex2_approx(z[u][nt * 2] - sub), p1 = ex2_approx(z[u][nt * 2 + 1] - sub);
-        l[u] += p0 + p1;
-        const uint32_t w = pack_bf16(p0, p1);
-        hi[nt * 2 + u] = w;
-        lo[nt * 2 + u] = pack_bf16(p0 - __uint_as_float(w << 16), p1 - __uint_as_float(w & 0xffff0000u));
-      }
+    for (int k = 0; k < 2; ++k) {
+      const float p0 = ex2_approx(z[k][0] - sub0), p1 = ex2_approx(z[k][1] - sub1);
+      l[0] += p0;
+      l[1] += p1;
+      const uint32_t w = pack_bf16(p0, p1);
+      hi[k] = mat8_trans(w);
+      lo[k] = mat8_trans(pack_bf16(p0 - __uint_as_float(w << 16), p1 - __uint_as_float(w & 0xffff0000u)));
     }
 #pragma unroll
     for (int d = 0; d < DH / 16; ++d) {
-      uint32_t v0, v1, v2, v3;               // values [16 positions x 16 columns] as two B fragments
-      ldsm_x4_t(sV + tile_off<DH>(lane & 15, d * 2 + (lane >> 4)), v0, v1, v2, v3);
-      mma_bf16_16816(o[2 * d], hi, v0, v1);
-      mma_bf16_16816(o[2 * d + 1], hi, v2, v3);
-      mma_bf16_16816(o[2 * d], lo, v0, v1);
-      mma_bf16_16816(o[2 * d + 1], lo, v2, v3);
+      uint32_t v[4];                         // values transposed: 16 columns x 16 positions
+      ldsm_x4_t(sV + tile_off<DH>((lane & 7) + ((lane >> 4) << 3), d * 2 + ((lane >> 3) & 1)), v[0], v[1], v[2], v[3]);
+      mma_bf16_16816(o[d], v, hi[0], hi[1]);
+      mma_bf16_16816(o[d], v, lo[0], lo[1]);
     }
   }
 
-  // Leaves (max, sum) and the output of this warp's first `rows` rows in shared memory: so [16][DH] (8 columns of a row at the
-  // place pg_at gives, so that the 8 rows of a store meet different banks), sml [16][2].
+  // Leaves (max, sum) and the output of the tile's first `rows` queries in shared memory: so [8][DH] (8 columns of a row at the
+  // place pg_at gives, so that the rows of a store meet different banks), sml [8][2].
   __device__ __forceinline__ void finish(float* so, float* sml, int rows) {
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       float t = l[u];
-      t += __shfl_xor_sync(0xffffffffu, t, 1);
-      t += __shfl_xor_sync(0xffffffffu, t, 2);
-      const int r = gq + 8 * u;
+      t += __shfl_xor_sync(0xffffffffu, t, 4);
+      t += __shfl_xor_sync(0xffffffffu, t, 8);
+      t += __shfl_xor_sync(0xffffffffu, t, 16);
+      const int r = 2 * tq + u;
       if (r >= rows) continue;
-      if (tq == 0) { sml[r * 2] = m[u]; sml[r * 2 + 1] = t; }
+      if (gq == 0) { sml[r * 2] = m[u]; sml[r * 2 + 1] = t; }
 #pragma unroll
-      for (int i = 0; i < DH / 8; ++i)
-        *reinterpret_cast<float2*>(so + pg_at<DH>(r, i * 8) + 2 * tq) = make_float2(o[i][2 * u], o[i][2 * u + 1]);
+      for (int i = 0; i < DH / 16; ++i) {
+        so[pg_at<DH>(r, i * 16) + gq] = o[i][u];
+        so[pg_at<DH>(r, i * 16 + 8) + gq] = o[i][2 + u];
+      }
     }
   }
 };
@@ -411,13 +401,13 @@ struct PagedWarp<float, DH> {
   static constexpr int KW = 8;
   static constexpr int DL = DH / 32;         // output columns per lane
   float o[PG_ROWS][DL];
-  float *sq, *sp;                            // queries [16][DH] of the CTA, this warp's probabilities [8][16]
+  float *sq, *sp;                            // queries of the CTA, this warp's probabilities
   int rows;                                  // query rows of this tile
 
-  // Shared memory behind the rings: queries of the item [16][DH], then per warp probabilities [KW][PG_ROWS] and factors [16].
+  // Shared memory behind the rings: queries of the item [PG_ROWS][DH], then per warp probabilities [KW][PG_ROWS] and factors.
   static constexpr int SMEM = (PG_ROWS * DH + PG_WARPS * (KW + 1) * PG_ROWS) * 4;
 
-  float mrow, lrow;                          // running max and sum of row (lane & 15); both half-warps hold the same
+  float mrow, lrow;                          // running max and sum of row lane % PG_ROWS; the lanes of a row hold the same
 
   static constexpr bool EARLY = false;       // the queries are shared by the warps
   __device__ __forceinline__ void load(const PagedAttn& P, int b, int h, int mt, uint8_t* extra) {
@@ -449,7 +439,7 @@ struct PagedWarp<float, DH> {
   static __device__ __forceinline__ uint32_t off(int row, int chunk) { return (uint32_t)(row * (DH * 4) + ((chunk ^ (row & 7)) << 4)); }
 
   __device__ __forceinline__ bool words(const PagedAttn& P, int b, int mt, int R) {
-    const int rr = mt * PG_ROWS + (threadIdx.x & 15);
+    const int rr = mt * PG_ROWS + (threadIdx.x & (PG_ROWS - 1));
     return __all_sync(0xffffffffu, rr >= R || row_word(P, b, rr / P.group) != 0ull);
   }
 
@@ -482,16 +472,16 @@ struct PagedWarp<float, DH> {
       if (quarter == (r & 3)) sp[kk * PG_ROWS + r] = (plain || see(row_word(P, b, (mt * PG_ROWS + r) / P.group), kk)) ? t * P.scale_log2 : -INFINITY;
     }
     __syncwarp();
-    // softmax statistics: lane r of each half-warp holds row r
+    // softmax statistics: lane r holds row r % PG_ROWS
     {
-      const int r = lane & 15;
+      const int r = lane & (PG_ROWS - 1);
       float z[KW], mx = -INFINITY;
 #pragma unroll
       for (int k = 0; k < KW; ++k) {
         z[k] = r < rows ? sp[k * PG_ROWS + r] : -INFINITY;
         mx = fmaxf(mx, z[k]);
       }
-      if (score && lane < 16 && r < rows) {
+      if (score && lane < PG_ROWS && r < rows) {
 #pragma unroll
         for (int k = 0; k < KW; k += 4) *reinterpret_cast<float4*>(score + r * P.score_ld + k) = make_float4(z[k], z[k + 1], z[k + 2], z[k + 3]);
       }
@@ -505,9 +495,9 @@ struct PagedWarp<float, DH> {
       for (int k = 0; k < KW; ++k) {
         const float p = exp2f(z[k] - sub);
         lrow += p;
-        if (lane < 16) sp[k * PG_ROWS + r] = p;
+        if (lane < PG_ROWS) sp[k * PG_ROWS + r] = p;
       }
-      if (lane < 16) sp[KW * PG_ROWS + r] = f;
+      if (lane < PG_ROWS) sp[KW * PG_ROWS + r] = f;
       if (__any_sync(0xffffffffu, f != 1.f)) {
         __syncwarp();
 #pragma unroll
@@ -547,7 +537,7 @@ struct PagedWarp<float, DH> {
 
   __device__ __forceinline__ void finish(float* so, float* sml, int) {
     const int lane = threadIdx.x & 31;
-    if (lane < 16) { sml[lane * 2] = mrow; sml[lane * 2 + 1] = lrow; }
+    if (lane < PG_ROWS) { sml[lane * 2] = mrow; sml[lane * 2 + 1] = lrow; }
 #pragma unroll
     for (int r = 0; r < PG_ROWS; ++r)
 #pragma unroll
@@ -566,7 +556,7 @@ template <typename T, int DH> struct PagedCfg {
   static constexpr int RING = PG_STAGES * STAGE;                // of one warp
   static constexpr int EXTRA = sizeof(T) == 4 ? PagedWarp<float, DH>::SMEM : 0;
   static constexpr int SMEM = PG_WARPS * RING + EXTRA;
-  static_assert(STAGE == PG_ROWS * DH * 4, "a warp's output takes one stage of its ring");
+  static_assert(PG_ROWS * DH * 4 <= STAGE, "a warp's output takes the place of one stage of its ring");
 };
 
 template <typename T>
