@@ -60,6 +60,7 @@ struct PagedAttn {
   float* item_ml;                            // [items][PG_ROWS][2]: max and sum of every item, with score
   int* arrived;                              // [ctas]: pieces delivered of the item that is cut first at the end of a CTA's stretch; zero between calls
   float* score; long long score_ld;          // [batch, hq, score_ld] scaled log2-domain scores, or null
+  int* joins;                                // [ctas][8]: the item that is cut first at the end of a CTA's stretch (tensor-memory kernel)
   float* weight_out;                         // [batch, hkv, cap] or null
   int ctas;                                  // stretches the line is cut into at most
   int min_tiles;                             // ... and the least tiles of one
@@ -846,36 +847,63 @@ __global__ void __launch_bounds__(256) paged_empty_kernel(T* out, const int* len
 }
 
 // weight_out = weight + sum over the group's heads of exp2(score - max) / sum, slots 0 .. keys - 1 of every (sequence, head),
-// 512 slots per CTA at a time.
+// 256 slots per CTA at a time; a thread's scores of eight heads are under way together.
 __global__ void __launch_bounds__(256) paged_weights_kernel(const PagedAttn P) {
   pdl_trigger();
-  constexpr int CHUNK = 512;
-  __shared__ PagedLine L;
+  constexpr int CHUNK = 256;
+  __shared__ int pre[PG_MAX_SEQ + 1], s_len[PG_MAX_SEQ];
+  __shared__ float2 ml[128];                 // per head: maximum, 1 / sum
   pdl_wait();
-  paged_line(L, P, CHUNK);                   // here a tile is a chunk of slots
-  const int cap = (int)P.c.cap(), n_chunks = L.pre[PG_MAX_SEQ] * P.c.hkv;
-  int b = 0;
-  for (int w = blockIdx.x; w < n_chunks; w += gridDim.x) {
-    while (w >= L.pre[b + 1] * P.c.hkv) ++b;
-    const int per = L.pre[b + 1] - L.pre[b], in_b = w - L.pre[b] * P.c.hkv, h = in_b / per;
-    const int slot0 = (in_b - h * per) * CHUNK, keys = min(L.len[b] + P.n_new, cap);
-    const size_t at = ((size_t)b * P.c.hkv + h) * (size_t)cap;
-    const float* score = P.score + ((long long)b * P.hq + h * P.group) * P.score_ld;
-    const float* ml = P.item_ml + (size_t)(b * P.c.hkv + h) * P.tiles * PG_ROWS * 2;
+  const int cap = (int)P.c.cap();
+  if (threadIdx.x < 32) {                    // chunks per head, summed over the sequences before
+    const int lane = threadIdx.x;
+    int own[2], sum = 0;
 #pragma unroll
-    for (int u = 0; u < CHUNK / 256; ++u) {
-      const int slot = slot0 + u * 256 + threadIdx.x;
-      if (slot >= keys) continue;
-      const float old = (P.c.weight && slot < L.len[b]) ? P.c.weight[at + slot] : 0.f;
-      float sum = 0.f;
-#pragma unroll 4
-      for (int g = 0; g < P.group; ++g) {
-        const float2 t = __ldg(reinterpret_cast<const float2*>(ml) + g);
-        const float z = __ldg(score + g * P.score_ld + slot);
-        sum = fmaf(exp2f(z - (t.x == -INFINITY ? 0.f : t.x)), t.y == 0.f ? 0.f : 1.f / t.y, sum);
-      }
-      P.weight_out[at + slot] = old + sum;
+    for (int u = 0; u < 2; ++u) {
+      const int b = lane * 2 + u, len = b < P.c.batch ? min(P.c.len[b], cap) : -1;
+      s_len[b] = len;
+      own[u] = len < 0 ? 0 : (min(len + P.n_new, cap) + CHUNK - 1) / CHUNK;
+      sum += own[u];
     }
+    int inc = sum;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int t = __shfl_up_sync(0xffffffffu, inc, o);
+      if (lane >= o) inc += t;
+    }
+    pre[lane * 2] = inc - sum;
+    pre[lane * 2 + 1] = inc - sum + own[0];
+    if (lane == 31) pre[PG_MAX_SEQ] = inc;
+  }
+  __syncthreads();
+  const int n_chunks = pre[PG_MAX_SEQ] * P.c.hkv;
+  for (int w = blockIdx.x; w < n_chunks; w += gridDim.x) {
+    const int b = line_seq(pre, P.c.hkv, w), per = pre[b + 1] - pre[b], in_b = w - pre[b] * P.c.hkv, h = in_b / per;
+    const int slot = (in_b - h * per) * CHUNK + threadIdx.x, keys = min(s_len[b] + P.n_new, cap);
+    const size_t at = ((size_t)b * P.c.hkv + h) * (size_t)cap + slot;
+    const float* score = P.score + ((long long)b * P.hq + h * P.group) * P.score_ld + slot;
+    const bool in = slot < keys;
+    const float old = in && P.c.weight && slot < s_len[b] ? P.c.weight[at] : 0.f;
+    float z[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) z[u] = in && u < P.group ? __ldg(score + u * P.score_ld) : -INFINITY;
+    if (threadIdx.x < P.group) {
+      const float2 t = __ldg(reinterpret_cast<const float2*>(P.item_ml) + (size_t)(b * P.c.hkv + h) * P.tiles * PG_ROWS + threadIdx.x);
+      ml[threadIdx.x] = make_float2(t.x == -INFINITY ? 0.f : t.x, t.y == 0.f ? 0.f : 1.f / t.y);
+    }
+    __syncthreads();
+    float sum = 0.f;
+    for (int g0 = 0; g0 < P.group; g0 += 8) {
+      if (g0 > 0) {
+#pragma unroll
+        for (int u = 0; u < 8; ++u) z[u] = in && g0 + u < P.group ? __ldg(score + (g0 + u) * P.score_ld) : -INFINITY;
+      }
+#pragma unroll
+      for (int u = 0; u < 8; ++u)
+        if (g0 + u < P.group) sum = fmaf(exp2f(z[u] - ml[g0 + u].x), ml[g0 + u].y, sum);
+    }
+    if (in) P.weight_out[at] = old + sum;
+    __syncthreads();
   }
 }
 

@@ -52,22 +52,16 @@ __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* tm,
       : "memory");
 }
 // Joins the pieces of the items that a stretch's end cut, in the order of their positions; an item that several ends cut
-// belongs to the first of them. CTA (end of a stretch, quarter of the columns): a warp per 32 rows, a row per lane.
+// belongs to the first of them, whose CTA has written down what it is. CTA (end of a stretch, quarter of the columns): a warp
+// per 32 rows, a row per lane.
 template <int DH>
-__global__ void __launch_bounds__(256) paged_join_kernel(const PagedAttn P, int tile) {
+__global__ void __launch_bounds__(256) paged_join_kernel(const PagedAttn P) {
   pdl_trigger();
-  __shared__ PagedLine L;
   pdl_wait(KID_ATTN_MERGE);
-  paged_line(L, P, tile);
-  const int c = blockIdx.x + 1;
-  if (L.total == 0 || c >= L.ctas) return;
-  PagedPlace S;
-  const int x = line_begin(L, c);
-  S.at(L, P, x);
-  const int x0 = x - S.t;
-  if (S.t == 0 || line_owner(L, x0) != c - 1) return;
-  const int c1 = line_owner(L, x0 + S.T_b - 1), fp = first_place(L, c - 1, x0);
-  const int r = threadIdx.x, rr = S.mt * PT_ROWS + r;                // row of the item, of the (sequence, head)
+  const int4 j0 = __ldg(reinterpret_cast<const int4*>(P.joins) + blockIdx.x * 2), j1 = __ldg(reinterpret_cast<const int4*>(P.joins) + blockIdx.x * 2 + 1);
+  const int c = blockIdx.x + 1, c1 = j0.x, fp = j0.y, b = j0.z, h = j0.w, mt = j1.x;         // c1: last CTA with a piece, 0: no join
+  if (c1 == 0) return;
+  const int r = threadIdx.x, rr = mt * PT_ROWS + r;                  // row of the item, of the (sequence, head)
   const int R = P.n * P.group;
   if ((rr & ~31) >= R) return;
   float M = -INFINITY, Z = 0.f;
@@ -92,7 +86,7 @@ __global__ void __launch_bounds__(256) paged_join_kernel(const PagedAttn P, int 
   }
   if (rr >= R) return;
   const float inv = Z == 0.f ? 0.f : 1.f / Z;
-  bf16* dst = (bf16*)P.out + (((size_t)S.b * P.n + rr / P.group) * P.hq + S.h * P.group + rr % P.group) * DH + blockIdx.y * (DH / 4);
+  bf16* dst = (bf16*)P.out + (((size_t)b * P.n + rr / P.group) * P.hq + h * P.group + rr % P.group) * DH + blockIdx.y * (DH / 4);
 #pragma unroll
   for (int d = 0; d < N4; d += 2) {
     uint4 y = make_uint4(0u, 0u, 0u, 0u);
@@ -210,6 +204,7 @@ __global__ void __launch_bounds__(PT_THREADS, 1) paged_tree_kernel(const __grid_
   if (!idle) W.begin(L);
 
   if (idle) {
+    if (threadIdx.x == 0) P.joins[blockIdx.x * 8] = 0;
   } else if (warp == 0) {
     // ------------------------------ copies ------------------------------
     const int rows = min(PT_KB, 1 << P.c.shift), sub_n = PT_KB / rows;        // rows of a box, boxes per chunk
@@ -240,6 +235,15 @@ __global__ void __launch_bounds__(PT_THREADS, 1) paged_tree_kernel(const __grid_
           if (mine) tma_load_3d(slot_at(s) + chunk * C::CHUNK + sub * rows * 128, kv ? &PP.tmV : &PP.tmK, x0, y, page, full_bar(s));
         }
       }
+    }
+    if (lane == 0) {                         // the item that the end of this stretch cuts first, for the join
+      PagedPlace S;
+      S.at(L, P, L.x_end - 1);
+      const int x0 = L.x_end - 1 - S.t;
+      int4* j = reinterpret_cast<int4*>(P.joins) + blockIdx.x * 2;
+      const bool cut = x0 >= L.x_begin && x0 + S.T_b > L.x_end;
+      j[0] = make_int4(cut ? line_owner(L, x0 + S.T_b - 1) : 0, x0 > L.x_begin ? 1 : 0, S.b, S.h);
+      j[1] = make_int4(S.mt, 0, 0, 0);
     }
     if (!ok && lane == 0) {                  // given up: the copies under way still land before the CTA ends
       const long long t_end = clock64() + WS_WAIT_CYCLES;
