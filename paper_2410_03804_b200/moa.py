@@ -259,6 +259,7 @@ _raw_stream = torch._C._cuda_getCurrentRawStream
 
 def _serving_call(index: int, stream, call, what: str, *args):
     """Makes a call of the serving operators with its tensors' device current, on the given or that device's current stream."""
+    assert stream is None or stream.device_index == index, "the stream is of another device"
     if torch._C._cuda_getDevice() == index:
         status = call(*args, _raw_stream(index) if stream is None else stream.cuda_stream)
     else:
@@ -266,6 +267,16 @@ def _serving_call(index: int, stream, call, what: str, *args):
             status = call(*args, _raw_stream(index) if stream is None else stream.cuda_stream)
     if status != MOA_OK:
         _check(status, what)
+
+
+def _made(make, stream):
+    """A tensor that a call makes for itself: of the call's stream, so that its memory's earlier uses and its fill come before."""
+    if stream is None:
+        return make()
+    with torch.cuda.stream(stream):
+        t = make()
+    t.record_stream(torch.cuda.current_stream(t.device))       # where a result is read afterwards
+    return t
 
 
 def _is(t: torch.Tensor, dtype, index: int) -> bool:
@@ -335,9 +346,7 @@ class PagedCache:
 
     def _own_scratch(self, ws, make, stream):
         if ws is None:
-            ws = make()
-            if stream is not None:
-                ws.record_stream(stream)
+            ws = _made(make, stream)
         assert _is(ws, torch.uint8, self.index), "ws: cuda uint8, contiguous"
         return ws
 
@@ -375,9 +384,7 @@ def moa_paged_attention(cache: PagedCache, q: torch.Tensor, k_new=None, v_new=No
         assert (_is(mask, torch.int64, at) or _is(mask, torch.uint64, at)) and mask.numel() == b * n, "mask: int64 [batch, n]"
         mp = mask.data_ptr()
     if out is None:
-        out = torch.empty((b, n, hq, dh), dtype=dt, device=cache.device)
-        if stream is not None:
-            out.record_stream(stream)
+        out = _made(lambda: torch.empty((b, n, hq, dh), dtype=dt, device=cache.device), stream)
     else:
         assert _is(out, dt, at) and out.shape == q.shape, "out: [batch, n, hq, head_dim]"
     if weight_out is not None:
@@ -471,22 +478,16 @@ def _rule_rows(rules: LogitRules, logits: torch.Tensor, tok, parent):
     return at, b, n, v, 0 if dt is torch.float32 else 1
 
 
-def _kept(t, stream):
-    if stream is not None:
-        t.record_stream(stream)
-    return t
-
-
 def moa_logit_rules(rules: LogitRules, logits: torch.Tensor, tok=None, parent=None, out=None, choice=None, stream=None):
     """Applies the rules to logits [batch, n, V]; tok, parent int32 [batch, n]: the kept tree whose slots the rows are.
     Returns (adjusted logits, arg-max int32 [batch, n]); out may be the logits themselves."""
     at, b, n, v, dt = _rule_rows(rules, logits, tok, parent)
     if out is None:
-        out = _kept(torch.empty_like(logits), stream)
+        out = _made(lambda: torch.empty_like(logits), stream)
     else:
         assert _is(out, logits.dtype, at) and out.shape == logits.shape, "out: as the logits"
     if choice is None:
-        choice = _kept(torch.empty((b, n), dtype=torch.int32, device=logits.device), stream)
+        choice = _made(lambda: torch.empty((b, n), dtype=torch.int32, device=logits.device), stream)
     else:
         assert _is(choice, torch.int32, at) and choice.shape == (b, n), "choice: int32 [batch, n]"
     _serving_call(at, stream, load_library().moa_logit_rules, "moa_logit_rules", rules._ref, None if tok is None else tok.data_ptr(),
@@ -500,7 +501,7 @@ def moa_verify_greedy_rules(rules: LogitRules, tok: torch.Tensor, parent: torch.
     assert tok is not None, "a verification needs the tree"
     at, b, n, v, dt = _rule_rows(rules, target_logits, tok, parent)
     if out is None:
-        out = tuple(_kept(torch.empty(s, dtype=torch.int32, device=target_logits.device), stream)
+        out = tuple(_made(lambda: torch.empty(s, dtype=torch.int32, device=target_logits.device), stream)
                     for s in ((b, n), (b, cap), (b, cap), (b,), (b,)))
     else:
         for t, s in zip(out, ((b, n), (b, cap), (b, cap), (b,), (b,))):

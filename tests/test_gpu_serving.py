@@ -234,6 +234,28 @@ def test_tree_attention(dtype, dh, hq, hkv, n, unused, page, lens):
             assert torch.equal(c.k[p, r], kn[b, i]) and torch.equal(c.v[p, r], vn[b, i])
 
 
+@pytest.mark.parametrize("dtype,dh,hq,hkv,n,unused,page,lens", [c for c in TREE_CASES if c[0] == "bf16"])
+def test_tree_attention_in_a_large_cache(dtype, dh, hq, hkv, n, unused, page, lens):
+    """The same rows in caches with room for many more positions, which take another kernel from 17 rows on."""
+    moa, rng = _moa(), np.random.default_rng(n * 77 + dh + 1)
+    batch = len(lens)
+    tiles = -(-n * hq // hkv // 8)
+    c = _cache(rng, dtype, lens, hkv, dh, page, n + 2**17 // (batch * hkv * tiles) + page)
+    q, kn, vn = _rows_of(rng, dtype, batch, n, hq, hkv, dh)
+    if unused:
+        kn[:, n - unused:], vn[:, n - unused:] = NAN, float("inf")
+    _, _, mask = _trees(rng, batch, n, unused)
+    out = torch.full((batch, n, hq, dh), 5.0, dtype=T[dtype], device="cuda")
+    before = out.clone()
+    moa.moa_paged_attention(c, q, kn, vn, mask=mask, out=out)
+    torch.cuda.synchronize()
+    _check_attention(c, dtype, q, kn, vn, mask.cpu().numpy(), out, lens, n, before=before)
+    for b, L in enumerate(lens):
+        for i in range(n - unused if L >= 0 else 0):
+            p, r = int(c.page_table[b, (L + i) // page]), (L + i) % page
+            assert torch.equal(c.k[p, r], kn[b, i]) and torch.equal(c.v[p, r], vn[b, i])
+
+
 def test_causal_rows_and_committed_only():
     """Without a mask the rows are causal; new_rows=False leaves the committed slots, and a sequence without any gives zeros."""
     moa, rng = _moa(), np.random.default_rng(3)
@@ -402,6 +424,168 @@ def test_attention_on_another_stream_and_replayed():
     assert c.len.tolist() == [-1, 351]
 
 
+STEEP_CASES = [
+    # dtype, dh, hq, hkv, n, page, len
+    ("bf16", 128, 16, 2, 1, 16, 1500),
+    ("f32", 64, 4, 2, 1, 8, 700),
+    ("bf16", 128, 16, 2, 40, 16, 1700),
+    ("bf16", 64, 32, 1, 52, 128, 1001),
+]
+
+
+@pytest.mark.parametrize("dtype,dh,hq,hkv,n,page,L", STEEP_CASES)
+@pytest.mark.parametrize("shape", ["rising", "falling", "peaks"])
+def test_scores_far_apart(dtype, dh, hq, hkv, n, page, L, shape):
+    """Scores that climb by hundreds over the positions, fall, or stand out at single ones: the running maximum moves often,
+    by more than one factor of 2^8 at a time, or never again."""
+    moa, rng = _moa(), np.random.default_rng(L + n)
+    c = _cache(rng, dtype, [L], hkv, dh, page, n)
+    u = torch.from_numpy(rng.choice([-1.0, 1.0], dh)).to(T[dtype]).cuda()              # the direction that queries share
+    j = torch.arange(L, dtype=torch.float64)
+    a = {"rising": 30 * j / L, "falling": 30 - 30 * j / L, "peaks": torch.where(j % 131 == 77, 25.0 + j / L, 0.0)}[shape]
+    for x in range(0, L, page):
+        p, m = int(c.page_table[0, x // page]), min(page, L - x)
+        c.k[p, :m] += (a[x:x + m, None, None].cuda() * u.double()).to(T[dtype])
+    q, kn, vn = _rows_of(rng, dtype, 1, n, hq, hkv, dh)
+    q += u
+    _, anc, mask = _trees(rng, 1, n, 0)
+    out = moa.moa_paged_attention(c, q, kn, vn, mask=mask)
+    torch.cuda.synchronize()
+    _check_attention(c, dtype, q, kn, vn, mask.cpu().numpy(), out, [L], n)
+
+
+@pytest.mark.parametrize("page,hq,n", [(8, 128, 64), (128, 64, 21), (256, 32, 21), (1024, 16, 21)])
+def test_tree_rows_on_missing_pages_and_at_the_end_of_the_cache(page, hq, n):
+    """Rows of several tokens: pages that the table does not have are left out, new rows behind the last slot are neither
+    stored nor seen, unused slots in a causal batch of uneven lengths."""
+    moa, rng = _moa(), np.random.default_rng(page)
+    hkv, dh = 2, 128
+    lens = [3 * page + 5, 2 * page, 0]
+    c = _cache(rng, "bf16", lens, hkv, dh, page, n)
+    per = c.page_table.shape[1]
+    table = c.page_table.clone()
+    table[0, 1], table[1, 0] = -1, c.k.shape[0]
+    q, _, _ = _rows_of(rng, "bf16", 3, n, hq, hkv, dh)
+    out = moa.moa_paged_attention(moa.PagedCache(c.k, c.v, table, c.len), q, new_rows=False).double().cpu().numpy()
+    for b, gone in ((0, 1), (1, 0)):
+        K, V = _slots(c, b, lens[b])
+        see = np.arange(lens[b]) // page != gone
+        for i in range(0, n, 5):
+            for h in range(hq):
+                ref, _, mass, spread = _attend(q[b, i, h].double().cpu().numpy(), K[:, h // (hq // 2)], V[:, h // (hq // 2)], see, dh ** -0.5)
+                assert np.all(np.abs(out[b, i, h] - ref) <= _bound("bf16", dh, lens[b], spread, mass, ref, once=True))
+    assert np.all(out[2] == 0)
+    c.k[torch.isnan(c.k)] = 0.25
+    c.v[torch.isnan(c.v)] = 0.5
+    full = torch.tensor([per * page, per * page - 2, per * page - n], dtype=torch.int32, device="cuda")
+    c3 = moa.PagedCache(c.k, c.v, c.page_table, full)
+    q, kn, vn = _rows_of(rng, "bf16", 3, n, hq, hkv, dh)
+    k0 = c.k.clone()
+    out = moa.moa_paged_attention(c3, q, kn, vn)
+    torch.cuda.synchronize()
+    _check_attention(c3, "bf16", q, kn, vn, None, out, full.tolist(), n)
+    for b, m in ((1, 2), (2, n)):
+        for i in range(m):
+            s = int(full[b]) + i
+            k0[int(c.page_table[b, s // page]), s % page] = kn[b, i]
+    assert torch.equal(c.k, k0)
+
+
+def test_one_workspace_for_calls_of_every_kind():
+    """One workspace, zeroed once, serves tokens, trees and weights in turn, on one stream, and each call answers as with a
+    workspace of its own."""
+    moa, rng = _moa(), np.random.default_rng(21)
+    lens, hq, hkv, dh = [900, 3, 2100, -1], 32, 4, 128
+    c = _cache(rng, "bf16", lens, hkv, dh, 16, 64, track=True)
+    kinds = [(1, True), (61, False), (1, False), (2, False), (64, False), (1, True)]
+    ws = max((c.workspace(n, hq, w) for n, w in kinds), key=lambda t: t.numel())
+    got, want = [], []
+    for n, w in kinds * 2:
+        q, kn, vn = _rows_of(rng, "bf16", 4, n, hq, hkv, dh)
+        outs = []
+        for space in (ws, c.workspace(n, hq, w)):
+            wo = torch.full_like(c.weight, -7.0) if w else None
+            out = torch.full((4, n, hq, dh), 5.0, dtype=torch.bfloat16, device="cuda")
+            moa.moa_paged_attention(c, q, kn, vn, out=out, weight_out=wo, ws=space)
+            outs.append((out, wo))
+        got.append(outs[0])
+        want.append(outs[1])
+    torch.cuda.synchronize()
+    for (a, wa), (b, wb) in zip(got, want):
+        assert torch.equal(a, b) and (wa is None or torch.equal(wa, wb))
+
+
+def test_two_streams_at_once():
+    """Calls of two streams, each with its own workspace and output, over one cache whose rows are in the pages."""
+    moa, rng = _moa(), np.random.default_rng(31)
+    lens, hq, hkv, dh = [3000, 1, 777], 32, 8, 128
+    c = _cache(rng, "bf16", lens, hkv, dh, 16, 1)
+    q1, _, _ = _rows_of(rng, "bf16", 3, 1, hq, hkv, dh)
+    q2, _, _ = _rows_of(rng, "bf16", 3, 30, hq, hkv, dh)
+    want = [moa.moa_paged_attention(c, q, new_rows=False) for q in (q1, q2)]
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    outs = [[torch.empty_like(w) for _ in range(20)] for w in want]
+    spaces = [c.workspace(1, hq), c.workspace(30, hq)]
+    torch.cuda.synchronize()
+    for i in range(20):
+        for s, q, o, ws in zip(streams, (q1, q2), outs, spaces):
+            moa.moa_paged_attention(c, q, new_rows=False, out=o[i], ws=ws, stream=s)
+    torch.cuda.synchronize()
+    for w, o in zip(want, outs):
+        assert all(torch.equal(w, x) for x in o)
+
+
+def test_scratch_of_a_call_on_another_stream():
+    """Scratch and results that a call on a given stream makes for itself do not wait for, or overtake, the current stream."""
+    moa, rng = _moa(), np.random.default_rng(51)
+    c = _cache(rng, "bf16", [3000, 500], 4, 128, 16, 1)
+    q, _, _ = _rows_of(rng, "bf16", 2, 1, 16, 4, 128)
+    want = moa.moa_paged_attention(c, q, new_rows=False)
+    size = c.workspace(1, 16).numel()
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        dirt = [torch.full((size,), 7, dtype=torch.uint8, device="cuda") for _ in range(3)]
+        del dirt
+    dirt = [torch.full((size,), 7, dtype=torch.uint8, device="cuda") for _ in range(3)]
+    torch.cuda.synchronize()
+    del dirt
+    torch.cuda._sleep(50_000_000)                # the current stream is busy for some 25 ms
+    got = [moa.moa_paged_attention(c, q, new_rows=False, stream=side) for _ in range(3)]
+    side.synchronize()
+    assert all(torch.equal(g, want) for g in got)
+    torch.cuda.synchronize()
+
+
+def test_evict_replayed():
+    """A captured eviction in place follows the length of each replay."""
+    moa, rng = _moa(), np.random.default_rng(41)
+    c = _cache(rng, "bf16", [70, 40], 2, 64, 16, 2, track=True)
+    ws = c.evict_workspace(64)
+    start = [t.clone() for t in (c.k, c.v, c.weight, c.pos)]
+    moa.moa_paged_evict(c, 64, 4, 8, ws=ws)
+    torch.cuda.synchronize()
+    want = [t.clone() for t in (c.k, c.v, c.weight, c.pos)]
+    assert c.len.tolist() == [64, 40]
+    def back():
+        for t, s in zip((c.k, c.v, c.weight, c.pos), start):
+            t.copy_(s)
+        c.len.copy_(torch.tensor([70, 40], dtype=torch.int32))
+    back()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        moa.moa_paged_evict(c, 64, 4, 8, ws=ws)
+    for _ in range(2):
+        back()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert c.len.tolist() == [64, 40]
+        assert all(torch.equal(t.view(torch.uint8), w.view(torch.uint8)) for t, w in zip((c.k, c.v, c.weight, c.pos), want))
+        graph.replay()                           # nothing is left to evict
+        torch.cuda.synchronize()
+        assert all(torch.equal(t.view(torch.uint8), w.view(torch.uint8)) for t, w in zip((c.k, c.v, c.weight, c.pos), want))
+
+
 # ------------------------------------------------------------------------------------------------------------ eviction
 def _evict_reference(w, pos, L, seen, budget, sink, recent):
     """(kept slots, [(source, destination)]) of one head."""
@@ -426,6 +610,9 @@ EVICT_CASES = [
     ("bf16", 128, 1, 16, [5], 1, 0, 0, "odd"),
     ("bf16", 64, 2, 16, [600, 599], 598, 0, 3, "odd"),
     ("f32", 64, 1, 1024, [12289, 12288], 6000, 4, 0, "random"),
+    ("bf16", 64, 8, 16, [1500, 1301, 1300, 1299, 0, -1, 3000, 1302, 2600, 1900], 1300, 4, 64, "random"),      # many heads
+    ("f32", 64, 40, 8, [300, 40, 129], 40, 2, 5, "odd"),
+    ("bf16", 128, 38, 32, [5000], 4999, 0, 0, "ties"),
 ]
 
 
@@ -596,6 +783,33 @@ def test_logit_rules(dtype, batch, n, vocab, tree, n_bias, allow, record):
         plain = moa.moa_verify_greedy(t_dev, p_dev, one_hot.cuda(), 7)
         for a, b in zip(five, plain):
             assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("batch,n,vocab", [(1, 3, 20011), (10, 61, 2003)])
+def test_rules_when_everything_was_said(dtype, batch, n, vocab):
+    """A record that holds every token, more than a CTA lists, with the output off the logits' 16-byte boundaries or alike."""
+    moa, rng = _moa(), np.random.default_rng(vocab)
+    xt = torch.from_numpy((rng.standard_normal((batch, n, vocab)) * 3).astype(np.float32)).to(T[dtype]).cuda()
+    counts = rng.integers(0, 4, (batch, vocab)).astype(np.int32)
+    seen = np.ones((batch, vocab), bool)
+    rep, freq, pres = (rng.random(batch).astype(np.float32) + s for s in (0.8, 0.1, -0.3))
+    may = rng.random((batch, n, vocab)) < 0.7
+    dev = lambda a: torch.from_numpy(np.ascontiguousarray(a)).cuda()  # noqa: E731
+    rules = moa.LogitRules(vocab, dev(counts), dev(_bits(seen)), dev(rep), dev(freq), dev(pres), None, None, dev(_bits(may)))
+    x = xt.float().cpu().numpy()
+    want, want_c = np.empty_like(x), np.empty((batch, n), np.int32)
+    for b in range(batch):
+        for i in range(n):
+            want[b, i], want_c[b, i] = _rules_reference(x[b, i], counts[b], seen[b], rep[b], freq[b], pres[b], None, None, may[b, i], [])
+    wt = torch.from_numpy(want).to(T[dtype]).float().numpy()
+    for shift in (0, 1, 4):
+        flat = torch.full((x.size + 8,), 9.0, dtype=T[dtype], device="cuda")
+        out = flat[shift:shift + x.size].view(batch, n, vocab)
+        got, choice = moa.moa_logit_rules(rules, xt, out=out)
+        assert np.array_equal(got.float().cpu().numpy(), wt)
+        assert np.array_equal(choice.cpu().numpy(), want_c)
+        assert torch.all(flat[:shift] == 9.0) and torch.all(flat[shift + x.size:] == 9.0)
 
 
 def test_no_rules_is_the_plain_arg_max():
