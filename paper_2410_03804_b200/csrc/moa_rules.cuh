@@ -14,11 +14,15 @@
 // record knows a few thousand of 128256 tokens. A CTA (or eight in a cluster) takes a row. It marks the allowed tokens of its
 // slice that any other rule touches (the record's, the path's, the biased ones) in a bitmap in shared memory, lists them, and
 // takes the listed ones side by side over its threads, so that their scattered loads (logit, count) are under way together;
-// path and biases are in a small hash table. The stream then looks at bits only: a masked or listed token counts as -inf,
-// four tokens of a table's byte selectors at a time, and the place of the best of 16 bytes is looked up once, at the end.
-// (976 rows of 128256 bf16 with 300 biases: 111 us, two waves of four CTAs per SM, of which the list costs 10 us each. Listed
-// tokens taken by the stream as it met them: 284 us. A second pass walking the bitmap: 115 us. A CTA walking the rows of a
-// sequence with one list for all, its copies ahead: 131 us, its rows' dependent steps no longer hidden by other CTAs.)
+// path and biases are in a small hash table. The stream then looks at bits only, in shared memory: a masked or listed token
+// counts as -inf, four tokens of a table's byte selectors at a time, and the place of the best of 16 bytes is looked up once,
+// at the end. Pieces are loaded four ahead. When a CTA has a row of its own, a quarter of its warps take the list while the
+// others stream.
+// Measured, 976 rows of 128256 bf16 with 300 biases: 73 us = 3.7 TB/s, of which the bitmap, the table and the list take the
+// first 15 us of a CTA. The allowed bits read again as bytes from global memory beside each piece: 109 us; list first, then
+// the stream by all warps: 82 us; listed tokens taken by the stream as it met them: 284 us; a CTA walking the rows of a
+// sequence with one list for all: 131 us, its rows' dependent steps no longer hidden by other CTAs. CTAs of 128 threads, seven
+// to an SM and all rows at once: 85 us against 73 us of 256 threads.
 #pragma once
 #include "moa_verify.cuh"
 
@@ -26,7 +30,8 @@ namespace moa {
 
 constexpr int RU_MAX_PATH = 256;             // tree slots per sequence
 constexpr int RU_MAX_BIAS = 1024;
-constexpr int RU_LIST = 1536;                // listed tokens of a slice; those behind them are taken one by one
+constexpr int RU_THREADS = 256;               // of a CTA that takes a row alone
+constexpr int RU_LIST = 1280;                // listed tokens of a slice; those behind them are taken one by one
 
 struct RulesArgs {
   const int* counts;                         // [batch, V] or null
@@ -57,9 +62,10 @@ __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(NT) rules_kernel(co
   extern __shared__ __align__(16) uint32_t ru_smem[];
   __shared__ float cv[CL];
   __shared__ int ci[CL];
-  __shared__ int s_path[RU_MAX_PATH], s_tok[RU_MAX_PATH], s_par[RU_MAX_PATH];
-  __shared__ int s_np, s_listed;
-  __shared__ int list[RU_LIST];
+  __shared__ int s_path[RU_MAX_PATH];
+  __shared__ int s_np, s_listed, s_step;
+  __shared__ int list[RU_LIST];                    // before it is filled: tokens and parents of the tree
+  int *s_tok = list, *s_par = list + RU_MAX_PATH;
   __shared__ uint2 picks[256];                     // 16-bit types: byte selectors of four words for every byte of mask bits
   __shared__ uint2 best[2][NT / 32];               // per warp: stream (key, first token of its 16 bytes), touched (key, token)
   const int rank = blockIdx.x, row = blockIdx.y, b = row / A.n, ti = row - b * A.n;
@@ -67,13 +73,12 @@ __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(NT) rules_kernel(co
   const int per_cta = ((A.V + CL - 1) / CL + 31) & ~31;
   const int e0 = min(A.V, rank * per_cta), e1 = min(A.V, e0 + per_cta);
   const int n_words = (e1 - e0 + 31) >> 5;
-  // shared memory: hash table (id, path count, bias entries, lowest of them, bias), then the slice's bitmap
+  // shared memory: hash table (id; path count + 2^16 * bias entries; lowest of them, later the bias), then the slice's bitmap
   int* h_id = reinterpret_cast<int*>(ru_smem);
   int* h_cnt = h_id + A.table;
-  int* h_n = h_cnt + A.table;
-  int* h_first = h_n + A.table;
-  float* h_val = reinterpret_cast<float*>(h_first + A.table);
-  uint32_t* mark = reinterpret_cast<uint32_t*>(h_val + A.table);
+  int* h_first = h_cnt + A.table;
+  float* h_val = reinterpret_cast<float*>(h_first);
+  uint32_t* mark = reinterpret_cast<uint32_t*>(h_first + A.table);
   const unsigned hmask = A.table > 0 ? (unsigned)A.table - 1u : 0u;
   // every CTA of the cluster is running before another writes to its shared memory (waited for at the end)
   if constexpr (CL > 1) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
@@ -85,9 +90,9 @@ __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(NT) rules_kernel(co
   const bool dense = counts && !seen;        // counts without the record's bits: every count is read
   if constexpr (sizeof(T) == 2) {                  // bit 2 q: the low half of word q, bit 2 q + 1: its high half; 0: from the other operand
     auto pick = [](unsigned two) { return 0x7654u - (two & 1u) * 0x0044u - (two >> 1) * 0x4400u; };
-    if (tid < 256) picks[tid] = make_uint2(pick(tid & 3) | pick((tid >> 2) & 3) << 16, pick((tid >> 4) & 3) | pick((tid >> 6) & 3) << 16);
+    for (int i = tid; i < 256; i += NT) picks[i] = make_uint2(pick(i & 3) | pick((i >> 2) & 3) << 16, pick((i >> 4) & 3) | pick((i >> 6) & 3) << 16);
   }
-  if (tid == 0) s_listed = 0;
+  if (tid == 0) s_listed = s_step = 0;
   // ---- bitmap and hash table ----
   const int size = e1 - e0;
   auto in_slice = [&](int id) { return id >= e0 && id < e1; };
@@ -114,7 +119,7 @@ __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(NT) rules_kernel(co
     }
   }
   if (A.table > 0) {
-    for (int i = tid; i < A.table; i += NT) { h_id[i] = -1; h_cnt[i] = 0; h_n[i] = 0; h_first[i] = 0x7fffffff; }
+    for (int i = tid; i < A.table; i += NT) { h_id[i] = -1; h_cnt[i] = 0; h_first[i] = 0x7fffffff; }
     if (A.tok)
       for (int i = tid; i < A.n; i += NT) { s_tok[i] = A.tok[(size_t)b * A.n + i]; s_par[i] = A.parent[(size_t)b * A.n + i]; }
     __syncthreads();
@@ -129,7 +134,7 @@ __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(NT) rules_kernel(co
         }
       s_np = np;
     }
-    auto slot_of = [&](int id) {             // the table has at least twice the slots that can be asked for
+    auto slot_of = [&](int id) {             // the table has at least a third more slots than can be asked for
       unsigned s = ru_hash(id, hmask);
       while (true) {
         const int old = atomicCAS(&h_id[s], -1, id);
@@ -143,7 +148,7 @@ __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(NT) rules_kernel(co
       const int id = __ldg(bid + i);
       if (!in_slice(id) || !may(id - e0)) continue;
       const int s = slot_of(id);
-      atomicAdd(&h_n[s], 1);
+      atomicAdd(&h_cnt[s], 1 << 16);
       atomicMin(&h_first[s], i);
       atomicOr(&mark[(id - e0) >> 5], 1u << ((id - e0) & 31));
     }
@@ -156,10 +161,11 @@ __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(NT) rules_kernel(co
       atomicOr(&mark[(id - e0) >> 5], 1u << ((id - e0) & 31));
     }
     for (int s = tid; s < A.table; s += NT) {          // (the path only adds entries without a bias)
-      if (h_n[s] == 0) continue;
+      const int entries = h_cnt[s] >> 16;
+      if (entries == 0) continue;
       const int i0 = h_first[s], id = h_id[s];
       float v = __ldg(bval + i0);
-      if (h_n[s] > 1)                        // the same id twice: summed in list order, whatever order the threads came in
+      if (entries > 1)                        // the same id twice: summed in list order, whatever order the threads came in
         for (int i = i0 + 1; i < A.n_bias; ++i)
           if (__ldg(bid + i) == id) v = __fadd_rn(v, __ldg(bval + i));
       h_val[s] = v;
@@ -167,7 +173,7 @@ __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(NT) rules_kernel(co
   }
   __syncthreads();
 
-  // ---- the list of the marked tokens, in no order ----
+  // ---- the list of the marked tokens, in no order, and the bits of those that the stream takes: allowed, not marked ----
   const T* xr = (const T*)A.x + (size_t)row * A.V;
   T* orow = A.out ? (T*)A.out + (size_t)row * A.V : nullptr;
   const float rep = A.rep ? A.rep[b] : 1.f, freq = A.freq ? A.freq[b] : 0.f, pres = A.pres ? A.pres[b] : 0.f;
@@ -182,9 +188,10 @@ __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(NT) rules_kernel(co
         const int id = h_id[s];
         if (id == -1) break;
         if (id == e0 + e) {
-          c += h_cnt[s];
-          known = known || h_cnt[s] > 0;
-          biased = h_n[s] > 0;
+          const int on_path = h_cnt[s] & 0xffff;
+          c += on_path;
+          known = known || on_path > 0;
+          biased = (h_cnt[s] >> 16) > 0;
           bias = h_val[s];
           break;
         }
@@ -198,17 +205,27 @@ __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(NT) rules_kernel(co
     best_of(x, e, tv, te);
   };
   auto in_record = [&](int e) { return seen && ((__ldg(seen + (e >> 5)) >> (e & 31)) & 1u); };
-  for (int wi = tid; wi < n_words; wi += NT) {
-    unsigned m = mark[wi];
-    if (m == 0u) continue;
-    int at = atomicAdd(&s_listed, __popc(m));
-    for (; m != 0u; m &= m - 1u, ++at) {
-      const int e = wi * 32 + __ffs(m) - 1;
-      if (at < RU_LIST) {
-        list[at] = e;
-      } else {                                     // (rare) no room
-        const bool known = in_record(e);
-        touch(e, to_f(xr[e0 + e]), known, counts && (known || dense) ? __ldg(counts + e0 + e) : 0);
+  uint32_t* pass = A.out ? mark + ((per_cta + 31) >> 5) + 1 : mark;      // without an output nobody asks for the marks again
+  for (int w0 = tid; w0 < n_words; w0 += 4 * NT) {
+    unsigned a[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) a[u] = allow ? __ldg(allow + min(w0 + u * NT, n_words - 1)) : ~0u;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int wi = w0 + u * NT;
+      if (wi >= n_words) break;
+      unsigned m = mark[wi];
+      pass[wi] = a[u] & ~m;
+      if (m == 0u) continue;
+      int at = atomicAdd(&s_listed, __popc(m));
+      for (; m != 0u; m &= m - 1u, ++at) {
+        const int e = wi * 32 + __ffs(m) - 1;
+        if (at < RU_LIST) {
+          list[at] = e;
+        } else {                                   // (rare) no room
+          const bool known = in_record(e);
+          touch(e, to_f(xr[e0 + e]), known, counts && (known || dense) ? __ldg(counts + e0 + e) : 0);
+        }
       }
     }
   }
@@ -218,115 +235,113 @@ __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(NT) rules_kernel(co
   constexpr int PER = 16 / sizeof(T), UN = 4;
   constexpr unsigned ALL = (1u << PER) - 1u;
   const uint8_t* mark8 = reinterpret_cast<const uint8_t*>(mark);
-  const uint8_t* allow8 = reinterpret_cast<const uint8_t*>(allow);
+  const uint8_t* pass8 = reinterpret_cast<const uint8_t*>(pass);
   // the row's 16-byte pieces start `head` tokens into the slice; with an output that does not lie alike, there are none
   const T* xs = xr + e0;
   T* os = orow ? orow + e0 : nullptr;
   const int head = os && (((uintptr_t)xs ^ (uintptr_t)os) & 15u) ? size : min(size, (int)((16u - (unsigned)((uintptr_t)xs & 15u)) % 16u / sizeof(T)));
   const int nvec = (size - head) / PER, tail = head + nvec * PER;
-  uint4 raw[UN];
-  unsigned al[UN];
-  auto load = [&](int c0) {
-#pragma unroll
-    for (int u = 0; u < UN; ++u) {
-      const int c = c0 + u * NT, e = head + c * PER;
-      if (c >= nvec) continue;
-      raw[u] = __ldcs(reinterpret_cast<const uint4*>(xs + head) + c);
-      if (allow8) {
-        al[u] = __ldg(allow8 + (e >> 3));
-        if ((e & 7) > 8 - PER) al[u] |= (unsigned)__ldg(allow8 + (e >> 3) + 1) << 8;
-      }
-    }
+  uint4 raw[UN];                                   // pieces under way: one that was taken is replaced at once
+  auto load = [&](int c, uint4& x) {
+    if (c < nvec) x = __ldcs(reinterpret_cast<const uint4*>(xs + head) + c);
   };
-  load(tid);
-  const int n_list = min(s_listed, RU_LIST);
-  for (int k0 = tid; k0 < n_list; k0 += 4 * NT) {
-    int e[4], c[4];
-    float x[4];
-    bool known[4];
+  auto bits_of = [&](const uint8_t* bits, int e) -> unsigned {
+    unsigned v = bits[e >> 3];
+    if ((e & 7) > 8 - PER) v |= (unsigned)bits[(e >> 3) + 1] << 8;
+    return v >> (e & 7) & ALL;
+  };
+  // A row's CTA: a quarter of the warps take the listed tokens while the others stream, and who gets to it takes the next
+  // UN * 32 pieces. A slice of eight has a few listed tokens per warp: all warps take them, their first pieces under way.
+  constexpr bool SPLIT = CL == 1;
+  constexpr int LT = SPLIT ? NT / 4 : NT;
+  const int lane = tid & 31, wid = tid >> 5;
+  int c0 = wid * UN * 32 + lane;
+  auto next_step = [&](int c) {
+    if (!SPLIT) return c + UN * NT;
+    int step = 0;
+    if (lane == 0) step = atomicAdd(&s_step, UN * 32);
+    return __shfl_sync(0xffffffffu, step, 0) + lane;
+  };
+  auto first_step = [&]() {
+    if (SPLIT) c0 = next_step(0);
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      e[u] = k0 + u * NT < n_list ? list[k0 + u * NT] : -1;
-      if (e[u] < 0) continue;
-      x[u] = to_f(xs[e[u]]);
-      known[u] = in_record(e[u]);
-      c[u] = counts ? __ldg(counts + e0 + e[u]) : 0;         // without its bit it does not count
+    for (int u = 0; u < UN; ++u) load(c0 + u * 32, raw[u]);
+  };
+  if (!SPLIT || tid >= LT) first_step();
+  if (tid < LT) {
+    const int n_list = min(s_listed, RU_LIST);
+    for (int k0 = tid; k0 < n_list; k0 += 4 * LT) {
+      int e[4], c[4];
+      float x[4];
+      bool known[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        e[u] = k0 + u * LT < n_list ? list[k0 + u * LT] : -1;
+        if (e[u] < 0) continue;
+        x[u] = to_f(xs[e[u]]);
+        known[u] = in_record(e[u]);
+        c[u] = counts ? __ldg(counts + e0 + e[u]) : 0;         // without its bit it does not count
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+        if (e[u] >= 0) touch(e[u], x[u], known[u], known[u] || dense ? c[u] : 0);
     }
-#pragma unroll
-    for (int u = 0; u < 4; ++u)
-      if (e[u] >= 0) touch(e[u], x[u], known[u], known[u] || dense ? c[u] : 0);
-  }
-  // the few tokens before and behind the pieces
-  for (int k = tid; k < head + size - tail; k += NT) {
-    const int e = k < head ? k : tail + k - head;
-    if ((mark8[e >> 3] >> (e & 7)) & 1u) continue;
-    const float x = may(e) ? to_f(xs[e]) : -INFINITY;
-    if (os) os[e] = from_f<T>(x);
-    best_of(x, e, tv, te);
+    // the few tokens before and behind the pieces
+    for (int k = tid; k < head + size - tail; k += LT) {
+      const int e = k < head ? k : tail + k - head;
+      if (os && ((mark8[e >> 3] >> (e & 7)) & 1u)) continue;
+      const float x = (pass8[e >> 3] >> (e & 7)) & 1u ? to_f(xs[e]) : -INFINITY;
+      if (os) os[e] = from_f<T>(x);
+      best_of(x, e, tv, te);
+    }
+    if (SPLIT) first_step();
   }
   float bv = -INFINITY;                            // best of the stream
   int be = 0x7fffffff;                             // the first token of the 16 bytes it is in
-  for (int c0 = tid; c0 - tid < nvec; c0 += UN * NT) {
-    if (c0 != tid) load(c0);
-    uint4 w[UN];
-    unsigned mk[UN], ok[UN];
-#pragma unroll
-    for (int u = 0; u < UN; ++u) {                 // a piece that does not exist has no allowed token
-      const int c = c0 + u * NT, e = min(head + c * PER, size - 1);
-      unsigned v = mark8[e >> 3];
-      if ((e & 7) > 8 - PER) v |= (unsigned)mark8[(e >> 3) + 1] << 8;
-      mk[u] = v >> (e & 7) & ALL;
-      ok[u] = allow8 ? al[u] >> (e & 7) & ALL : ALL;
-      if (c >= nvec) ok[u] = mk[u] = 0u;
-      const unsigned in = ok[u] & ~mk[u];
-      if constexpr (sizeof(T) == 4) {
-        w[u] = make_uint4(in & 1u ? raw[u].x : 0xff800000u, in & 2u ? raw[u].y : 0xff800000u, in & 4u ? raw[u].z : 0xff800000u,
-                          in & 8u ? raw[u].w : 0xff800000u);
-      } else {
-        const uint2 p = picks[in];
-        w[u] = make_uint4(__byte_perm(raw[u].x, 0xff80ff80u, p.x), __byte_perm(raw[u].y, 0xff80ff80u, p.x >> 16),
-                          __byte_perm(raw[u].z, 0xff80ff80u, p.y), __byte_perm(raw[u].w, 0xff80ff80u, p.y >> 16));
-      }
-    }
+  while (c0 - lane < nvec) {
+    const int c1 = next_step(c0);
 #pragma unroll
     for (int u = 0; u < UN; ++u) {
+      const int c = c0 + u * 32, e = head + c * PER;
+      if (c >= nvec) break;
+      const unsigned in = bits_of(pass8, e);
+      uint4 w;
       float vm;
       if constexpr (sizeof(T) == 4) {
-        vm = fmaxf(fmaxf(__uint_as_float(w[u].x), __uint_as_float(w[u].y)), fmaxf(__uint_as_float(w[u].z), __uint_as_float(w[u].w)));
+        w = make_uint4(in & 1u ? raw[u].x : 0xff800000u, in & 2u ? raw[u].y : 0xff800000u, in & 4u ? raw[u].z : 0xff800000u, in & 8u ? raw[u].w : 0xff800000u);
+        vm = fmaxf(fmaxf(__uint_as_float(w.x), __uint_as_float(w.y)), fmaxf(__uint_as_float(w.z), __uint_as_float(w.w)));
       } else {
+        const uint2 p = picks[in];
+        w = make_uint4(__byte_perm(raw[u].x, 0xff80ff80u, p.x), __byte_perm(raw[u].y, 0xff80ff80u, p.x >> 16),
+                       __byte_perm(raw[u].z, 0xff80ff80u, p.y), __byte_perm(raw[u].w, 0xff80ff80u, p.y >> 16));
         auto two = [](uint32_t v) { return *reinterpret_cast<__nv_bfloat162*>(&v); };
-        const __nv_bfloat162 m = __hmax2(__hmax2(two(w[u].x), two(w[u].y)), __hmax2(two(w[u].z), two(w[u].w)));       // NaN only of NaNs
+        const __nv_bfloat162 m = __hmax2(__hmax2(two(w.x), two(w.y)), __hmax2(two(w.z), two(w.w)));       // NaN only of NaNs
         const uint32_t mw = *reinterpret_cast<const uint32_t*>(&m);
         vm = fmaxf(__uint_as_float(mw << 16), __uint_as_float(mw & 0xffff0000u));
       }
-      be = vm > bv ? head + (c0 + u * NT) * PER : be;        // rising tokens: the first of equals stays
+      load(c1 + u * 32, raw[u]);
+      be = vm > bv ? e : be;                       // rising tokens: the first of equals stays
       bv = fmaxf(bv, vm);
-    }
-    if (os) {
-#pragma unroll
-      for (int u = 0; u < UN; ++u) {
-        const int c = c0 + u * NT, e = head + c * PER;
-        if (c >= nvec) continue;
-        const unsigned skip = mk[u];               // written above
+      if (os) {
+        const unsigned skip = bits_of(mark8, e);   // marked: written by the list's threads
         if (skip == 0u) {
-          __stcs(reinterpret_cast<uint4*>(os + e), w[u]);
+          __stcs(reinterpret_cast<uint4*>(os + e), w);
         } else {
 #pragma unroll
           for (int q = 0; q < PER; ++q)
             if (!((skip >> q) & 1u)) {
-              const uint32_t v = sizeof(T) == 4 ? (q == 0 ? w[u].x : q == 1 ? w[u].y : q == 2 ? w[u].z : w[u].w)
-                                                : (q < 2 ? w[u].x : q < 4 ? w[u].y : q < 6 ? w[u].z : w[u].w);
+              const uint32_t v = sizeof(T) == 4 ? (q == 0 ? w.x : q == 1 ? w.y : q == 2 ? w.z : w.w) : (q < 2 ? w.x : q < 4 ? w.y : q < 6 ? w.z : w.w);
               if constexpr (sizeof(T) == 4) os[e + q] = __uint_as_float(v);
               else os[e + q] = __ushort_as_bfloat16((unsigned short)(v >> (16 * (q & 1))));
             }
         }
       }
     }
+    c0 = c1;
   }
 
   if constexpr (CL > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
   if (!A.choice) return;                           // the same for the whole grid
-  const int lane = tid & 31, wid = tid >> 5;
 #pragma unroll
   for (int kind = 0; kind < 2; ++kind) {
     const unsigned key = ru_key(kind ? tv : bv);
@@ -345,7 +360,7 @@ __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(NT) rules_kernel(co
     }
     if (key[0] != 0u) {                            // which of the 16 bytes' tokens it was: a lane each
       const int e = (int)at[0] + lane;
-      const bool in = lane < PER && !((mark8[e >> 3] >> (e & 7)) & 1u) && (!allow8 || ((__ldg(allow8 + (e >> 3)) >> (e & 7)) & 1u));
+      const bool in = lane < PER && ((pass8[e >> 3] >> (e & 7)) & 1u);
       const unsigned hit = __ballot_sync(0xffffffffu, in && ru_key(to_f(xs[in ? e : 0])) == key[0]);
       at[0] += __ffs(hit) - 1;
     }
