@@ -316,7 +316,7 @@ moa_status moa_paged_append(const moa_paged_cache *cache, const void *k_new, con
  *   q           T [batch, n, hq, head_dim], rows q_stride elements apart; head h belongs to key / value head h / (hq / hkv)
  *   k_new,v_new T [batch, n, hkv, head_dim], rows new_stride elements apart: appended by this call as moa_paged_append
  *               would (slots that no row sees are not written), or NULL when the rows are in the pages already
- *   scale       0 means 1 / sqrt(head_dim)
+ *   scale       0 means 1 / sqrt(head_dim); at most 2e38
  *   out         T [batch, n, hq, head_dim]
  *   weight_out  device float [batch, hkv, max_pages * page_size], may be cache->weight, or NULL; n = 1 only: for every slot
  *               that the row sees, cache->weight (0 for the new slot, or without it) + the sum over the group's query heads

@@ -715,6 +715,7 @@ RULE_CASES = [
     ("f32", 2, 300, 640, False, 3, True, "both"),
     ("f32", 64, 61, 32, True, 4, True, "both"),
     ("bf16", 1, 1, 300001, False, 7, True, "both"),
+    ("bf16", 1, 1, 518400, False, 1024, False, "both"),
 ]
 
 

@@ -57,7 +57,7 @@ ATT = dict(q=P, q_stride=4096, k_new=P, v_new=P, new_stride=1024, n=1, n_new=1, 
     (dict(q=None), NULL), (dict(out=None), NULL), (dict(ws=None), NULL), (dict(k_new=None), NULL), (dict(v_new=None), NULL),
     (dict(n=0, n_new=0), SHAPE), (dict(n=65, n_new=65), SHAPE), (dict(n=2, n_new=1), SHAPE), (dict(n_new=0), SHAPE), (dict(hq=12), SHAPE),
     (dict(hq=0), SHAPE), (dict(hq=8 * 129, q_stride=1 << 20), SHAPE), (dict(q_stride=4088), SHAPE), (dict(new_stride=1016), SHAPE),
-    (dict(n=2, n_new=2, weight_out=P), SHAPE), (dict(scale=-1.0), SHAPE), (dict(scale=float("nan")), SHAPE), (dict(scale=float("inf")), SHAPE),
+    (dict(n=2, n_new=2, weight_out=P), SHAPE), (dict(scale=-1.0), SHAPE), (dict(scale=float("nan")), SHAPE), (dict(scale=float("inf")), SHAPE), (dict(scale=2.5e38), SHAPE),
     (dict(q_stride=4100), ALIGN), (dict(new_stride=1028), ALIGN), (dict(q=P + 8), ALIGN), (dict(out=P + 8), ALIGN), (dict(ws=P + 4), ALIGN),
     (dict(k_new=P + 2), ALIGN)])
 def test_attention_refuses(change, status):
