@@ -231,7 +231,10 @@ __global__ void __launch_bounds__(PT_THREADS, 1) paged_tree_kernel(const __grid_
           const uint32_t s = cnt % PT_SLOTS;
           ok = mbar_wait(empty_bar(s), ((cnt / PT_SLOTS) & 1u) ^ 1u, abort_flag);
           ok = __all_sync(0xffffffffu, ok);
-          if (cnt == 2) {                    // the first queries before the ring fills: together they are what the start waits for
+          // The first queries before the ring fills: together they are what the start waits for. Only inside the first
+          // segment, which cannot end before this block comes: behind it the queries of the next one may have completed
+          // the barrier's second phase, and the wait for the first would miss it.
+          if (cnt == 2 && t == 1) {
             ok = mbar_wait(q_bar(0), 0u, abort_flag);
             ok = __all_sync(0xffffffffu, ok);
           }
