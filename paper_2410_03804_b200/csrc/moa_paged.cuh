@@ -605,13 +605,14 @@ __global__ void __launch_bounds__(PG_THREADS, 1) paged_rows_kernel(const PagedAt
     if (lane < C::KW && key < f_keys) {
       if (key >= f_len && !((f_any >> (key - f_len)) & 1ull)) {
         src = 0;
-      } else if (key >= f_len && P.k_new) {
-        src = 2;
-        off = ((long long)F.b * P.n + (key - f_len)) * P.new_stride + (long long)F.h * DH;
       } else {
         off = P.c.row(F.b, key, DH);
         src = off >= 0 ? 1 : 0;
         off += (long long)F.h * DH;
+        if (src != 0 && key >= f_len && P.k_new) {                   // a new row whose page the table does not have is left out, too
+          src = 2;
+          off = ((long long)F.b * P.n + (key - f_len)) * P.new_stride + (long long)F.h * DH;
+        }
       }
     }
     if (++F.t == F.T_b && f_x + 1 < x_end) {

@@ -23,3 +23,47 @@ def test_tree_items_of_one_block(dh, hkv, hq, n):
     _check_attention(c, "bf16", q, kn, vn, mask.cpu().numpy(), out, lens, n)
     for _ in range(50):
         assert torch.equal(moa.moa_paged_attention(c, q, mask=mask), out)
+
+
+@pytest.mark.parametrize("dtype,hq,n,extra", [("bf16", 8, 1, 0), ("f32", 4, 1, 0), ("bf16", 2, 5, 0), ("f32", 8, 19, 0),
+                                              ("bf16", 16, 19, 0), ("bf16", 16, 19, 5000)])
+def test_new_rows_on_missing_pages(dtype, hq, n, extra):
+    """New rows whose page the table does not have are left out, whichever kernel a cache's size leads to, and whether the
+    call appends them or they were appended before; their slots get no weight."""
+    moa, rng = _moa(), np.random.default_rng(n + extra + hq)
+    hkv, dh, page = 2, 64, 8
+    lens = [40, 37, 64, 16]                      # the rows begin with a page, inside one, ...
+    c = _cache(rng, dtype, lens, hkv, dh, page, n + extra, track=True)
+    table = c.page_table.clone()
+    gone = [(0, 5), (1, 4), (2, 9 if n > 8 else 8), (3, 2)]
+    for b, p in gone:
+        table[b, p] = -1 if b % 2 else c.k.shape[0] + b
+    c2 = moa.PagedCache(c.k, c.v, table, c.len, c.weight, c.pos, c.seen)
+    q, kn, vn = _rows_of(rng, dtype, 4, n, hq, hkv, dh)
+    _, _, mask = _trees(rng, 4, n, 0)
+    w_in = c.weight.clone()
+    wo = torch.full_like(c.weight, -7.0) if n == 1 else None
+    k0 = c.k.clone()
+    out = moa.moa_paged_attention(c2, q, kn, vn, mask=mask, weight_out=wo)
+    torch.cuda.synchronize()
+    words = mask.cpu().numpy()
+    for b, L in enumerate(lens):
+        K, V = _slots(c, b, L)
+        K, V = np.concatenate([K, kn[b].double().cpu().numpy()]), np.concatenate([V, vn[b].double().cpu().numpy()])
+        there = np.arange(L + n) // page != gone[b][1]
+        for i in range(n):
+            see = there.copy()
+            see[L:] &= [bool((int(words[b, i]) >> j) & 1) for j in range(n)]
+            for h in range(hq):
+                g = h // (hq // hkv)
+                ref, w, mass, spread = _attend(q[b, i, h].double().cpu().numpy(), K[:, g], V[:, g], see, dh ** -0.5)
+                assert np.all(np.abs(out[b, i, h].double().cpu().numpy() - ref) <= _bound(dtype, dh, L + n, spread, mass, ref, once=n > 1)), (b, i, h)
+        for i in range(n):
+            if there[L + i]:
+                k0[int(table[b, (L + i) // page]), (L + i) % page] = kn[b, i]
+        if wo is not None:                       # the group's weights are shared out among the slots that are there
+            got = (wo[b, :, :L].double() - w_in[b, :, :L].double()).cpu().numpy()[:, there[:L]].sum(-1)
+            got = got + (wo[b, :, L].double().cpu().numpy() if there[L] else 0.0)
+            assert np.allclose(got, hq // hkv, rtol=1e-4)
+    assert torch.equal(c.k.view(torch.uint8), k0.view(torch.uint8))
+    assert torch.equal(moa.moa_paged_attention(c2, q, mask=mask), out)
