@@ -3,6 +3,9 @@
 //
 //   s_j = scale * q . k_j,  p_j = exp(s_j - max s) / sum exp(s - max s),  out = sum_j p_j v_j
 //
+// Scores, and the running maxima that are taken of them, are kept as the products leave them; only differences from a maximum
+// are scaled: exp(scale * (s - max)). So a large scale takes no score out of fp32, and the largest one always gives 1.
+//
 // What bounds it: one token reads every cached byte once for 4 * group multiply-adds per 4 bytes (bf16), so the cache
 // stream from HBM does. The layout follows from that: the queries that share a key / value head -- (rows of the sequence)
 // x (heads of the group) -- are stacked 8 to a tile, so a cached row is read once per 8 of them.
@@ -59,7 +62,7 @@ struct PagedAttn {
   float *part_o, *part_ml;                   // [2 * ctas][rows of an item][dh], the same [2]: pieces
   float* item_ml;                            // [items][PG_ROWS][2]: max and sum of every item, with score
   int* arrived;                              // [ctas]: pieces delivered of the item that is cut first at the end of a CTA's stretch; zero between calls
-  float* score; long long score_ld;          // [batch, hq, score_ld] scaled log2-domain scores, or null
+  float* score; long long score_ld;          // [batch, hq, score_ld] unscaled scores, or null
   int* joins;                                // [ctas][8]: the item that is cut first at the end of a CTA's stretch (tensor-memory kernel)
   float* weight_out;                         // [batch, hkv, cap] or null
   int ctas;                                  // stretches the line is cut into at most
@@ -240,7 +243,7 @@ __device__ __forceinline__ unsigned long long row_word(const PagedAttn& P, int b
   return P.mask ? __ldg(P.mask + (size_t)b * P.n + i) : causal_word(i);
 }
 
-// PagedWarp: one warp's running state over a query tile (maxima in the log2 domain, sums, outputs, all in fp32), merged over the
+// PagedWarp: one warp's running state over a query tile (maxima of the unscaled scores, sums, outputs, all in fp32), merged over the
 // CTA's warps at the end of an item.
 
 // ---------------------------------------------------------------------------------------------
@@ -321,7 +324,7 @@ struct PagedWarp<bf16, DH> {
     }
     float z[2][2];                           // [position gq, gq + 8][query 2 tq, 2 tq + 1]
 #pragma unroll
-    for (int e = 0; e < 4; ++e) z[e >> 1][e & 1] = (s[0][e] + s[1][e]) * P.scale_log2;
+    for (int e = 0; e < 4; ++e) z[e >> 1][e & 1] = s[0][e] + s[1][e];
     if (!plain) {
 #pragma unroll
       for (int e = 0; e < 4; ++e)
@@ -342,7 +345,7 @@ struct PagedWarp<bf16, DH> {
       mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
       mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
       const float mn = fmaxf(m[u], mx);
-      f[u] = (mn == m[u]) ? 1.f : ex2_approx(m[u] - mn);          // m = -inf: 0
+      f[u] = (mn == m[u]) ? 1.f : ex2_approx((m[u] - mn) * P.scale_log2);          // m = -inf: 0
       m[u] = mn;
     }
     if (__any_sync(0xffffffffu, f[0] != 1.f || f[1] != 1.f)) {
@@ -355,7 +358,7 @@ struct PagedWarp<bf16, DH> {
     uint32_t hi[2], lo[2];                   // right operand: positions 0..7 and 8..15 x queries
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
-      const float p0 = ex2_approx(z[k][0] - sub0), p1 = ex2_approx(z[k][1] - sub1);
+      const float p0 = ex2_approx((z[k][0] - sub0) * P.scale_log2), p1 = ex2_approx((z[k][1] - sub1) * P.scale_log2);
       l[0] += p0;
       l[1] += p1;
       const uint32_t w = pack_bf16(p0, p1);
@@ -470,7 +473,7 @@ struct PagedWarp<float, DH> {
       float t = acc[r];
       t += __shfl_xor_sync(0xffffffffu, t, 8);
       t += __shfl_xor_sync(0xffffffffu, t, 16);
-      if (quarter == (r & 3)) sp[kk * PG_ROWS + r] = (plain || see(row_word(P, b, (mt * PG_ROWS + r) / P.group), kk)) ? t * P.scale_log2 : -INFINITY;
+      if (quarter == (r & 3)) sp[kk * PG_ROWS + r] = (plain || see(row_word(P, b, (mt * PG_ROWS + r) / P.group), kk)) ? t : -INFINITY;
     }
     __syncwarp();
     // softmax statistics: lane r holds row r % PG_ROWS
@@ -487,14 +490,14 @@ struct PagedWarp<float, DH> {
         for (int k = 0; k < KW; k += 4) *reinterpret_cast<float4*>(score + r * P.score_ld + k) = make_float4(z[k], z[k + 1], z[k + 2], z[k + 3]);
       }
       const float mn = fmaxf(mrow, mx);
-      const float f = mn == mrow ? 1.f : exp2f(mrow - mn);
+      const float f = mn == mrow ? 1.f : exp2f((mrow - mn) * P.scale_log2);
       mrow = mn;
       const float sub = mn == -INFINITY ? 0.f : mn;
       lrow *= f;
       __syncwarp();
 #pragma unroll
       for (int k = 0; k < KW; ++k) {
-        const float p = exp2f(z[k] - sub);
+        const float p = exp2f((z[k] - sub) * P.scale_log2);
         lrow += p;
         if (lane < PG_ROWS) sp[k * PG_ROWS + r] = p;
       }
@@ -734,7 +737,7 @@ __global__ void __launch_bounds__(PG_THREADS, 1) paged_rows_kernel(const PagedAt
       float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
       for (int w = 0; w < PG_WARPS; ++w) {
-        const float f = exp2f(sml[w][r][0] - ref);
+        const float f = exp2f((sml[w][r][0] - ref) * P.scale_log2);
         Z = fmaf(f, sml[w][r][1], Z);
         const float4 y = *reinterpret_cast<const float4*>(pg_smem + w * C::RING + st * C::STAGE + pg_at<DH>(r, c * 4) * 4);
         a.x = fmaf(f, y.x, a.x); a.y = fmaf(f, y.y, a.y); a.z = fmaf(f, y.z, a.z); a.w = fmaf(f, y.w, a.w);
@@ -780,7 +783,7 @@ __global__ void __launch_bounds__(PG_THREADS, 1) paged_rows_kernel(const PagedAt
       float M = -INFINITY, Z = 0.f;
       float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
       auto add = [&](float m, float z, const float4& o, float ref) {
-        const float f = exp2f(m - ref);
+        const float f = exp2f((m - ref) * P.scale_log2);
         Z = fmaf(f, z, Z);
         a.x = fmaf(f, o.x, a.x); a.y = fmaf(f, o.y, a.y); a.z = fmaf(f, o.z, a.z); a.w = fmaf(f, o.w, a.w);
       };
@@ -798,7 +801,7 @@ __global__ void __launch_bounds__(PG_THREADS, 1) paged_rows_kernel(const PagedAt
           float mx = M;
 #pragma unroll
           for (int u = 0; u < 8; ++u) mx = fmaxf(mx, ml[u].x);
-          const float ref = mx == -INFINITY ? 0.f : mx, g = exp2f(M - ref);
+          const float ref = mx == -INFINITY ? 0.f : mx, g = exp2f((M - ref) * P.scale_log2);
           Z *= g;
           a.x *= g; a.y *= g; a.z *= g; a.w *= g;
 #pragma unroll
@@ -814,7 +817,7 @@ __global__ void __launch_bounds__(PG_THREADS, 1) paged_rows_kernel(const PagedAt
         if (work && sub == 0) {
           float mx = M;
           for (int q = 1; q < subs; ++q) mx = fmaxf(mx, sub_o[(q * units + unit) * 6]);
-          const float ref = mx == -INFINITY ? 0.f : mx, g = exp2f(M - ref);
+          const float ref = mx == -INFINITY ? 0.f : mx, g = exp2f((M - ref) * P.scale_log2);
           Z *= g;
           a.x *= g; a.y *= g; a.z *= g; a.w *= g;
           for (int q = 1; q < subs; ++q) {
@@ -847,7 +850,7 @@ __global__ void __launch_bounds__(256) paged_empty_kernel(T* out, const int* len
   for (int d = threadIdx.x; d < per_seq; d += 256) out[(size_t)b * per_seq + d] = from_f<T>(0.f);
 }
 
-// weight_out = weight + sum over the group's heads of exp2(score - max) / sum, slots 0 .. keys - 1 of every (sequence, head),
+// weight_out = weight + sum over the group's heads of exp(scale * (score - max)) / sum, slots 0 .. keys - 1 of every (sequence, head),
 // 256 slots per CTA at a time; a thread's scores of eight heads are under way together.
 __global__ void __launch_bounds__(256) paged_weights_kernel(const PagedAttn P) {
   pdl_trigger();
@@ -901,7 +904,7 @@ __global__ void __launch_bounds__(256) paged_weights_kernel(const PagedAttn P) {
       }
 #pragma unroll
       for (int u = 0; u < 8; ++u)
-        if (g0 + u < P.group) sum = fmaf(exp2f(z[u] - ml[g0 + u].x), ml[g0 + u].y, sum);
+        if (g0 + u < P.group) sum = fmaf(exp2f((z[u] - ml[g0 + u].x) * P.scale_log2), ml[g0 + u].y, sum);
     }
     if (in) P.weight_out[at] = old + sum;
     __syncthreads();

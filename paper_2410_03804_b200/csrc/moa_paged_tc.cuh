@@ -82,7 +82,7 @@ __global__ void __launch_bounds__(256) paged_join_kernel(const PagedAttn P) {
   for (int i = c - 1; i <= c1; ++i) {
     const size_t piece = piece_of(i, c - 1, fp);
     const float2 ml = __ldg(reinterpret_cast<const float2*>(P.part_ml) + piece * PT_ROWS + r);
-    const float f = exp2f(ml.x - ref);
+    const float f = exp2f((ml.x - ref) * P.scale_log2);
     Z = fmaf(f, ml.y, Z);
 #pragma unroll
     for (int d = 0; d < N4; ++d) {
@@ -426,12 +426,11 @@ __global__ void __launch_bounds__(PT_THREADS, 1) paged_tree_kernel(const __grid_
           m4[1] = max3_nan(m4[1], s[62], s[63]);
           m_blk = max3_nan(max3_nan(m4[0], m4[1], m4[2]), m4[3], m4[3]);
         }
-        m_blk *= P.scale_log2;
         float f = 1.f;
         if (m_ref == -INFINITY) {
           m_ref = m_blk;                     // nothing has been added for this row yet
-        } else if (m_blk > m_ref + TC_RESCALE_LOG2) {
-          f = ex2_approx(m_ref - m_blk);
+        } else if ((m_blk - m_ref) * P.scale_log2 > TC_RESCALE_LOG2) {
+          f = ex2_approx((m_ref - m_blk) * P.scale_log2);
           m_ref = m_blk;
           l_run *= f;
         }
@@ -450,11 +449,21 @@ __global__ void __launch_bounds__(PT_THREADS, 1) paged_tree_kernel(const __grid_
           }
         }
         const float sub = m_ref == -INFINITY ? 0.f : m_ref;
-        const uint64_t scale2 = f2_pack(P.scale_log2, P.scale_log2), sub2 = f2_pack(-sub, -sub);
+        // scale * (score - reference) as one multiply-add, score * scale - (scale * reference). The latter is a rounded product,
+        // half a unit of its last place off: the row's common factor, below 2^0.5 while it is below 2^24. From there on (or
+        // where it leaves fp32) the difference is taken first.
+        const float scaled = __fmul_rn(sub, P.scale_log2);
+        const bool steep = __any_sync(0xffffffffu, fabsf(scaled) >= 16777216.f);
+        const float minus = steep ? 0.f : -scaled;
+        const uint64_t scale2 = f2_pack(P.scale_log2, P.scale_log2), sub2 = f2_pack(minus, minus);
         uint64_t l2[2] = {0ull, 0ull};
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
           if (half) load_half(1);
+          if (steep) {
+#pragma unroll
+            for (int e = 0; e < 64; ++e) s[e] -= sub;
+          }
 #pragma unroll
           for (int e = 0; e < 64; e += 16) {
             uint32_t w8[8];

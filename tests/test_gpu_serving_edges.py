@@ -67,3 +67,40 @@ def test_new_rows_on_missing_pages(dtype, hq, n, extra):
             assert np.allclose(got, hq // hkv, rtol=1e-4)
     assert torch.equal(c.k.view(torch.uint8), k0.view(torch.uint8))
     assert torch.equal(moa.moa_paged_attention(c2, q, mask=mask), out)
+
+
+@pytest.mark.parametrize("dtype,n,extra", [("bf16", 1, 0), ("f32", 1, 0), ("bf16", 3, 0), ("f32", 9, 0), ("bf16", 40, 5000)])
+@pytest.mark.parametrize("scale", [3e5, 1e8, 7e11, 1e30, 1e36, 2e38])
+@pytest.mark.parametrize("below", [False, True])
+def test_scores_far_from_zero(dtype, n, extra, scale, below):
+    """Scores are whole numbers, exact in fp32, and the scale sets them so far apart that a row's largest share the weight
+    evenly: out = the mean of their values. Off by: p = 1 and their count are exact; the sum of m products and the division
+    round in fp32 (m + 1 times 2^-23 of the mean of |v| with room for the order), the result once to its type."""
+    moa, rng = _moa(), np.random.default_rng(n)
+    L, hq, hkv, dh = 333, 16, 2, 128
+    c = _cache(rng, dtype, [L], hkv, dh, 16, n + extra, track=n == 1)
+    q, kn, vn = _rows_of(rng, dtype, 1, n, hq, hkv, dh)
+    g = torch.Generator().manual_seed(n)
+    whole = lambda shape: torch.randint(-2, 0 if below else 3, shape, generator=g).to(T[dtype]).cuda()  # noqa: E731
+    q.copy_(whole(q.shape).abs() if below else whole(q.shape))
+    kn.copy_(whole(kn.shape))
+    c.k.copy_(whole(c.k.shape))
+    _, anc, mask = _trees(rng, 1, n, 0)
+    wo = torch.zeros_like(c.weight) if n == 1 else None
+    if n == 1:
+        c.weight.zero_()
+    out = moa.moa_paged_attention(c, q, kn, vn, mask=mask, scale=scale, weight_out=wo)
+    K, V = _slots(c, 0, L + n)
+    acc = np.zeros((hkv, L + n))
+    for i in range(n):
+        see = np.concatenate([np.ones(L, bool), anc[0, i]])
+        for h in range(hq):
+            s = np.where(see, K[:, h // 8] @ q[0, i, h].double().cpu().numpy(), -np.inf)
+            top = s == s.max()
+            acc[h // 8] += top / top.sum()
+            v, m = V[top, h // 8], top.sum()
+            ref, mass = v.mean(0), np.abs(v).mean(0)
+            tol = (2.0**-8 if dtype == "bf16" else 2.0**-24) * np.abs(ref) + (m + 1) * 2.0**-23 * mass
+            assert np.all(np.abs(out[0, i, h].double().cpu().numpy() - ref) <= tol), (i, h)
+    if n == 1:
+        assert np.all(np.abs(wo[0, :, :L + 1].double().cpu().numpy() - acc) <= 9 * 2.0**-23 * acc)
