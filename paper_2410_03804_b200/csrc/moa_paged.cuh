@@ -243,6 +243,17 @@ __device__ __forceinline__ unsigned long long row_word(const PagedAttn& P, int b
   return P.mask ? __ldg(P.mask + (size_t)b * P.n + i) : causal_word(i);
 }
 
+// A value that is not finite belongs to the rows that see its slot, and zero times it is not zero. A slot of a tree is seen by
+// some rows only: there such values are added to those rows' sums by themselves, and zeros take their place in the products.
+__device__ __forceinline__ bool odd_f(float v) { return !(fabsf(v) < INFINITY); }
+__device__ __forceinline__ bool odd_lo(uint32_t w) { return (w & 0x7f80u) == 0x7f80u; }              // of two bf16 values, the lower one
+__device__ __forceinline__ bool odd_hi(uint32_t w) { return (w & 0x7f800000u) == 0x7f800000u; }
+__device__ __forceinline__ bool odd_any(const uint4& x) {
+  return odd_lo(x.x) || odd_hi(x.x) || odd_lo(x.y) || odd_hi(x.y) || odd_lo(x.z) || odd_hi(x.z) || odd_lo(x.w) || odd_hi(x.w);
+}
+__device__ __forceinline__ uint32_t odd_cleared(uint32_t w) { return w & (odd_lo(w) ? 0xffff0000u : ~0u) & (odd_hi(w) ? 0xffffu : ~0u); }
+__device__ __forceinline__ uint4 odd_cleared(const uint4& x) { return make_uint4(odd_cleared(x.x), odd_cleared(x.y), odd_cleared(x.z), odd_cleared(x.w)); }
+
 // PagedWarp: one warp's running state over a query tile (maxima of the unscaled scores, sums, outputs, all in fp32), merged over the
 // CTA's warps at the end of an item.
 
@@ -310,7 +321,7 @@ struct PagedWarp<bf16, DH> {
   // One step: 16 positions, keys at K, values at V. see(w, j): whether a row with mask word w sees position j of the step;
   // plain: every row sees every position. score: the tile's first row of scores, or null.
   template <typename See>
-  __device__ __forceinline__ void step(const PagedAttn& P, const uint8_t* K, const uint8_t* V, bool plain, See see, float* score, int, int mt, int R) {
+  __device__ __forceinline__ void step(const PagedAttn& P, const uint8_t* K, uint8_t* V, bool plain, See see, float* score, int, int mt, int R) {
     const int lane = threadIdx.x & 31;
     const uint32_t sK = smem_u32(K), sV = smem_u32(V);
     float s[2][4];                           // two chains halve the products' latency
@@ -353,6 +364,28 @@ struct PagedWarp<bf16, DH> {
       for (int i = 0; i < DH / 16; ++i) { o[i][0] *= f[0]; o[i][1] *= f[1]; o[i][2] *= f[0]; o[i][3] *= f[1]; }
       l[0] *= f[0];
       l[1] *= f[1];
+    }
+    if (!plain && P.n > 1) {
+      constexpr int N = KW * DH * 2 / 512;   // 16-byte pieces of the values per lane
+      bool odd = false;
+#pragma unroll
+      for (int u = 0; u < N; ++u) odd = odd || odd_any(reinterpret_cast<const uint4*>(V)[u * 32 + lane]);
+      if (__any_sync(0xffffffffu, odd)) {    // (rare)
+#pragma unroll 1
+        for (int j = 0; j < KW; ++j) {
+          const bool s0 = see(word[0], j), s1 = see(word[1], j);
+#pragma unroll
+          for (int e = 0; e < DH / 8; ++e) {
+            const float v = __bfloat162float(*reinterpret_cast<const bf16*>(V + tile_off<DH>(j, e) + gq * 2));
+            if (odd_f(v) && s0) o[e >> 1][2 * (e & 1)] += v;
+            if (odd_f(v) && s1) o[e >> 1][2 * (e & 1) + 1] += v;
+          }
+        }
+        __syncwarp();
+#pragma unroll
+        for (int u = 0; u < N; ++u) reinterpret_cast<uint4*>(V)[u * 32 + lane] = odd_cleared(reinterpret_cast<const uint4*>(V)[u * 32 + lane]);
+        __syncwarp();
+      }
     }
     const float sub0 = m[0] == -INFINITY ? 0.f : m[0], sub1 = m[1] == -INFINITY ? 0.f : m[1];       // seen nothing: exp2(-inf - 0) = 0
     uint32_t hi[2], lo[2];                   // right operand: positions 0..7 and 8..15 x queries
@@ -448,7 +481,7 @@ struct PagedWarp<float, DH> {
   }
 
   template <typename See>
-  __device__ __forceinline__ void step(const PagedAttn& P, const uint8_t* K, const uint8_t* V, bool plain, See see, float* score, int b, int mt, int) {
+  __device__ __forceinline__ void step(const PagedAttn& P, const uint8_t* K, uint8_t* V, bool plain, See see, float* score, int b, int mt, int) {
     const int lane = threadIdx.x & 31;
     const int kk = lane & 7, quarter = lane >> 3;
     float acc[PG_ROWS];
@@ -522,6 +555,16 @@ struct PagedWarp<float, DH> {
       } else {
         const float2 t = *reinterpret_cast<const float2*>(V + off(k, lane >> 1) + (lane & 1) * 8);
         v[0] = t.x; v[1] = t.y;
+      }
+      if (!plain && P.n > 1) {
+#pragma unroll
+        for (int d = 0; d < DL; ++d)
+          if (odd_f(v[d])) {                 // (rare)
+#pragma unroll
+            for (int r = 0; r < PG_ROWS; ++r)
+              if (r < rows && see(row_word(P, b, (mt * PG_ROWS + r) / P.group), k)) o[r][d] += v[d];
+            v[d] = 0.f;
+          }
       }
 #pragma unroll
       for (int r = 0; r < PG_ROWS; r += 4) {
@@ -687,8 +730,6 @@ __global__ void __launch_bounds__(PG_THREADS, 1) paged_rows_kernel(const PagedAt
           const int key = base + j;
           return key < len ? w != 0ull : ((w >> (key - len)) & 1ull) != 0ull;
         };
-        float* at = P.score ? P.score + ((long long)b * P.hq + h * P.group + mt * PG_ROWS) * P.score_ld + base : nullptr;
-        W.step(P, sK, sV, plain, sees, at, b, mt, R);
         // the item's first query tile writes the new rows it holds to their pages
         if (P.k_new && mt == 0 && base + C::KW > len) {
           for (int r = r_first; r < C::KW; r += R_STEP) {
@@ -701,6 +742,8 @@ __global__ void __launch_bounds__(PG_THREADS, 1) paged_rows_kernel(const PagedAt
             *reinterpret_cast<uint4*>((T*)P.c.v + o + (long long)h * DH + ch * C::E) = *reinterpret_cast<const uint4*>(sV + d);
           }
         }
+        float* at = P.score ? P.score + ((long long)b * P.hq + h * P.group + mt * PG_ROWS) * P.score_ld + base : nullptr;
+        W.step(P, sK, sV, plain, sees, at, b, mt, R);
       } else if (P.score && base < keys) {                           // nothing there: the weights' pass reads -inf
         for (int i = lane; i < C::KW * min(PG_ROWS, R - mt * PG_ROWS); i += 32)
           P.score[((long long)b * P.hq + h * P.group + mt * PG_ROWS + i / C::KW) * P.score_ld + base + i % C::KW] = -INFINITY;

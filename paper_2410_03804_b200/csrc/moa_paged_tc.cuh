@@ -180,6 +180,7 @@ __global__ void __launch_bounds__(PT_THREADS, 1) paged_tree_kernel(const __grid_
   auto p_bar = [&](int i) { return bar0 + 8u * (2 * PT_SLOTS + 6 + i); };
   uint32_t* tmem_slot = (uint32_t*)(bp + oBar + 8 * (2 * PT_SLOTS + 8));
   volatile int* abort_flag = (volatile int*)(tmem_slot + 1);
+  volatile int* odd_flag = abort_flag + 1;   // a new slot's value that is not finite was met
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int R = P.n * P.group;
   pdl_trigger();
@@ -191,7 +192,7 @@ __global__ void __launch_bounds__(PT_THREADS, 1) paged_tree_kernel(const __grid_
       mbar_init(s_bar(i), 1);
       mbar_init(p_bar(i), 128);
     }
-    *abort_flag = 0;
+    *abort_flag = *odd_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
@@ -385,16 +386,27 @@ __global__ void __launch_bounds__(PT_THREADS, 1) paged_tree_kernel(const __grid_
             if (at < 64) { vis[0] &= ~(bits << at); live[0] &= ~(bits << at); }
             if (at >= 64 || P.c.shift > 6) { vis[1] &= ~(bits << (at & 63)); live[1] &= ~(bits << (at & 63)); }
           }
-          // zero times what lies in a slot that does not exist may not be zero: such values are cleared, by the tile's 128
-          // threads a row each, once they have landed (the other tile clears the same rows itself)
-          if (~(live[0] & live[1]) != 0ull) {
+          // Zero times what lies in a slot that does not exist may not be zero: such values are cleared, by the tile's 128
+          // threads a row each, once they have landed. So are the values of new slots that are not finite; the rows that
+          // see them get them at the segment's end. (The other tile clears the same bytes itself.)
+          if (k0 + PT_KB > len || ~(live[0] & live[1]) != 0ull) {
             const uint32_t v = 2 * g + 1, vs = v % PT_SLOTS;
             dead = __any_sync(0xffffffffu, !mbar_wait(full_bar(vs), (v / PT_SLOTS) & 1u, abort_flag));
             if (dead) continue;
-            if (!(((row < 64 ? live[0] : live[1]) >> (row & 63)) & 1ull)) {
+            const bool there = (((row < 64 ? live[0] : live[1]) >> (row & 63)) & 1ull) != 0ull;
+            if (!there || k0 + row >= len) {
               uint8_t* d = bp + oRing + vs * C::SLOT + row * 128;
 #pragma unroll
-              for (int p = 0; p < DH / 8; ++p) *reinterpret_cast<uint4*>(d + (p >> 3) * C::CHUNK + ((p & 7) << 4)) = make_uint4(0u, 0u, 0u, 0u);
+              for (int p = 0; p < DH / 8; ++p) {
+                uint4* at = reinterpret_cast<uint4*>(d + (p >> 3) * C::CHUNK + (((p ^ row) & 7) << 4));
+                if (!there) {
+                  *at = make_uint4(0u, 0u, 0u, 0u);
+                } else if (odd_any(*at)) {
+                  *odd_flag = 1;
+                  __threadfence_block();     // who finds the bytes cleared finds the flag
+                  *at = odd_cleared(*at);
+                }
+              }
             }
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
           }
@@ -494,6 +506,8 @@ __global__ void __launch_bounds__(PT_THREADS, 1) paged_tree_kernel(const __grid_
       const float inv = dead ? __int_as_float(0x7fffffff) : l_run == 0.f ? 0.f : 1.f / l_run;
       const size_t piece_at = (size_t)blockIdx.x * 2 + (W.x0 > W.x_begin ? 1 : 0), prow = piece_at * PT_ROWS + i * 128 + row;
       const bool none = l_run == 0.f && !dead;                       // the row sees nothing
+      __threadfence_block();
+      const bool odd = *odd_flag != 0;
 #pragma unroll 1
       for (int d = 0; d < DH; d += 16) {
         float o[16];
@@ -502,6 +516,20 @@ __global__ void __launch_bounds__(PT_THREADS, 1) paged_tree_kernel(const __grid_
         } else {
 #pragma unroll
           for (int e = 0; e < 16; ++e) o[e] = 0.f;
+        }
+        if (odd) {                           // (rare) values of new slots that are not finite, for the rows that see them
+          for (int j = 0; j < P.n_new; ++j) {
+            const long long key = (long long)len + j, block = key / PT_KB - W.t0;
+            if (!((word >> j) & 1ull) || key >= keys || block < 0 || block >= W.nb) continue;
+            const long long at = P.c.row(W.b, key, DH);
+            if (at < 0) continue;
+            const bf16* v = (const bf16*)P.c.v + at + (long long)W.h * DH + d;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+              const float x = __bfloat162float(v[e]);
+              if (odd_f(x)) o[e] += x;
+            }
+          }
         }
         if (W.whole) {                       // staged over this thread's own query row, whose last scores have been formed
           uint32_t w8[8];

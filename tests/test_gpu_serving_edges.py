@@ -104,3 +104,42 @@ def test_scores_far_from_zero(dtype, n, extra, scale, below):
             assert np.all(np.abs(out[0, i, h].double().cpu().numpy() - ref) <= tol), (i, h)
     if n == 1:
         assert np.all(np.abs(wo[0, :, :L + 1].double().cpu().numpy() - acc) <= 9 * 2.0**-23 * acc)
+
+
+@pytest.mark.parametrize("dtype,dh,hq,hkv,n,extra,lens", [("bf16", 128, 2, 2, 5, 0, [30, 0]), ("bf16", 64, 6, 2, 16, 0, [121]), ("f32", 128, 8, 2, 9, 0, [70]),
+                                                          ("f32", 64, 3, 3, 33, 0, [15, 250]), ("bf16", 128, 64, 8, 61, 600, [100, 0, 700]),
+                                                          ("bf16", 64, 8, 2, 40, 5000, [333, 1])])
+@pytest.mark.parametrize("there", [False, True])
+def test_values_that_are_not_finite(dtype, dh, hq, hkv, n, extra, lens, there):
+    """Infinities and NaN among the keys and values of a tree's slots reach the rows that see those slots, in the columns they
+    stand in, and no other row."""
+    moa, rng = _moa(), np.random.default_rng(n + dh)
+    B = len(lens)
+    c = _cache(rng, dtype, lens, hkv, dh, 16, n + extra)
+    q, kn, vn = _rows_of(rng, dtype, B, n, hq, hkv, dh)
+    parent, anc, mask = _trees(rng, B, n, 0)
+    for b in range(B):                           # leaves and inner slots, but not the root
+        i, j, k, m = rng.permutation(np.arange(1, n))[:4]
+        vn[b, i, :, 3] = float("inf")
+        vn[b, j, 0] = -float("inf")
+        vn[b, k, :, dh - 9:] = NAN
+        kn[b, m, hkv - 1, 5] = NAN
+    if there:
+        moa.moa_paged_append(c, kn, vn)
+    out = moa.moa_paged_attention(c, q, *(() if there else (kn, vn)), mask=mask).double().cpu().numpy()
+    for b, L in enumerate(lens):
+        K, V = _slots(c, b, L + n)
+        assert np.array_equal(V[L:], vn[b].double().cpu().numpy(), equal_nan=True) and np.array_equal(K[L:], kn[b].double().cpu().numpy(), equal_nan=True)
+        for i in range(n):
+            see = np.concatenate([np.ones(L, bool), anc[b, i]])
+            for h in range(hq):
+                g = h // (hq // hkv)
+                seen = np.where(see[:, None], V[:, g], 0.0)
+                qi = q[b, i, h].double().cpu().numpy()
+                ref, _, _, _ = _attend(qi, K[:, g], seen, see, dh ** -0.5)
+                sure = np.isfinite(ref)
+                if sure.any():
+                    fin, _, mass, spread = _attend(qi, K[:, g], np.where(np.isfinite(seen), seen, 0.0), see, dh ** -0.5)
+                    tol = _bound(dtype, dh, L + n, spread, mass, fin, once=True)
+                    assert np.all(np.abs(out[b, i, h] - fin)[sure] <= tol[sure]), (b, i, h)
+                assert np.array_equal(out[b, i, h][~sure], ref[~sure], equal_nan=True), (b, i, h, out[b, i, h][~sure], ref[~sure])
