@@ -43,9 +43,10 @@ struct PagedView {
   const int* seen;                           // [batch] next position, null when pos is
   int batch, max_pages, n_pages, shift, hkv; // page_size = 1 << shift
   __device__ __forceinline__ long long cap() const { return (long long)max_pages << shift; }
+  __device__ __forceinline__ int page_of(int b, long long slot) const { return __ldg(table + (size_t)b * max_pages + (size_t)(slot >> shift)); }
   // element offset of (slot, head 0) of sequence b, or -1 where the table has no such page
   __device__ __forceinline__ long long row(int b, long long slot, int dh) const {
-    const int page = __ldg(table + (size_t)b * max_pages + (size_t)(slot >> shift));
+    const int page = page_of(b, slot);
     if (page < 0 || page >= n_pages) return -1;
     return page * page_stride + (slot & ((1 << shift) - 1)) * (long long)hkv * dh;
   }
@@ -893,8 +894,8 @@ __global__ void __launch_bounds__(256) paged_empty_kernel(T* out, const int* len
   for (int d = threadIdx.x; d < per_seq; d += 256) out[(size_t)b * per_seq + d] = from_f<T>(0.f);
 }
 
-// weight_out = weight + sum over the group's heads of exp(scale * (score - max)) / sum, slots 0 .. keys - 1 of every (sequence, head),
-// 256 slots per CTA at a time; a thread's scores of eight heads are under way together.
+// weight_out = weight + sum over the group's heads of exp(scale * (score - max)) / sum, for those of slots 0 .. keys - 1 of every
+// (sequence, head) that the row sees, 256 slots per CTA at a time; a thread's scores of eight heads are under way together.
 __global__ void __launch_bounds__(256) paged_weights_kernel(const PagedAttn P) {
   pdl_trigger();
   constexpr int CHUNK = 256;
@@ -930,6 +931,8 @@ __global__ void __launch_bounds__(256) paged_weights_kernel(const PagedAttn P) {
     const size_t at = ((size_t)b * P.c.hkv + h) * (size_t)cap + slot;
     const float* score = P.score + ((long long)b * P.hq + h * P.group) * P.score_ld + slot;
     const bool in = slot < keys;
+    const int page = in ? P.c.page_of(b, slot) : -1;
+    const unsigned long long word = row_word(P, b, 0);               // one row; bit 0: its own slot
     const float old = in && P.c.weight && slot < s_len[b] ? P.c.weight[at] : 0.f;
     float z[8];
 #pragma unroll
@@ -949,7 +952,7 @@ __global__ void __launch_bounds__(256) paged_weights_kernel(const PagedAttn P) {
       for (int u = 0; u < 8; ++u)
         if (g0 + u < P.group) sum = fmaf(exp2f((z[u] - ml[g0 + u].x) * P.scale_log2), ml[g0 + u].y, sum);
     }
-    if (in) P.weight_out[at] = old + sum;
+    if (page >= 0 && page < P.c.n_pages && (slot < s_len[b] ? word != 0ull : (word & 1ull) != 0ull)) P.weight_out[at] = old + sum;
     __syncthreads();
   }
 }

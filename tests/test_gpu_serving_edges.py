@@ -143,3 +143,46 @@ def test_values_that_are_not_finite(dtype, dh, hq, hkv, n, extra, lens, there):
                     tol = _bound(dtype, dh, L + n, spread, mass, fin, once=True)
                     assert np.all(np.abs(out[b, i, h] - fin)[sure] <= tol[sure]), (b, i, h)
                 assert np.array_equal(out[b, i, h][~sure], ref[~sure], equal_nan=True), (b, i, h, out[b, i, h][~sure], ref[~sure])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("own", [False, True])
+@pytest.mark.parametrize("track", [False, True])
+def test_weights_of_slots_that_the_row_does_not_see(dtype, own, track):
+    """weight_out has entries for the slots that the row sees: not for pages that the table does not have, a row whose mask
+    word is 0, or a row that does not see its own slot."""
+    moa, rng = _moa(), np.random.default_rng(17)
+    hq, hkv, dh, page = 6, 2, 64, 16
+    lens, words = [90, 300, 40, 32, 33, -1, 0, 0], [1, 1, 0, 2, 1, 1, 2, 0]
+    c = _cache(rng, dtype, lens, hkv, dh, page, 1, track=True)
+    table = c.page_table.clone()
+    gone = {0: 1, 1: 18, 4: 2}                   # inside, the new slot's and the last cached ones', the new slot's page
+    for b, p in gone.items():
+        table[b, p] = -5 if b else c.k.shape[0]
+    w_in = c.weight.clone()
+    c2 = moa.PagedCache(c.k, c.v, table, c.len, c.weight, *((c.pos, c.seen) if track else ()))
+    q, kn, vn = _rows_of(rng, dtype, len(lens), 1, hq, hkv, dh)
+    wo = c.weight if own else torch.full_like(c.weight, -7.0)
+    mask = torch.tensor(words, dtype=torch.int64).reshape(-1, 1).cuda()
+    moa.moa_paged_attention(c2, q, kn, vn, mask=mask, weight_out=wo)
+    got = wo.double().cpu().numpy()
+    for b, L in enumerate(lens):
+        want = (w_in if own else torch.full_like(wo, -7.0))[b].double().cpu().numpy()
+        rel = np.zeros_like(want)
+        if L >= 0:
+            if own and track:
+                want[:, L] = 0.0                 # the new slot's weight, as moa_paged_append sets it
+            K, V = _slots(c, b, L)
+            K, V = np.concatenate([K, kn[b].double().cpu().numpy()]), np.concatenate([V, vn[b].double().cpu().numpy()])
+            see = np.arange(L + 1) // page != gone.get(b, -1)
+            see[:L] &= words[b] != 0
+            see[L] &= words[b] & 1 != 0
+            old = w_in[b].double().cpu().numpy()[:, :L + 1].copy()
+            old[:, L] = 0.0
+            acc = np.zeros_like(old)
+            for h in range(hq):
+                acc[h // 3] += _attend(q[b, 0, h].double().cpu().numpy(), K[:, h // 3], V[:, h // 3], see, dh ** -0.5)[1]
+            want[:, :L + 1][:, see] = (old + acc)[:, see]
+            # as in the weights' other tests: the errors of p, then the group's sum and the addition in fp32
+            rel[:, :L + 1][:, see] = ((2 * (dh + 1) * 2.0**-23 * 60 + 2.0**-20 + 3 * (L + 1) * 2.0**-24 + 4 * 2.0**-24) * acc + 2.0**-23 * (old + acc))[:, see]
+        assert np.all(np.abs(got[b] - want) <= rel), (b, np.argwhere(np.abs(got[b] - want) > rel)[:4])
