@@ -340,10 +340,12 @@ moa_status moa_paged_commit(const moa_paged_cache *cache, int32_t n, const int32
 /* Eviction by accumulated attention weight. Of a sequence with len[b] > budget every key / value head keeps budget slots of
  * its own: those of positions < sink and >= seen[b] - recent, and of the others the ones with the largest weight (a NaN
  * after all numbers, equal weights by the lower slot). The kept slots behind the budget move to the freed slots before it,
- * both in rising order; slots from the budget on are free afterwards. Needs cache->weight, pos and seen; sink + recent <=
- * budget.
+ * both in rising order; slots from the budget on are free afterwards. Slots on a page that the table does not have hold no
+ * row: behind the budget they are given up before all others; before it they stay as they are and count towards it. Needs
+ * cache->weight, pos and seen; sink + recent <= budget.
  *   weight_out, pos_out  shaped as cache->weight and pos and may be them: entries of the slots in use afterwards
- *   len_out     device int32 [batch], may be cache->len, or NULL: min(len, budget)
+ *   len_out     device int32 [batch], may be cache->len, or NULL: min(len, budget), so the negative length of a sequence that is
+ *               not in use
  *   ws          device scratch of moa_paged_evict_workspace_bytes bytes */
 moa_status moa_paged_evict_workspace_bytes(const moa_paged_cache *cache, int32_t budget, size_t *bytes);
 moa_status moa_paged_evict(const moa_paged_cache *cache, int32_t budget, int32_t sink, int32_t recent, float *weight_out, int32_t *pos_out,

@@ -2,7 +2,8 @@
 //
 // Per (sequence, head) with L slots in use and a budget m < L, the m slots to keep are: the first positions (pos < sink), the
 // latest ones (pos >= seen - recent), and of the others those with the largest weight, a NaN after every number, equal weights
-// by the lower slot. Keys carry their rotation, so the order of the slots is free: the kept slots behind the budget move into
+// by the lower slot. A slot on a page that the table does not have holds no row: behind the budget it is given up before all
+// others, before the budget it stays where it is and counts, since no row can move there. Keys carry their rotation, so the order of the slots is free: the kept slots behind the budget move into
 // the freed slots before it, both in rising order -- at most min(m, L - m) rows move, and no row is both read and written.
 //
 // What bounds it: the rows that move (4 * dh elements of traffic each), and for small caches the latency of the launch and of
@@ -35,10 +36,13 @@ struct EvictArgs {
   int* len_out;                              // or null; not len itself
 };
 
-// Rises with the weight; NaN lowest, -0 as +0, protected positions above everything.
-__device__ __forceinline__ uint32_t evict_key(float w, int pos, int sink, int edge) {
+// Rises with the weight; NaN below all numbers, -0 as +0, protected positions above everything. Slots without a page: above
+// everything before the budget, lowest of all behind it. So none is a source of a move -- as many slots as the budget have
+// higher keys, or all that have a page lie before it -- and none a destination.
+__device__ __forceinline__ uint32_t evict_key(float w, int pos, int sink, int edge, bool page, bool low) {
+  if (!page) return low ? 0xffffffffu : 0u;
   if (pos < sink || pos >= edge) return 0xffffffffu;
-  if (w != w) return 0u;
+  if (w != w) return 1u;
   const uint32_t u = __float_as_uint(w + 0.f);
   return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
 }
@@ -87,10 +91,10 @@ __device__ __forceinline__ void evict_rows(const EvictArgs& A, int bh, int f0, i
     const int n = min(WINDOW, f1 - w0);
     for (int i = tid; i < n; i += NT) {
       const int s = __ldcg(src + w0 + i), d = __ldcg(dst + w0 + i);
-      longlong2 o = make_longlong2(A.c.row(b, s, DH), A.c.row(b, d, DH));
+      longlong2 o = make_longlong2(A.c.row(b, s, DH), A.c.row(b, d, DH));      // both are there: see evict_key
       A.weight_out[base + d] = A.c.weight[base + s];
       A.pos_out[base + d] = A.c.pos[base + s];
-      o.x = o.y < 0 || o.x < 0 ? -1 : o.x + (long long)h * DH;       // a page that the table does not have
+      o.x = o.y < 0 || o.x < 0 ? -1 : o.x + (long long)h * DH;
       o.y += (long long)h * DH;
       at[i] = o;
     }
@@ -140,7 +144,9 @@ __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(EV_THREADS) evict_k
   const bool cut = L > m;
   const int edge = cut ? (int)max(-2147483648ll, (long long)A.c.seen[b] - A.recent) : 0;
   const bool held = L <= EV_KEYS;
-  auto key_of = [&](int i) { return held ? ev_keys[i] : evict_key(wt[i], ps[i], A.sink, edge); };
+  const int* table = A.c.table + (size_t)b * A.c.max_pages;
+  auto has_page = [&](int i) { return (unsigned)table[i >> A.c.shift] < (unsigned)A.c.n_pages; };
+  auto key_of = [&](int i) { return held ? ev_keys[i] : evict_key(wt[i], ps[i], A.sink, edge, has_page(i), i < m); };
   uint32_t bound = 0u;                       // keys above it are kept, of those equal to it the first `need`
   int shift = 24, need = m, n_equal = 0;
   if (cut) {
@@ -148,15 +154,17 @@ __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(EV_THREADS) evict_k
       for (int i = tid; i < L; i += 4 * EV_THREADS) {
         float w[4];
         int p[4];
+        bool page[4];
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
           const int j = min(i + u * EV_THREADS, L - 1);
           w[u] = wt[j];
           p[u] = ps[j];
+          page[u] = has_page(j);
         }
 #pragma unroll
         for (int u = 0; u < 4; ++u)
-          if (i + u * EV_THREADS < L) ev_keys[i + u * EV_THREADS] = evict_key(w[u], p[u], A.sink, edge);
+          if (i + u * EV_THREADS < L) ev_keys[i + u * EV_THREADS] = evict_key(w[u], p[u], A.sink, edge, page[u], i + u * EV_THREADS < m);
       }
     }
     for (int i = tid; i < 4 * 256; i += EV_THREADS) (&hist[0][0])[i] = 0;

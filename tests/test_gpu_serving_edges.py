@@ -186,3 +186,59 @@ def test_weights_of_slots_that_the_row_does_not_see(dtype, own, track):
             # as in the weights' other tests: the errors of p, then the group's sum and the addition in fp32
             rel[:, :L + 1][:, see] = ((2 * (dh + 1) * 2.0**-23 * 60 + 2.0**-20 + 3 * (L + 1) * 2.0**-24 + 4 * 2.0**-24) * acc + 2.0**-23 * (old + acc))[:, see]
         assert np.all(np.abs(got[b] - want) <= rel), (b, np.argwhere(np.abs(got[b] - want) > rel)[:4])
+
+
+@pytest.mark.parametrize("dtype,dh,hkv,page,lens,budget,sink,recent", [
+    ("bf16", 64, 2, 16, [300, 100, 65, 640], 64, 4, 20),
+    ("f32", 128, 20, 8, [300, 99, 41, 640], 40, 2, 5),                    # many heads
+    ("bf16", 64, 1, 32, [13000, 20000, 12288, 700], 6400, 4, 100),        # more slots than keys in shared memory
+])
+@pytest.mark.parametrize("apart", [False, True])
+@pytest.mark.parametrize("gone", ["low", "high", "both", "most"])
+def test_evict_with_missing_pages(dtype, dh, hkv, page, lens, budget, sink, recent, apart, gone):
+    """Slots on pages that the table does not have: before the budget they stay and count, behind it they go first. Every row
+    that moves takes its weight and position along, and none moves from or to such a page."""
+    moa, rng = _moa(), np.random.default_rng(budget + len(gone))
+    c = _cache(rng, dtype, lens, hkv, dh, page, 2, track=True)
+    c.weight.copy_(torch.from_numpy(np.floor(rng.random(tuple(c.weight.shape)) * 40).astype(np.float32) / 8))
+    c.weight[:, :, 1::7] = NAN
+    c.pos.copy_(torch.from_numpy(np.stack([np.stack([rng.permutation(c.slots) for _ in range(hkv)]) for _ in lens]).astype(np.int32)))
+    table, edge = c.page_table.clone(), -(-budget // page)
+    for b, L in enumerate(lens):
+        last = (L - 1) // page
+        low, high = rng.permutation(edge)[:max(1, edge // 3)], edge + rng.permutation(max(0, last + 1 - edge))[:max(1, (last - edge) // 3)]
+        if gone == "most":
+            low, high = rng.permutation(edge)[:edge // 2], np.arange(edge, last + 1)[1:]
+        for p in ([] if gone == "high" else low.tolist()) + ([] if gone == "low" else high.tolist()):
+            table[b, p] = -1 if p % 2 else c.k.shape[0] + p
+    c2 = moa.PagedCache(c.k, c.v, table, c.len, c.weight, c.pos, c.seen)
+    w, pos, seen = c.weight.cpu().numpy(), c.pos.cpu().numpy(), c.seen.cpu().numpy()
+    k0, v0 = c.k.clone(), c.v.clone()
+    wo, po = (torch.full_like(c.weight, -7.0), torch.full_like(c.pos, -7)) if apart else (c.weight, c.pos)
+    moa.moa_paged_evict(c2, budget, sink, recent, weight_out=wo, pos_out=po)
+    torch.cuda.synchronize()
+    assert c.len.tolist() == [min(L, budget) for L in lens]
+    want_w, want_p = (np.full_like(w, -7.0), np.full_like(pos, -7)) if apart else (w.copy(), pos.copy())
+    there = ((table >= 0) & (table < c.k.shape[0])).cpu().numpy()
+    for b, L in enumerate(lens):
+        for h in range(hkv):
+            def key(j):
+                if not there[b, j // page]:
+                    return (0 if j < budget else 3, 0.0, j)
+                if pos[b, h, j] < sink or pos[b, h, j] >= seen[b] - recent:
+                    return (0, 0.0, j)
+                return (2, 0.0, j) if np.isnan(w[b, h, j]) else (1, -float(w[b, h, j]), j)
+            kept = set(sorted(range(L), key=key)[:budget])
+            src, dst = [j for j in range(budget, L) if j in kept], [j for j in range(min(L, budget)) if j not in kept]
+            assert len(src) == len(dst) and all(there[b, j // page] for j in src + dst)
+            stay = [j for j in kept if j < budget]
+            want_w[b, h, stay], want_p[b, h, stay] = w[b, h, stay], pos[b, h, stay]
+            want_w[b, h, dst], want_p[b, h, dst] = w[b, h, src], pos[b, h, src]
+            if src:
+                s, d = torch.tensor(src, device="cuda"), torch.tensor(dst, device="cuda")
+                at = table[b].long()
+                ks, vs = c.k[at[s // page], s % page, h].clone(), c.v[at[s // page], s % page, h].clone()
+                k0[at[d // page], d % page, h], v0[at[d // page], d % page, h] = ks, vs
+    assert torch.equal(c.k.view(torch.uint8), k0.view(torch.uint8)) and torch.equal(c.v.view(torch.uint8), v0.view(torch.uint8))
+    assert np.array_equal(po.cpu().numpy(), want_p)
+    assert np.array_equal(wo.cpu().numpy().view(np.int32), want_w.view(np.int32))
