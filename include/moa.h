@@ -332,7 +332,9 @@ moa_status moa_paged_attention(const moa_paged_cache *cache, const void *q, int6
 
 /* Ends a cycle for n uncommitted rows. With acc_slot (device int32 [batch, cap]) and acc_len (device int32 [batch]), as
  * moa_verify_greedy writes them: the accepted rows' keys and values move to slots len[b] .. len[b] + acc_len[b] - 1, the
- * others are given up (n <= MOA_PAGED_MAX_ROWS; the listed slots rise). advance != 0: len (and seen) grow by acc_len, or by
+ * others are given up (n <= MOA_PAGED_MAX_ROWS; the listed slots rise). The pages of the n rows have to be in the table: of a
+ * row on a missing page nothing is stored, so it cannot be kept; a listed row that comes from such a page leaves its new slot
+ * as it was, one that goes to such a page is lost, and the other listed rows are kept all the same. advance != 0: len (and seen) grow by acc_len, or by
  * n when acc_len is NULL. With several layers that share len: the layers' calls without advance, then one with it. */
 moa_status moa_paged_commit(const moa_paged_cache *cache, int32_t n, const int32_t *acc_slot, const int32_t *acc_len, int32_t cap,
                             int32_t advance, void *stream);

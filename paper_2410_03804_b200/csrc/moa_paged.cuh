@@ -994,9 +994,9 @@ __global__ void __launch_bounds__(256) paged_append_kernel(PagedView C, const T*
 
 // Keeps the accepted path of n uncommitted rows: slot len + acc_slot[j] moves to slot len + j, j < acc_len. acc_slot rises
 // strictly and acc_slot[j] >= j, so a row's source is read before any row that could overwrite it is written when all of
-// them are read first: one CTA per (sequence, head) holds the path's rows (cap <= 64) in registers. Entries that do not
-// rise end the path. Then len (and seen) advance, when asked to, by one thread of the sequence's first CTA -- the heads'
-// CTAs read len, so the advance is a launch of its own.
+// them are read first: one CTA per (sequence, head) holds the path's rows (n <= 64) in registers. Entries that do not rise end
+// the path; a row from or to a page that the table does not have is skipped. The heads' CTAs read len, so its advance is a
+// launch of its own (paged_advance_kernel).
 template <typename T>
 __global__ void __launch_bounds__(256) paged_path_kernel(PagedView C, int n, const int* acc_slot, const int* acc_len, int cap, int dh) {
   pdl_trigger();

@@ -242,3 +242,29 @@ def test_evict_with_missing_pages(dtype, dh, hkv, page, lens, budget, sink, rece
     assert torch.equal(c.k.view(torch.uint8), k0.view(torch.uint8)) and torch.equal(c.v.view(torch.uint8), v0.view(torch.uint8))
     assert np.array_equal(po.cpu().numpy(), want_p)
     assert np.array_equal(wo.cpu().numpy().view(np.int32), want_w.view(np.int32))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_commit_with_missing_pages(dtype):
+    """A listed row that comes from a missing page leaves its new slot as it was, one that goes to such a page is lost; the
+    others are kept, and nothing else is written."""
+    moa, rng = _moa(), np.random.default_rng(5)
+    lens, n, hkv, dh, page = [30, 13, 24], 40, 2, 64, 8
+    c = _cache(rng, dtype, lens, hkv, dh, page, n)
+    _, kn, vn = _rows_of(rng, dtype, 3, n, hkv, hkv, dh)
+    moa.moa_paged_append(c, kn, vn)
+    table = c.page_table.clone()
+    table[0, 6], table[1, 2], table[2, 3] = -1, c.k.shape[0], -9
+    path = torch.tensor([[0, 1, 5, 18, 19, 33, 39], [0, 3, 4, 10, 12, 30, -1], [0, 2, 30, 31, -1, -1, -1]], dtype=torch.int32, device="cuda")
+    m = torch.tensor([7, 6, 4], dtype=torch.int32, device="cuda")
+    k0, v0 = c.k.clone(), c.v.clone()
+    k1, v1, at, there = c.k.clone(), c.v.clone(), table.tolist(), lambda p: 0 <= p < c.k.shape[0]
+    for b, L in enumerate(lens):
+        for j in range(int(m[b])):
+            s, d = L + int(path[b, j]), L + j
+            ps, pd = at[b][s // page], at[b][d // page]
+            if there(ps) and there(pd):
+                k1[pd, d % page], v1[pd, d % page] = k0[ps, s % page], v0[ps, s % page]
+    moa.moa_paged_commit(moa.PagedCache(c.k, c.v, table, c.len), n, path, m)
+    assert c.len.tolist() == [37, 19, 28]
+    assert torch.equal(c.k.view(torch.uint8), k1.view(torch.uint8)) and torch.equal(c.v.view(torch.uint8), v1.view(torch.uint8))
