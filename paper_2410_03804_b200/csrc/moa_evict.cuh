@@ -40,11 +40,11 @@ struct EvictArgs {
 // everything before the budget, lowest of all behind it. So none is a source of a move -- as many slots as the budget have
 // higher keys, or all that have a page lie before it -- and none a destination.
 __device__ __forceinline__ uint32_t evict_key(float w, int pos, int sink, int edge, bool page, bool low) {
-  if (!page) return low ? 0xffffffffu : 0u;
-  if (pos < sink || pos >= edge) return 0xffffffffu;
-  if (w != w) return 1u;
   const uint32_t u = __float_as_uint(w + 0.f);
-  return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
+  uint32_t k = (u & 0x80000000u) ? ~u : (u | 0x80000000u);
+  k = w != w ? 1u : k;
+  k = pos < sink || pos >= edge ? 0xffffffffu : k;
+  return page ? k : low ? 0xffffffffu : 0u;
 }
 
 // Exclusive prefix sum of one value per thread over the CTA; total gets the sum. Ends with a barrier.

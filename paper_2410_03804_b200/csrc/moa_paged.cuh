@@ -321,7 +321,7 @@ struct PagedWarp<bf16, DH> {
 
   // One step: 16 positions, keys at K, values at V. see(w, j): whether a row with mask word w sees position j of the step;
   // plain: every row sees every position. score: the tile's first row of scores, or null.
-  template <typename See>
+  template <bool MANY, typename See>
   __device__ __forceinline__ void step(const PagedAttn& P, const uint8_t* K, uint8_t* V, bool plain, See see, float* score, int, int mt, int R) {
     const int lane = threadIdx.x & 31;
     const uint32_t sK = smem_u32(K), sV = smem_u32(V);
@@ -366,7 +366,7 @@ struct PagedWarp<bf16, DH> {
       l[0] *= f[0];
       l[1] *= f[1];
     }
-    if (!plain && P.n > 1) {
+    if (MANY && !plain) {
       constexpr int N = KW * DH * 2 / 512;   // 16-byte pieces of the values per lane
       bool odd = false;
 #pragma unroll
@@ -458,8 +458,7 @@ struct PagedWarp<float, DH> {
       const int r = mt * PG_ROWS + rl;
       float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
       if (r < R)
-        x = __ldg(reinterpret_cast<const float4*>((const float*)P.q + ((long long)b * P.n + r / P.group) * P.q_stride +
-                                                  (long long)(h * P.group + r % P.group) * DH) + c);
+        x = reinterpret_cast<const float4*>((const float*)P.q + ((long long)b * P.n + r / P.group) * P.q_stride + (long long)(h * P.group + r % P.group) * DH)[c];
       reinterpret_cast<float4*>(sq)[i] = x;
     }
     __syncthreads();
@@ -481,7 +480,7 @@ struct PagedWarp<float, DH> {
     return __all_sync(0xffffffffu, rr >= R || row_word(P, b, rr / P.group) != 0ull);
   }
 
-  template <typename See>
+  template <bool MANY, typename See>
   __device__ __forceinline__ void step(const PagedAttn& P, const uint8_t* K, uint8_t* V, bool plain, See see, float* score, int b, int mt, int) {
     const int lane = threadIdx.x & 31;
     const int kk = lane & 7, quarter = lane >> 3;
@@ -557,7 +556,7 @@ struct PagedWarp<float, DH> {
         const float2 t = *reinterpret_cast<const float2*>(V + off(k, lane >> 1) + (lane & 1) * 8);
         v[0] = t.x; v[1] = t.y;
       }
-      if (!plain && P.n > 1) {
+      if (MANY && !plain) {
 #pragma unroll
         for (int d = 0; d < DL; ++d)
           if (odd_f(v[d])) {                 // (rare)
@@ -613,7 +612,9 @@ __device__ __forceinline__ void store4(T* dst, const float4 a) {
   else *reinterpret_cast<float4*>(dst) = a;
 }
 
-template <typename T, int DH>
+// MANY: more than one row per sequence, so that some rows may see a slot that others do not (those steps inline cost a token's
+// call 2 %).
+template <typename T, int DH, bool MANY>
 __global__ void __launch_bounds__(PG_THREADS, 1) paged_rows_kernel(const PagedAttn P) {
   using C = PagedCfg<T, DH>;
   pdl_trigger();
@@ -744,7 +745,7 @@ __global__ void __launch_bounds__(PG_THREADS, 1) paged_rows_kernel(const PagedAt
           }
         }
         float* at = P.score ? P.score + ((long long)b * P.hq + h * P.group + mt * PG_ROWS) * P.score_ld + base : nullptr;
-        W.step(P, sK, sV, plain, sees, at, b, mt, R);
+        W.template step<MANY>(P, sK, sV, plain, sees, at, b, mt, R);
       } else if (P.score && base < keys) {                           // nothing there: the weights' pass reads -inf
         for (int i = lane; i < C::KW * min(PG_ROWS, R - mt * PG_ROWS); i += 32)
           P.score[((long long)b * P.hq + h * P.group + mt * PG_ROWS + i / C::KW) * P.score_ld + base + i % C::KW] = -INFINITY;

@@ -162,6 +162,74 @@ __device__ __forceinline__ unsigned long long row_bits(unsigned long long w, lon
   return v & low_bits(keys - base);
 }
 
+// Rare steps of the softmax, kept out of its loop's code: inline they cost the loop 2 to 6 % without ever running.
+
+// Probabilities of a block's scores (tensor memory, at tS), over the scores, for rows with scores far from zero; returns their sum.
+__device__ __noinline__ float pt_steep(uint32_t tS, bool masked, unsigned long long vis0, unsigned long long vis1, float sub, float scale) {
+  float l = 0.f;
+#pragma unroll 1
+  for (int e0 = 0; e0 < PT_KB; e0 += 16) {   // the probabilities, two to a column, stay behind the scores that are read
+    float s[16];
+    tc_ld16(tS + (uint32_t)e0, s);
+    const uint32_t v = (uint32_t)((e0 < 64 ? vis0 : vis1) >> (e0 & 63));
+    uint32_t w8[8];
+#pragma unroll
+    for (int e = 0; e < 16; e += 2) {
+      const float p0 = masked && !((v >> e) & 1u) ? 0.f : ex2_approx((s[e] - sub) * scale);
+      const float p1 = masked && !((v >> e) & 2u) ? 0.f : ex2_approx((s[e + 1] - sub) * scale);
+      l += p0 + p1;
+      w8[e / 2] = pack_bf16(p0, p1);
+    }
+    tc_st8(tS + (uint32_t)(e0 / 2), w8);
+  }
+  return l;
+}
+// A row of a ring slot's values: cleared, or, where its position is there, cleared of what is not finite.
+template <int DH>
+__device__ __noinline__ void pt_clear(uint8_t* at, int row, bool there, volatile int* odd_flag) {
+  auto piece = [&](int p) { return reinterpret_cast<uint4*>(at + (p >> 3) * PtCfg<DH>::CHUNK + (((p ^ row) & 7) << 4)); };
+  if (!there) {
+#pragma unroll
+    for (int p = 0; p < DH / 8; ++p) *piece(p) = make_uint4(0u, 0u, 0u, 0u);
+    return;
+  }
+  uint32_t top = 0u;                         // exponents of all ones carry into the signs
+#pragma unroll
+  for (int p = 0; p < DH / 8; ++p) {
+    const uint4 x = *piece(p);
+    top |= ((x.x & 0x7f807f80u) + 0x00800080u) | ((x.y & 0x7f807f80u) + 0x00800080u);
+    top |= ((x.z & 0x7f807f80u) + 0x00800080u) | ((x.w & 0x7f807f80u) + 0x00800080u);
+  }
+  if ((top & 0x80008000u) == 0u) return;
+  *odd_flag = 1;
+  __threadfence_block();                     // who finds the bytes cleared finds the flag
+#pragma unroll 1
+  for (int p = 0; p < DH / 8; ++p) *piece(p) = odd_cleared(*piece(p));
+}
+// Adds to a row's output (tensor memory, at tO) the values that are not finite of the new slots that it sees among positions
+// from .. to - 1. A whole warp; the rows' words may differ.
+template <int DH>
+__device__ __noinline__ void pt_add_odd(const PagedAttn& P, int b, int h, long long from, long long to, int len, long long keys, unsigned long long word,
+                                        uint32_t tO) {
+  for (int d = 0; d < DH; d += 16) {
+    float o[16];
+    tc_ld16(tO + (uint32_t)d, o);
+    for (int j = 0; j < P.n_new; ++j) {
+      const long long key = (long long)len + j, at = key >= from && key < to && key < keys && ((word >> j) & 1ull) ? P.c.row(b, key, DH) : -1;
+      if (at < 0) continue;
+      const bf16* v = (const bf16*)P.c.v + at + (long long)h * DH + d;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const float x = __bfloat162float(v[e]);
+        if (odd_f(x)) o[e] += x;
+      }
+    }
+    __syncwarp();
+    tc_st16(tO + (uint32_t)d, o);
+  }
+  asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+}
+
 template <int DH>
 __global__ void __launch_bounds__(PT_THREADS, 1) paged_tree_kernel(const __grid_constant__ PagedTree PP) {
   using C = PtCfg<DH>;
@@ -394,20 +462,7 @@ __global__ void __launch_bounds__(PT_THREADS, 1) paged_tree_kernel(const __grid_
             dead = __any_sync(0xffffffffu, !mbar_wait(full_bar(vs), (v / PT_SLOTS) & 1u, abort_flag));
             if (dead) continue;
             const bool there = (((row < 64 ? live[0] : live[1]) >> (row & 63)) & 1ull) != 0ull;
-            if (!there || k0 + row >= len) {
-              uint8_t* d = bp + oRing + vs * C::SLOT + row * 128;
-#pragma unroll
-              for (int p = 0; p < DH / 8; ++p) {
-                uint4* at = reinterpret_cast<uint4*>(d + (p >> 3) * C::CHUNK + (((p ^ row) & 7) << 4));
-                if (!there) {
-                  *at = make_uint4(0u, 0u, 0u, 0u);
-                } else if (odd_any(*at)) {
-                  *odd_flag = 1;
-                  __threadfence_block();     // who finds the bytes cleared finds the flag
-                  *at = odd_cleared(*at);
-                }
-              }
-            }
+            if (!there || k0 + row >= len) pt_clear<DH>(bp + oRing + vs * C::SLOT + row * 128, row, there, odd_flag);
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
           }
         }
@@ -465,33 +520,29 @@ __global__ void __launch_bounds__(PT_THREADS, 1) paged_tree_kernel(const __grid_
         // half a unit of its last place off: the row's common factor, below 2^0.5 while it is below 2^24. From there on (or
         // where it leaves fp32) the difference is taken first.
         const float scaled = __fmul_rn(sub, P.scale_log2);
-        const bool steep = __any_sync(0xffffffffu, fabsf(scaled) >= 16777216.f);
-        const float minus = steep ? 0.f : -scaled;
-        const uint64_t scale2 = f2_pack(P.scale_log2, P.scale_log2), sub2 = f2_pack(minus, minus);
-        uint64_t l2[2] = {0ull, 0ull};
+        if (__any_sync(0xffffffffu, fabsf(scaled) >= 16777216.f)) {
+          l_run += pt_steep(tS, masked, vis[0], vis[1], sub, P.scale_log2);
+        } else {
+          const uint64_t scale2 = f2_pack(P.scale_log2, P.scale_log2), sub2 = f2_pack(-scaled, -scaled);
+          uint64_t l2[2] = {0ull, 0ull};
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-          if (half) load_half(1);
-          if (steep) {
+          for (int half = 0; half < 2; ++half) {
+            if (half) load_half(1);
 #pragma unroll
-            for (int e = 0; e < 64; ++e) s[e] -= sub;
-          }
+            for (int e = 0; e < 64; e += 16) {
+              uint32_t w8[8];
 #pragma unroll
-          for (int e = 0; e < 64; e += 16) {
-            uint32_t w8[8];
-#pragma unroll
-            for (int u = 0; u < 8; ++u) {
-              float p0, p1;
-              f2_unpack(f2_fma(f2_pack(s[e + 2 * u], s[e + 2 * u + 1]), scale2, sub2), p0, p1);
-              p0 = ex2_approx(p0);
-              p1 = ex2_approx(p1);
-              l2[u & 1] = f2_add(l2[u & 1], f2_pack(p0, p1));
-              w8[u] = pack_bf16(p0, p1);
+              for (int u = 0; u < 8; ++u) {
+                float p0, p1;
+                f2_unpack(f2_fma(f2_pack(s[e + 2 * u], s[e + 2 * u + 1]), scale2, sub2), p0, p1);
+                p0 = ex2_approx(p0);
+                p1 = ex2_approx(p1);
+                l2[u & 1] = f2_add(l2[u & 1], f2_pack(p0, p1));
+                w8[u] = pack_bf16(p0, p1);
+              }
+              tc_st8(tS + (uint32_t)(half * 32 + e / 2), w8);
             }
-            tc_st8(tS + (uint32_t)(half * 32 + e / 2), w8);
           }
-        }
-        {
           float a0, a1;
           f2_unpack(f2_add(l2[0], l2[1]), a0, a1);
           l_run += a0 + a1;
@@ -503,11 +554,11 @@ __global__ void __launch_bounds__(PT_THREADS, 1) paged_tree_kernel(const __grid_
       // ---- the segment's result ----
       if (!dead) dead = __any_sync(0xffffffffu, !mbar_wait(o_bar(i), (c - 1u) & 1u, abort_flag));
       tc_fence_after();
+      __threadfence_block();
+      if (__any_sync(0xffffffffu, *odd_flag != 0 && !dead)) pt_add_odd<DH>(P, W.b, W.h, (long long)W.t0 * PT_KB, (long long)(W.t0 + W.nb) * PT_KB, len, keys, word, tO);
       const float inv = dead ? __int_as_float(0x7fffffff) : l_run == 0.f ? 0.f : 1.f / l_run;
       const size_t piece_at = (size_t)blockIdx.x * 2 + (W.x0 > W.x_begin ? 1 : 0), prow = piece_at * PT_ROWS + i * 128 + row;
       const bool none = l_run == 0.f && !dead;                       // the row sees nothing
-      __threadfence_block();
-      const bool odd = *odd_flag != 0;
 #pragma unroll 1
       for (int d = 0; d < DH; d += 16) {
         float o[16];
@@ -516,20 +567,6 @@ __global__ void __launch_bounds__(PT_THREADS, 1) paged_tree_kernel(const __grid_
         } else {
 #pragma unroll
           for (int e = 0; e < 16; ++e) o[e] = 0.f;
-        }
-        if (odd) {                           // (rare) values of new slots that are not finite, for the rows that see them
-          for (int j = 0; j < P.n_new; ++j) {
-            const long long key = (long long)len + j, block = key / PT_KB - W.t0;
-            if (!((word >> j) & 1ull) || key >= keys || block < 0 || block >= W.nb) continue;
-            const long long at = P.c.row(W.b, key, DH);
-            if (at < 0) continue;
-            const bf16* v = (const bf16*)P.c.v + at + (long long)W.h * DH + d;
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-              const float x = __bfloat162float(v[e]);
-              if (odd_f(x)) o[e] += x;
-            }
-          }
         }
         if (W.whole) {                       // staged over this thread's own query row, whose last scores have been formed
           uint32_t w8[8];
