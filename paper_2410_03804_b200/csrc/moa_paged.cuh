@@ -21,6 +21,10 @@
 // keeps a three-stage ring of its own in shared memory (cp.async, no barrier of the CTA in the loop), with its own running
 // maximum, sum and output. The copies run two steps ahead, across the items' borders; at an item's end the warps' states
 // are merged through the ring stage that was read last, while the other two fill.
+//
+// A kernel here may begin while the kernels before it in the stream still write its inputs (programmatic launches), so nothing
+// is read through the non-coherent path, whose data may not change while a kernel lives: what is read once comes past L1, the
+// rest by ordinary loads.
 #pragma once
 #include "moa_attn.cuh"
 
@@ -43,7 +47,7 @@ struct PagedView {
   const int* seen;                           // [batch] next position, null when pos is
   int batch, max_pages, n_pages, shift, hkv; // page_size = 1 << shift
   __device__ __forceinline__ long long cap() const { return (long long)max_pages << shift; }
-  __device__ __forceinline__ int page_of(int b, long long slot) const { return __ldg(table + (size_t)b * max_pages + (size_t)(slot >> shift)); }
+  __device__ __forceinline__ int page_of(int b, long long slot) const { return table[(size_t)b * max_pages + (size_t)(slot >> shift)]; }
   // element offset of (slot, head 0) of sequence b, or -1 where the table has no such page
   __device__ __forceinline__ long long row(int b, long long slot, int dh) const {
     const int page = page_of(b, slot);
@@ -236,12 +240,12 @@ __device__ __forceinline__ unsigned long long any_word(const PagedAttn& P, int b
   if (!P.mask) return causal_word(P.n - 1);
   const int lane = threadIdx.x & 31;
   const unsigned long long* m = P.mask + (size_t)b * P.n;
-  unsigned long long a = lane < P.n ? __ldg(m + lane) : 0ull;
-  if (lane + 32 < P.n) a |= __ldg(m + lane + 32);
+  unsigned long long a = lane < P.n ? m[lane] : 0ull;
+  if (lane + 32 < P.n) a |= m[lane + 32];
   return ((unsigned long long)__reduce_or_sync(0xffffffffu, (unsigned)(a >> 32)) << 32) | __reduce_or_sync(0xffffffffu, (unsigned)a);
 }
 __device__ __forceinline__ unsigned long long row_word(const PagedAttn& P, int b, int i) {
-  return P.mask ? __ldg(P.mask + (size_t)b * P.n + i) : causal_word(i);
+  return P.mask ? P.mask[(size_t)b * P.n + i] : causal_word(i);
 }
 
 // A value that is not finite belongs to the rows that see its slot, and zero times it is not zero. A slot of a tree is seen by
@@ -298,8 +302,8 @@ struct PagedWarp<bf16, DH> {
                                                             (long long)(h * P.group + rc % P.group) * DH);
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
-      qf[ks][0] = __ldg(src + ks * 8 + tq);
-      qf[ks][1] = __ldg(src + ks * 8 + 4 + tq);
+      qf[ks][0] = src[ks * 8 + tq];
+      qf[ks][1] = src[ks * 8 + 4 + tq];
     }
   }
   __device__ __forceinline__ void clear() {
@@ -937,9 +941,9 @@ __global__ void __launch_bounds__(256) paged_weights_kernel(const PagedAttn P) {
     const float old = in && P.c.weight && slot < s_len[b] ? P.c.weight[at] : 0.f;
     float z[8];
 #pragma unroll
-    for (int u = 0; u < 8; ++u) z[u] = in && u < P.group ? __ldg(score + u * P.score_ld) : -INFINITY;
+    for (int u = 0; u < 8; ++u) z[u] = in && u < P.group ? __ldcg(score + u * P.score_ld) : -INFINITY;
     if (threadIdx.x < P.group) {
-      const float2 t = __ldg(reinterpret_cast<const float2*>(P.item_ml) + (size_t)(b * P.c.hkv + h) * P.tiles * PG_ROWS + threadIdx.x);
+      const float2 t = __ldcg(reinterpret_cast<const float2*>(P.item_ml) + (size_t)(b * P.c.hkv + h) * P.tiles * PG_ROWS + threadIdx.x);
       ml[threadIdx.x] = make_float2(t.x == -INFINITY ? 0.f : t.x, t.y == 0.f ? 0.f : 1.f / t.y);
     }
     __syncthreads();
@@ -947,7 +951,7 @@ __global__ void __launch_bounds__(256) paged_weights_kernel(const PagedAttn P) {
     for (int g0 = 0; g0 < P.group; g0 += 8) {
       if (g0 > 0) {
 #pragma unroll
-        for (int u = 0; u < 8; ++u) z[u] = in && g0 + u < P.group ? __ldg(score + (g0 + u) * P.score_ld) : -INFINITY;
+        for (int u = 0; u < 8; ++u) z[u] = in && g0 + u < P.group ? __ldcg(score + (g0 + u) * P.score_ld) : -INFINITY;
       }
 #pragma unroll
       for (int u = 0; u < 8; ++u)
@@ -973,7 +977,7 @@ __global__ void __launch_bounds__(256) paged_append_kernel(PagedView C, const T*
   unsigned long long any = ~0ull;
   if (mask) {                                                        // n <= 64
     any = 0ull;
-    for (int i = 0; i < n; ++i) any |= __ldg(mask + (size_t)b * n + i);
+    for (int i = 0; i < n; ++i) any |= mask[(size_t)b * n + i];
   }
   for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < (long long)rows * per; i += (long long)gridDim.x * blockDim.x) {
     const int r = (int)(i / per), c = (int)(i - (long long)r * per);
@@ -982,8 +986,8 @@ __global__ void __launch_bounds__(256) paged_append_kernel(PagedView C, const T*
     const long long o = C.row(b, slot, dh);
     const size_t src = (size_t)((long long)b * n + r) * (size_t)row_stride + (size_t)c * E;
     if (o >= 0 && (!mask || ((any >> r) & 1ull))) {
-      *reinterpret_cast<uint4*>((T*)C.k + o + (long long)c * E) = __ldg(reinterpret_cast<const uint4*>(k_new + src));
-      *reinterpret_cast<uint4*>((T*)C.v + o + (long long)c * E) = __ldg(reinterpret_cast<const uint4*>(v_new + src));
+      *reinterpret_cast<uint4*>((T*)C.k + o + (long long)c * E) = __ldcg(reinterpret_cast<const uint4*>(k_new + src));
+      *reinterpret_cast<uint4*>((T*)C.v + o + (long long)c * E) = __ldcg(reinterpret_cast<const uint4*>(v_new + src));
     }
     if (C.pos && (c * E) % dh == 0) {
       const size_t at = ((size_t)b * C.hkv + c * E / dh) * (size_t)C.cap() + (size_t)slot;

@@ -64,7 +64,7 @@ template <int DH>
 __global__ void __launch_bounds__(256) paged_join_kernel(const PagedAttn P) {
   pdl_trigger();
   pdl_wait(KID_ATTN_MERGE);
-  const int4 j0 = __ldg(reinterpret_cast<const int4*>(P.joins) + blockIdx.x * 2), j1 = __ldg(reinterpret_cast<const int4*>(P.joins) + blockIdx.x * 2 + 1);
+  const int4 j0 = __ldcg(reinterpret_cast<const int4*>(P.joins) + blockIdx.x * 2), j1 = __ldcg(reinterpret_cast<const int4*>(P.joins) + blockIdx.x * 2 + 1);
   const int c = blockIdx.x + 1, c1 = j0.x, fp = j0.y, b = j0.z, h = j0.w, mt = j1.x;         // c1: last CTA with a piece, 0: no join
   if (c1 == 0) return;
   const int r = threadIdx.x, rr = mt * PT_ROWS + r;                  // row of the item, of the (sequence, head)
@@ -72,7 +72,7 @@ __global__ void __launch_bounds__(256) paged_join_kernel(const PagedAttn P) {
   if ((rr & ~31) >= R) return;
   float M = -INFINITY, Z = 0.f;
 #pragma unroll 4
-  for (int i = c - 1; i <= c1; ++i) M = fmaxf(M, __ldg(P.part_ml + ((size_t)piece_of(i, c - 1, fp) * PT_ROWS + r) * 2));
+  for (int i = c - 1; i <= c1; ++i) M = fmaxf(M, __ldcg(P.part_ml + ((size_t)piece_of(i, c - 1, fp) * PT_ROWS + r) * 2));
   const float ref = M == -INFINITY ? 0.f : M;
   constexpr int N4 = DH / 16;                                        // 16-byte pieces of a row in a quarter
   float4 a[N4];
@@ -81,12 +81,12 @@ __global__ void __launch_bounds__(256) paged_join_kernel(const PagedAttn P) {
 #pragma unroll 2
   for (int i = c - 1; i <= c1; ++i) {
     const size_t piece = piece_of(i, c - 1, fp);
-    const float2 ml = __ldg(reinterpret_cast<const float2*>(P.part_ml) + piece * PT_ROWS + r);
+    const float2 ml = __ldcg(reinterpret_cast<const float2*>(P.part_ml) + piece * PT_ROWS + r);
     const float f = exp2f((ml.x - ref) * P.scale_log2);
     Z = fmaf(f, ml.y, Z);
 #pragma unroll
     for (int d = 0; d < N4; ++d) {
-      const float4 o = __ldg(reinterpret_cast<const float4*>(P.part_o) + (piece * (DH / 4) + blockIdx.y * N4 + d) * PT_ROWS + r);
+      const float4 o = __ldcg(reinterpret_cast<const float4*>(P.part_o) + (piece * (DH / 4) + blockIdx.y * N4 + d) * PT_ROWS + r);
       a[d].x = fmaf(f, o.x, a[d].x); a[d].y = fmaf(f, o.y, a[d].y); a[d].z = fmaf(f, o.z, a[d].z); a[d].w = fmaf(f, o.w, a[d].w);
     }
   }
@@ -293,7 +293,7 @@ __global__ void __launch_bounds__(PT_THREADS, 1) paged_tree_kernel(const __grid_
       const int x0 = W.h * DH + chunk * 64;
       for (int t = 0; t < W.nb && ok; ++t) {
         const long long slot0 = (long long)(W.t0 + t) * PT_KB + sub * rows;
-        int page = mine && slot0 < keys ? __ldg(table + (slot0 >> P.c.shift)) : P.c.n_pages;
+        int page = mine && slot0 < keys ? table[slot0 >> P.c.shift] : P.c.n_pages;
         if (page < 0 || page > P.c.n_pages) page = P.c.n_pages;
         const int y = (int)(slot0 & ((1 << P.c.shift) - 1));
         for (int kv = 0; kv < 2; ++kv, ++cnt) {
@@ -402,12 +402,12 @@ __global__ void __launch_bounds__(PT_THREADS, 1) paged_tree_kernel(const __grid_
       // The segment's loads go out together, before the first is waited for: mask words, the first block's pages, queries.
       const int* table = P.c.table + (size_t)W.b * P.c.max_pages;
       const unsigned long long* mask = P.mask ? P.mask + (size_t)W.b * P.n : nullptr;
-      unsigned long long word = mask ? __ldg(mask + qi) : causal_word(qi);
-      unsigned long long any = mask && lane < P.n ? __ldg(mask + lane) : 0ull, any2 = mask && lane + 32 < P.n ? __ldg(mask + lane + 32) : 0ull;
+      unsigned long long word = mask ? mask[qi] : causal_word(qi);
+      unsigned long long any = mask && lane < P.n ? mask[lane] : 0ull, any2 = mask && lane + 32 < P.n ? mask[lane + 32] : 0ull;
       // the page of a block that this lane looks at (blocks of up to 16 pages), loaded a block ahead
       auto page_at = [&](int t) -> int {
         const long long at = (long long)(W.t0 + t) * PT_KB + ((long long)lane << P.c.shift);
-        return t < W.nb && (lane << P.c.shift) < PT_KB && at < keys ? __ldg(table + (at >> P.c.shift)) : 0;
+        return t < W.nb && (lane << P.c.shift) < PT_KB && at < keys ? table[at >> P.c.shift] : 0;
       };
       int page_next = page_at(0);
       // queries, coalesced: the warp's 32 rows, 32 * 8 / DH of them per instruction, into shared memory (the tile's last scores
@@ -420,7 +420,7 @@ __global__ void __launch_bounds__(PT_THREADS, 1) paged_tree_kernel(const __grid_
         uint4 x[PIECES];
 #pragma unroll
         for (int u = 0; u < PIECES; ++u)
-          x[u] = __ldg(reinterpret_cast<const uint4*>((const bf16*)P.q + __shfl_sync(0xffffffffu, off, u * RPI + lane / PIECES)) + piece);
+          x[u] = __ldcg(reinterpret_cast<const uint4*>((const bf16*)P.q + __shfl_sync(0xffffffffu, off, u * RPI + lane / PIECES)) + piece);
 #pragma unroll
         for (int u = 0; u < PIECES; ++u)
           *reinterpret_cast<uint4*>(bp + i * C::QTILE + pt_q_off(quad * 32 + u * RPI + lane / PIECES, piece)) = x[u];

@@ -96,11 +96,11 @@ __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(NT) rules_kernel(co
   // ---- bitmap and hash table ----
   const int size = e1 - e0;
   auto in_slice = [&](int id) { return id >= e0 && id < e1; };
-  auto may = [&](int e) { return !allow || ((__ldg(allow + (e >> 5)) >> (e & 31)) & 1u) != 0u; };
+  auto may = [&](int e) { return !allow || ((allow[e >> 5] >> (e & 31)) & 1u) != 0u; };
   if (dense) {
     for (int i = tid; i < ((size + 31) & ~31); i += NT) {             // whole warps
       const unsigned m = __ballot_sync(0xffffffffu, i < size && counts[e0 + min(i, size - 1)] > 0);
-      if ((i & 31) == 0) mark[i >> 5] = allow ? m & __ldg(allow + (i >> 5)) : m;
+      if ((i & 31) == 0) mark[i >> 5] = allow ? m & allow[i >> 5] : m;
     }
   } else {
     for (int i0 = tid; i0 < n_words; i0 += 4 * NT) {
@@ -108,8 +108,8 @@ __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(NT) rules_kernel(co
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
         const int i = min(i0 + u * NT, n_words - 1);
-        m[u] = seen ? __ldg(seen + i) : 0u;
-        a[u] = allow && seen ? __ldg(allow + i) : ~0u;
+        m[u] = seen ? seen[i] : 0u;
+        a[u] = allow && seen ? allow[i] : ~0u;
       }
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
@@ -145,7 +145,7 @@ __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(NT) rules_kernel(co
     const int* bid = A.bias_id + (size_t)b * A.n_bias;
     const float* bval = A.bias_val + (size_t)b * A.n_bias;
     for (int i = tid; i < A.n_bias; i += NT) {
-      const int id = __ldg(bid + i);
+      const int id = bid[i];
       if (!in_slice(id) || !may(id - e0)) continue;
       const int s = slot_of(id);
       atomicAdd(&h_cnt[s], 1 << 16);
@@ -164,10 +164,10 @@ __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(NT) rules_kernel(co
       const int entries = h_cnt[s] >> 16;
       if (entries == 0) continue;
       const int i0 = h_first[s], id = h_id[s];
-      float v = __ldg(bval + i0);
+      float v = bval[i0];
       if (entries > 1)                        // the same id twice: summed in list order, whatever order the threads came in
         for (int i = i0 + 1; i < A.n_bias; ++i)
-          if (__ldg(bid + i) == id) v = __fadd_rn(v, __ldg(bval + i));
+          if (bid[i] == id) v = __fadd_rn(v, bval[i]);
       h_val[s] = v;
     }
   }
@@ -204,12 +204,12 @@ __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(NT) rules_kernel(co
     if (orow) orow[e0 + e] = from_f<T>(x);
     best_of(x, e, tv, te);
   };
-  auto in_record = [&](int e) { return seen && ((__ldg(seen + (e >> 5)) >> (e & 31)) & 1u); };
+  auto in_record = [&](int e) { return seen && ((seen[e >> 5] >> (e & 31)) & 1u); };
   uint32_t* pass = A.out ? mark + ((per_cta + 31) >> 5) + 1 : mark;      // without an output nobody asks for the marks again
   for (int w0 = tid; w0 < n_words; w0 += 4 * NT) {
     unsigned a[4];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) a[u] = allow ? __ldg(allow + min(w0 + u * NT, n_words - 1)) : ~0u;
+    for (int u = 0; u < 4; ++u) a[u] = allow ? allow[min(w0 + u * NT, n_words - 1)] : ~0u;
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
       const int wi = w0 + u * NT;
@@ -224,7 +224,7 @@ __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(NT) rules_kernel(co
           list[at] = e;
         } else {                                   // (rare) no room
           const bool known = in_record(e);
-          touch(e, to_f(xr[e0 + e]), known, counts && (known || dense) ? __ldg(counts + e0 + e) : 0);
+          touch(e, to_f(xr[e0 + e]), known, counts && (known || dense) ? __ldcg(counts + e0 + e) : 0);
         }
       }
     }
@@ -280,7 +280,7 @@ __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(NT) rules_kernel(co
         if (e[u] < 0) continue;
         x[u] = to_f(xs[e[u]]);
         known[u] = in_record(e[u]);
-        c[u] = counts ? __ldg(counts + e0 + e[u]) : 0;         // without its bit it does not count
+        c[u] = counts ? __ldcg(counts + e0 + e[u]) : 0;         // without its bit it does not count
       }
 #pragma unroll
       for (int u = 0; u < 4; ++u)
