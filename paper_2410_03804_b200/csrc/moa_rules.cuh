@@ -290,9 +290,9 @@ __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(NT) rules_kernel(co
     for (int k = tid; k < head + size - tail; k += LT) {
       const int e = k < head ? k : tail + k - head;
       if (os && ((mark8[e >> 3] >> (e & 7)) & 1u)) continue;
-      const float x = (pass8[e >> 3] >> (e & 7)) & 1u ? to_f(xs[e]) : -INFINITY;
-      if (os) os[e] = from_f<T>(x);
-      best_of(x, e, tv, te);
+      const T x = (pass8[e >> 3] >> (e & 7)) & 1u ? xs[e] : from_f<T>(-INFINITY);
+      if (os) os[e] = x;                           // the bits of a NaN included, as the pieces are passed on
+      best_of(to_f(x), e, tv, te);
     }
     if (SPLIT) first_step();
   }

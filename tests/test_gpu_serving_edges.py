@@ -268,3 +268,31 @@ def test_commit_with_missing_pages(dtype):
     moa.moa_paged_commit(moa.PagedCache(c.k, c.v, table, c.len), n, path, m)
     assert c.len.tolist() == [37, 19, 28]
     assert torch.equal(c.k.view(torch.uint8), k1.view(torch.uint8)) and torch.equal(c.v.view(torch.uint8), v1.view(torch.uint8))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("vocab", [2003, 32001])
+def test_rules_in_small_and_large_calls(dtype, vocab):
+    """The rows of a large call, which take a CTA each, and the same rows in small ones, which take a cluster each: the same bits."""
+    moa, rng = _moa(), np.random.default_rng(vocab)
+    batch, n = 12, 9
+    g = torch.Generator().manual_seed(vocab)
+    x = (torch.randn((batch, n, vocab), generator=g) * 3).to(T[dtype]).cuda()
+    x[:, 3, ::7] = NAN
+    x[:, 5] = x[:, 5].round()
+    counts = (torch.rand((batch, vocab), generator=g) < 0.1).int().cuda() * 2
+    word = lambda may: (torch.nn.functional.pad(may, (0, -vocab % 32)).unflatten(-1, (-1, 32)).long() << torch.arange(32)).sum(-1)  # noqa: E731
+    bits = lambda may: torch.where((w := word(may)) >= 2**31, w - 2**32, w).int().cuda()  # noqa: E731
+    seen = bits((counts.cpu() > 0) | (torch.rand((batch, vocab), generator=g) < 0.05))
+    allow = bits(torch.rand((batch, n, vocab), generator=g) < 0.5)
+    rep, freq, pres = (torch.rand(batch, generator=g).cuda() + 0.5 for _ in range(3))
+    bias_id = torch.randint(-1, vocab + 1, (batch, 70), generator=g).int().cuda()
+    bias_val = torch.randn((batch, 70), generator=g).cuda()
+    parent, _, _ = _trees(rng, batch, n, 2)
+    tok, par = torch.randint(0, vocab, (batch, n), generator=g).int().cuda(), torch.from_numpy(parent).cuda()
+    out, choice = moa.moa_logit_rules(moa.LogitRules(vocab, counts, seen, rep, freq, pres, bias_id, bias_val, allow), x, tok, par)
+    for b in range(batch):
+        one = slice(b, b + 1)
+        rules = moa.LogitRules(vocab, *(t[one].contiguous() for t in (counts, seen, rep, freq, pres, bias_id, bias_val, allow)))
+        o, c = moa.moa_logit_rules(rules, x[one].contiguous(), tok[one].contiguous(), par[one].contiguous())
+        assert torch.equal(o.view(torch.uint8), out[one].view(torch.uint8)) and torch.equal(c, choice[one])
