@@ -312,10 +312,11 @@ moa_status moa_paged_append(const moa_paged_cache *cache, const void *k_new, con
  * over the slots j < len[b] and, when n_new = n, the rows' own slots len[b] + j' that row i sees: bit j' of mask[b, i]
  * (device uint64 [batch, n], as moa_tree_attn_mask packs it for n <= 64), or j' <= i when mask is NULL. n_new = 0: the
  * committed slots only, as in a cross-attention. A row whose mask word is 0 (an unused slot) sees nothing, and a row that
- * sees nothing gives zeros. A new slot that no row sees is not read.
+ * sees nothing gives zeros. A new slot that no row sees is not read, and infinities and NaN among a slot's values reach the
+ * rows that see it only.
  *   q           T [batch, n, hq, head_dim], rows q_stride elements apart; head h belongs to key / value head h / (hq / hkv)
  *   k_new,v_new T [batch, n, hkv, head_dim], rows new_stride elements apart: appended by this call as moa_paged_append
- *               would (slots that no row sees are not written), or NULL when the rows are in the pages already
+ *               would (keys and values of slots that no row sees are not written), or NULL when the rows are in the pages already
  *   scale       0 means 1 / sqrt(head_dim); at most 2e38
  *   out         T [batch, n, hq, head_dim]
  *   weight_out  device float [batch, hkv, max_pages * page_size], may be cache->weight, or NULL; n = 1 only: for every slot
@@ -323,8 +324,12 @@ moa_status moa_paged_append(const moa_paged_cache *cache, const void *k_new, con
  *               of the softmax weights. Other entries stay as they were.
  *   ws          device scratch of moa_paged_workspace_bytes bytes. ZERO IT ONCE after allocating it: its first bytes count the
  *               parts of the work that have been joined, and a call leaves them at zero again
- * Scores, statistics and sums are fp32. hq / hkv <= 128; batch * hkv * (n * hq / hkv / 16, rounded up) * (max_pages * page_size
- * / 64) <= 2^30. */
+ * Scores, statistics and sums are fp32. bf16 values are multiplied by probabilities of two bf16 terms; calls of many query rows
+ * (n > 1, more than 16 of them per key / value head, pages of at least 8 rows, and a cache with room for enough work, by its size
+ * and not by the lengths) run on tensor memory and round each probability once to bf16, which puts an output off by at most 2^-8
+ * of sum p |v|. A wait inside that kernel that runs out (about 2 s; it means a fault of the device) leaves NaN in the rows concerned: these
+ * calls have no status word. hq / hkv <= 128; batch * hkv * (n * hq / hkv / 8, rounded up) * (max_pages * page_size / 64, rounded up)
+ * <= 2^30. */
 moa_status moa_paged_workspace_bytes(const moa_paged_cache *cache, int32_t n, int32_t hq, int32_t weights, size_t *bytes);
 moa_status moa_paged_attention(const moa_paged_cache *cache, const void *q, int64_t q_stride, const void *k_new, const void *v_new,
                                int64_t new_stride, int32_t n, int32_t n_new, int32_t hq, const uint64_t *mask, float scale, void *out,
@@ -343,7 +348,9 @@ moa_status moa_paged_commit(const moa_paged_cache *cache, int32_t n, const int32
  * its own: those of positions < sink and >= seen[b] - recent, and of the others the ones with the largest weight (a NaN
  * after all numbers, equal weights by the lower slot). The kept slots behind the budget move to the freed slots before it,
  * both in rising order; slots from the budget on are free afterwards. Slots on a page that the table does not have hold no
- * row: behind the budget they are given up before all others; before it they stay as they are and count towards it. Needs
+ * row: behind the budget they are given up before all others; before it they stay as they are and count towards it. Only
+ * calls of one row per sequence accumulate weights: a slot that came in with a tree, or a prompt, has weight 0 until tokens
+ * attended to it, and where all weights are equal the lowest slots are kept beside the protected positions. Needs
  * cache->weight, pos and seen; sink + recent <= budget.
  *   weight_out, pos_out  shaped as cache->weight and pos and may be them: entries of the slots in use afterwards
  *   len_out     device int32 [batch], may be cache->len, or NULL: min(len, budget), so the negative length of a sequence that is

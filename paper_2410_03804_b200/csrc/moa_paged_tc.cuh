@@ -15,15 +15,18 @@
 // product costs about 60 cycles at N = 64 as at N = 128, and the pipe was the limit (4700 cycles per 128 positions).
 // Tensor memory: S_0 S_1 O_0 O_1, 128 columns each. The output is rescaled only when a row's maximum grew by more than 2^8.
 // The probabilities enter the second product rounded once to bf16 (each off by at most 2^-8 of itself, so an output is off by
-// at most 2^-8 * sum p |v|, the size of its own rounding to bf16), while their sum is taken in fp32 before the rounding.
+// at most 2^-8 * sum p |v|, the size of its own rounding to bf16), while their sum is taken in fp32 before the rounding. With two
+// terms, as in the row kernel, the error against 64 bits fell from 0.0023 to 0.0017 of the output (its rounding alone) and the
+// large case below went from 173 to 211 us, 204 to 245 over seconds.
 // Work split and pieces are those of the row kernel, with items of 256 query rows and one CTA per SM; the pieces are joined by
 // a kernel behind it (paged_join_kernel), whose CTAs are four per cut item: the 128 KB of an item are too much for one.
-// Measured: 16 sequences x 61 rows x 64 heads over 4096 positions (0.133 TFLOP of products, 0.27 GB of cache): 168 us,
-// 0.79 PFLOP/s without the padding to 512 rows, 0.83 with it; counters: 1.4 instructions a cycle, tensor memory busy 52 %
-// of the time. What is left is the chain score product -> exponentials -> output product of two tiles that take turns.
-// 61 rows x 32 heads over 2048 positions: 29 us, two thirds of it the start (tensor memory, table, first copies: 9 us) and
-// the join. The row kernel took 1537 and 44 us for the two.
-// Every wait is bounded; a CTA whose wait ran out writes NaN to its rows.
+// Measured: 16 sequences x 61 rows x 64 heads over 4096 positions (0.133 TFLOP of products, 0.27 GB of cache): 173 us in short
+// bursts of replays, 198 to 204 us over seconds of calls (0.65 to 0.67 PFLOP/s without the padding to 512 rows). With half the
+// sequences the counters show the tensor pipe and the exponential unit at 40 % each and 1.05 instructions a cycle and SM: neither
+// pipe is the limit, but the chain of one block -- score product, one thread's pass over its row of 128 scores, output product --
+// of which two tiles are under way. 61 rows x 32 heads over 2048 positions: 29 us, two thirds of it the start (tensor memory,
+// table, first copies: 9 us) and the join. The row kernel took 1537 and 44 us for the two.
+// Every wait is bounded; a CTA whose wait ran out writes NaN to its rows (the serving calls have no status word).
 #pragma once
 #include "moa_attn_tc.cuh"
 #include "moa_paged.cuh"

@@ -18,11 +18,11 @@
 // counts as -inf, four tokens of a table's byte selectors at a time, and the place of the best of 16 bytes is looked up once,
 // at the end. Pieces are loaded four ahead. When a CTA has a row of its own, a quarter of its warps take the list while the
 // others stream.
-// Measured, 976 rows of 128256 bf16 with 300 biases: 73 us = 3.7 TB/s, of which the bitmap, the table and the list take the
-// first 15 us of a CTA. The allowed bits read again as bytes from global memory beside each piece: 109 us; list first, then
-// the stream by all warps: 82 us; listed tokens taken by the stream as it met them: 284 us; a CTA walking the rows of a
-// sequence with one list for all: 131 us, its rows' dependent steps no longer hidden by other CTAs. CTAs of 128 threads, seven
-// to an SM and all rows at once: 85 us against 73 us of 256 threads.
+// Measured, 976 rows of 128256 bf16 with 300 biases: 70 us = 3.8 TB/s (73 us when the following were tried), of which the
+// bitmap, the table and the list take the first 15 us of a CTA. The allowed bits read again as bytes from global memory beside
+// each piece: 109 us; list first, then the stream by all warps: 82 us; listed tokens taken by the stream as it met them: 284 us;
+// a CTA walking the rows of a sequence with one list for all: 131 us, its rows' dependent steps no longer hidden by other CTAs.
+// CTAs of 128 threads, seven to an SM and all rows at once: 85 us against 73 us of 256 threads.
 #pragma once
 #include "moa_verify.cuh"
 

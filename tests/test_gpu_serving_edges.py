@@ -296,3 +296,33 @@ def test_rules_in_small_and_large_calls(dtype, vocab):
         rules = moa.LogitRules(vocab, *(t[one].contiguous() for t in (counts, seen, rep, freq, pres, bias_id, bias_val, allow)))
         o, c = moa.moa_logit_rules(rules, x[one].contiguous(), tok[one].contiguous(), par[one].contiguous())
         assert torch.equal(o.view(torch.uint8), out[one].view(torch.uint8)) and torch.equal(c, choice[one])
+
+
+@pytest.mark.parametrize("dh,hq,hkv,n,lens", [(128, 4, 2, 2, [700, 33]), (64, 8, 8, 16, [300]), (128, 16, 2, 2, [5000, 1]), (64, 6, 2, 5, [64, 0, 999])])
+def test_rows_of_small_calls_keep_probabilities_in_two_terms(dh, hq, hkv, n, lens):
+    """Up to 16 query rows per key / value head a bf16 call keeps its probabilities in two bf16 terms, like a token's: the
+    tolerance is that of one row."""
+    moa, rng = _moa(), np.random.default_rng(n * hq)
+    c = _cache(rng, "bf16", lens, hkv, dh, 16, n)
+    q, kn, vn = _rows_of(rng, "bf16", len(lens), n, hq, hkv, dh)
+    _, anc, mask = _trees(rng, len(lens), n, 0)
+    out = moa.moa_paged_attention(c, q, kn, vn, mask=mask)
+    for b, L in enumerate(lens):
+        K, V = _slots(c, b, L)
+        K, V = np.concatenate([K, kn[b].double().cpu().numpy()]), np.concatenate([V, vn[b].double().cpu().numpy()])
+        for i in range(n):
+            see = np.concatenate([np.ones(L, bool), anc[b, i]])
+            for h in range(hq):
+                ref, _, mass, spread = _attend(q[b, i, h].double().cpu().numpy(), K[:, h * hkv // hq], V[:, h * hkv // hq], see, dh ** -0.5)
+                assert np.all(np.abs(out[b, i, h].double().cpu().numpy() - ref) <= _bound("bf16", dh, L + n, spread, mass, ref)), (b, i, h)
+
+
+def test_line_of_work_beyond_its_limit_is_refused():
+    """The documented bound on sequences x heads x query tiles x positions: refused on the host, before anything is launched."""
+    import ctypes as C
+    moa = _moa()
+    fake, lib = 0x10000, moa.load_library()
+    cache = moa.MoaPagedCache(fake, fake, 1024 * 8 * 64, fake, fake, None, None, None, 64, 1024, 9, 1024, 8, 64, 0)
+    call = lambda hq: lib.moa_paged_attention(C.byref(cache), fake, hq * 64, None, None, 0, 64, 64, hq, None, 0.0, fake, None, fake, 0, None)  # noqa: E731
+    assert call(8 * 128) == 2                    # 64 * 8 * (64 * 128 / 8) * (1024 * 1024 / 64) = 2^33: a shape
+    assert call(8 * 16) == 5                     # 2^30: accepted, and refused for its workspace of no bytes
