@@ -327,9 +327,9 @@ moa_status moa_paged_append(const moa_paged_cache *cache, const void *k_new, con
  * Scores, statistics and sums are fp32. bf16 values are multiplied by probabilities of two bf16 terms; calls of many query rows
  * (n > 1, more than 16 of them per key / value head, pages of at least 8 rows, and a cache with room for enough work, by its size
  * and not by the lengths) run on tensor memory and round each probability once to bf16, which puts an output off by at most 2^-8
- * of sum p |v|. A wait inside that kernel that runs out (about 2 s; it means a fault of the device) leaves NaN in the rows concerned: these
- * calls have no status word. hq / hkv <= 128; batch * hkv * (n * hq / hkv / 8, rounded up) * (max_pages * page_size / 64, rounded up)
- * <= 2^30. */
+ * of sum p |v|. A wait inside that kernel that runs out (about 2 s; it means a fault of the device) leaves NaN in the rows
+ * concerned: these calls have no status word. hq / hkv <= 128; batch * hkv * (n * hq / hkv / 8, rounded up) * (max_pages *
+ * page_size / 64, rounded up) <= 2^30. */
 moa_status moa_paged_workspace_bytes(const moa_paged_cache *cache, int32_t n, int32_t hq, int32_t weights, size_t *bytes);
 moa_status moa_paged_attention(const moa_paged_cache *cache, const void *q, int64_t q_stride, const void *k_new, const void *v_new,
                                int64_t new_stride, int32_t n, int32_t n_new, int32_t hq, const uint64_t *mask, float scale, void *out,
@@ -339,8 +339,8 @@ moa_status moa_paged_attention(const moa_paged_cache *cache, const void *q, int6
  * moa_verify_greedy writes them: the accepted rows' keys and values move to slots len[b] .. len[b] + acc_len[b] - 1, the
  * others are given up (n <= MOA_PAGED_MAX_ROWS; the listed slots rise). The pages of the n rows have to be in the table: of a
  * row on a missing page nothing is stored, so it cannot be kept; a listed row that comes from such a page leaves its new slot
- * as it was, one that goes to such a page is lost, and the other listed rows are kept all the same. advance != 0: len (and seen) grow by acc_len, or by
- * n when acc_len is NULL. With several layers that share len: the layers' calls without advance, then one with it. */
+ * as it was, one that goes to such a page is lost, and the other listed rows are kept all the same. advance != 0: len (and
+ * seen) grow by acc_len, or by n when acc_len is NULL. With several layers that share len: the layers' calls without advance, then one with it. */
 moa_status moa_paged_commit(const moa_paged_cache *cache, int32_t n, const int32_t *acc_slot, const int32_t *acc_len, int32_t cap,
                             int32_t advance, void *stream);
 

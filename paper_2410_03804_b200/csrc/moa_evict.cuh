@@ -15,7 +15,7 @@
 // GPU, since the heads of uneven sequences have uneven numbers of them. Measured, cluster / two kernels, us, heads of 2049 slots cut
 // to 2048: 8 heads 8.8 / 9.4, 16: 14.3 / 9.6, 32: 20.9 / 9.8, 64: 33 / 10.0, 128: 59 / 10.2; of 4096 cut to 2048: 8 heads 12.0 / 13.4,
 // 16: 21.7 / 15.9, 32: 35 / 20.5, 128: 109 / 37; of 32768 cut to 8192: 8 heads 85 / 91, 16: 165 / 101, 32: 248 / 120. The cluster wins
-// while all of them run at once: 14 heads 8.4 / 8.8, 12.0 / 15.1 and (20000 cut to 8192) 55 / 62, but 16 heads a second round, since
+// while all of them run at once: 14 heads 8.4 / 8.8, 12.0 / 15.1 and (20000 cut to 8192) 55 / 62, but 16 heads a second wave, since
 // a group of 16 to 20 SMs holds two clusters only. The rule is ten SMs a head.
 // Selection: exact, on 32-bit keys, by up to four passes of 8 bits that end early when a bin is kept whole; then one pass in
 // slot order lists sources and destinations.
