@@ -179,9 +179,9 @@ def _codes(x):
     """Blocks [..., 16, dh] in 8 bits: codes -127 .. 127 and a scale [...] for each."""
     x = x.float()
     top = x.abs().amax((-1, -2))
-    none = top < 2.0**-100
-    scale = torch.where(none, 0.0, top / 127.0)
-    r = torch.where(none, 0.0, 127.0 / top)
+    none, most = top < 2.0**-100, torch.full_like(top, 127.0)          # (divisions of tensors by tensors are rounded once, by numbers not)
+    scale = torch.where(none, 0.0, top / most)
+    r = torch.where(none, 0.0, most / top)
     return (x * r[..., None, None]).round().clamp(-127, 127), scale
 
 
