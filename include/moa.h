@@ -395,6 +395,113 @@ moa_status moa_verify_greedy_rules(const moa_logit_rule_set *rules, const int32_
                                    const void *target_logits, int32_t logits_dtype, int32_t vocab, int32_t cap, int32_t *choice,
                                    int32_t *acc_slot, int32_t *acc_tok, int32_t *acc_len, int32_t *next_tok, void *stream);
 
+/* ---------------------------------------------------------------------------------------------------------------
+ * Around the paged caches: who holds which page, what stands between a fused projection and the cache, and a cache in 8 bits.
+ * One step of a batch of requests:
+ *   moa_page_plan on the requests' lengths, then per LLM layer moa_qk_norm_rope (to a paged cache by the plan's slots, or to rows that
+ *   moa_paged_attention / moa_paged8_attention append), the attention, and later its commit
+ * What is said above of devices, streams, captured graphs and workspaces holds for these calls, too. */
+
+/* The pages of a pool and who holds them. The pool's pages may be those of many layers' caches, of the same table. */
+typedef struct {
+  int32_t *page_table; /* device int32 [batch, max_pages]: pages of each sequence; -1 behind the ones it holds */
+  int32_t *held;       /* device int32 [batch]: pages that it holds */
+  int32_t *free_pages; /* device int32 [n_pages]: a stack of free pages ... */
+  int32_t *free_count; /* device int32 [1]: ... and how many there are */
+  int32_t batch;       /* <= MOA_MAX_BATCH */
+  int32_t max_pages, n_pages;
+  int32_t page_size;   /* a power of two <= 1024; max_pages * page_size <= 2^30, n_pages <= 2^28 */
+} moa_page_pool;
+
+/* Gives every sequence the pages of its len[b] committed and n_new[b] new rows (device int32 [batch]; n_new NULL: one row each,
+ * negative: none), and lays the new rows out as one packed batch:
+ *   1. a sequence gives back the pages behind ceil((len + n_new) / page_size); one with len[b] < 0, which is not in use, all of them.
+ *      They go onto the stack in the order of sequences and pages.
+ *   2. in the order of sequences, those that need more pages than they hold take them from the stack's top. One whose pages are not
+ *      there gets none, and none behind it that needs any overtakes it; the sequences that need none go on. One that needs more
+ *      than max_pages never fits and keeps nobody waiting.
+ *   3. rows[b] = n_new[b] where the pages are there and the rows of all such sequences up to b fit max_rows, else 0 and no page is taken.
+ *      row_start[b] = sum of rows before b (device int32 [batch + 1])
+ *   4. per row r < max_rows: row_seq[r] its sequence, row_pos[r] its position seen[b] + i (seen NULL: len[b] + i), slot[r] its
+ *      place page * page_size + row in the pool (device int32 twice, int64); -1 in all three behind the last row, and a slot on a
+ *      page outside 0 .. n_pages-1 is -1. All three may be NULL: no maps, and no bound on the rows.
+ * pool_out (NULL: the pool itself) gets the pool as it is afterwards; with arrays of its own, all of them, a plan may be dropped.
+ * Entries of the table behind held are then -1 and the stack behind its count may hold anything. */
+moa_status moa_page_plan(const moa_page_pool *pool, const moa_page_pool *pool_out, const int32_t *len, const int32_t *n_new, const int32_t *seen,
+                         int32_t *rows, int32_t *row_start, int32_t *row_seq, int32_t *row_pos, int64_t *slot, int32_t max_rows, void *stream);
+
+/* Norm of each query and key head, rotation by the row's position, and the store of queries, keys and values, in one pass:
+ *   y = x / sqrt(mean(x^2) + eps) * gain (without gains: y = x), computed in fp32 and rounded once
+ *   pairs (a, b) of y's first rot_dim elements become (a cos - b sin, b cos + a sin), angle = pos * freq[pair], formed in 64 bits.
+ *   Pair i is (i, rot_dim / 2 + i), or (2 i, 2 i + 1) when interleaved. */
+typedef struct {
+  const void *q, *k, *v;        /* T [rows, hq or hkv, head_dim], rows q_stride / kv_stride elements apart (parts of a fused projection); v: with cache only */
+  int64_t q_stride, kv_stride;  /* multiples of 16 bytes, as the other strides */
+  const void *q_gain, *k_gain;  /* T [head_dim], both or neither (then no norm) */
+  const int32_t *pos;           /* device int32 [rows]; a row with pos < 0 is padding: nothing of it is read or written */
+  const double *freq;           /* device double [rot_dim / 2], radians per position */
+  void *q_out;                  /* T [rows, hq, head_dim], rows q_out_stride apart; may be q */
+  int64_t q_out_stride;
+  void *k_out;                  /* T [rows, hkv, head_dim], rows k_out_stride apart; may be k. NULL with cache */
+  int64_t k_out_stride;
+  const moa_paged_cache *cache; /* or NULL: keys and values go to slot[r] of its pages (moa_page_plan), outside of the pool: nowhere. Its */
+  const int64_t *slot;          /*   table, lengths, weights and positions are neither read nor written (so not for a cache that evicts) */
+  int32_t rows;                 /* <= 2^24 */
+  int32_t hq, hkv, head_dim;    /* head_dim 64 or 128, hq and hkv <= 1024 */
+  int32_t rot_dim;              /* a multiple of 16, <= head_dim; 0: no rotation */
+  int32_t interleaved;
+  int32_t dtype;                /* moa_dtype of all rows and gains */
+  float eps;
+} moa_qk_norm_rope_args;
+moa_status moa_qk_norm_rope(const moa_qk_norm_rope_args *args, void *stream);
+
+/* A paged cache in 8 bits, for bf16 rows. Every 16 slots of a sequence, from a multiple of 16 on, form a block. A block whose slots are
+ * all committed is closed: each head's keys, and its values, are held as codes -127 .. 127 times one scale,
+ *   scale = max|x| / 127,  code = round-half-even(x * (127 / max|x|)),  over the 16 rows of the head, in fp32
+ * (a block whose values are all below 2^-100 as zeros; one with a value that is not finite as NaN: who sees it gets NaN). The rows of the
+ * open block and the rows that are not committed lie in 16 bits in a ring, slot j in row j % MOA_PAGED8_RING. So a row is rounded once,
+ * and rows that are not accepted have no part in a scale.
+ * Table, len, unused sequences and missing pages are as in moa_paged_cache, with these differences: the slots of the ring need no
+ * page yet, and a block that is closed on a page that the table does not have is lost. There is no eviction.
+ * A closed block of a head is a record of 32 * head_dim + 16 bytes, all codes plus 128: key of token t, dim d at byte
+ * ((t % 2) * (head_dim / 64) + d / 64) * 512 + t / 2 * 64 + d % 64; value at 16 * head_dim + d / 32 * 512 + d % 8 * 64 + t / 4 * 16
+ * + d / 8 % 4 * 4 + t % 4; then the scales of keys and values (float) and 8 bytes that are not used. moa_paged8_read gives rows. */
+#define MOA_PAGED8_RING 80
+typedef struct {
+  void *pages;               /* device bytes [n_pages, hkv, page_size / 16, 32 * head_dim + 16]; page p starts page_stride * p bytes in */
+  int64_t page_stride;       /* bytes, a multiple of 16 */
+  void *k_ring, *v_ring;     /* device bf16 [batch, MOA_PAGED8_RING, hkv, head_dim] */
+  const int32_t *page_table; /* device int32 [batch, max_pages] */
+  int32_t *len;              /* device int32 [batch] */
+  int32_t *seen;             /* device int32 [batch], advanced with len, or NULL */
+  int32_t batch;             /* <= MOA_MAX_BATCH */
+  int32_t max_pages, n_pages;
+  int32_t page_size;         /* a power of two, 16 .. 1024; max_pages * page_size <= 2^30 */
+  int32_t hkv, head_dim;     /* head_dim 64 or 128 */
+} moa_paged_cache8;
+
+/* Appends rows i < n_new[b] (all n when n_new is NULL) of k_new, v_new bf16 [batch, n, hkv, head_dim] as committed rows at slots
+ * len[b] + i, closing the blocks that become whole: a prompt, of any length. advance != 0: len (and seen) grow. With several layers that
+ * share len: the layers' calls without advance, the last one with it. No uncommitted rows may be held: their places may be taken. */
+moa_status moa_paged8_append(const moa_paged_cache8 *cache, const void *k_new, const void *v_new, int64_t row_stride, int32_t n,
+                             const int32_t *n_new, int32_t advance, void *stream);
+/* moa_paged_attention over the 8-bit cache, without weights: the new rows are kept in the ring. Scores, statistics and sums are fp32. The
+ * codes enter the products exactly, the probabilities times the values' scales rounded once to fp16: each off by at most 2^-11 of itself,
+ * or, where that is less, 2^-29 of the largest probability times the largest scale. */
+moa_status moa_paged8_workspace_bytes(const moa_paged_cache8 *cache, int32_t n, int32_t hq, size_t *bytes);
+moa_status moa_paged8_attention(const moa_paged_cache8 *cache, const void *q, int64_t q_stride, const void *k_new, const void *v_new,
+                                int64_t new_stride, int32_t n, int32_t n_new, int32_t hq, const uint64_t *mask, float scale, void *out,
+                                void *ws, size_t ws_bytes, void *stream);
+/* moa_paged_commit for the 8-bit cache: the accepted rows (without acc_slot: the first acc_len[b], or n, of them) are kept, and the
+ * blocks that become whole are closed. n <= MOA_PAGED_MAX_ROWS. Has to follow every attention whose rows are kept, once per layer. */
+moa_status moa_paged8_commit(const moa_paged_cache8 *cache, int32_t n, const int32_t *acc_slot, const int32_t *acc_len, int32_t cap,
+                             int32_t advance, void *stream);
+/* Rows of slots first[b] + i, i < n (first NULL: 0) as they stand for, to k_out, v_out [batch, n, hkv, head_dim] of dtype: code * scale
+ * rounded once, or an open row; zeros where no row is (below slot 0, from length[b] on, on a missing page). length: device int32
+ * [batch] committed rows, NULL: the cache's len. Rows of a sequence that is not in use (by either) stay as they were. */
+moa_status moa_paged8_read(const moa_paged_cache8 *cache, int32_t n, const int32_t *first, const int32_t *length, void *k_out, void *v_out,
+                           int32_t dtype, void *stream);
+
 /* Reads back the device status word kept in st->tree (0 = no device-side problem seen). Synchronises the stream. */
 moa_status moa_state_status(moa_ctx *ctx, moa_state *st, void *stream);
 

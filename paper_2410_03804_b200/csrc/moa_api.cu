@@ -16,8 +16,11 @@
 #include "moa_codec.cuh"
 #include "moa_evict.cuh"
 #include "moa_paged.cuh"
+#include "moa_paged8.cuh"
 #include "moa_paged_tc.cuh"
 #include "moa_phases.cuh"
+#include "moa_plan.cuh"
+#include "moa_qknorm.cuh"
 #include "moa_rules.cuh"
 #include "moa_tree.cuh"
 #include "moa_verify.cuh"
@@ -1798,3 +1801,4 @@ moa_status moa_state_status(moa_ctx* ctx, moa_state* st, void* stream) {
 }  // extern "C"
 
 #include "moa_serving.inc"
+#include "moa_serving8.inc"

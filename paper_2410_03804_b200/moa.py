@@ -23,7 +23,8 @@ EXPORTS = ["moa_create", "moa_destroy", "moa_tli_configure", "moa_state_bytes", 
            "moa_state_set_len", "moa_lsa_forward", "moa_sa_append", "moa_sa_append_static", "moa_drafter_prefill", "moa_tree_begin", "moa_draft_step",
            "moa_tree_expand", "moa_tree_attn_mask", "moa_verify_greedy", "moa_pack_tree", "moa_unpack_tree", "moa_quantize_rows", "moa_dequantize_rows",
            "moa_paged_workspace_bytes", "moa_paged_append", "moa_paged_attention", "moa_paged_commit", "moa_paged_evict_workspace_bytes",
-           "moa_paged_evict", "moa_token_record", "moa_logit_rules", "moa_verify_greedy_rules", "moa_state_status", "moa_profile_begin", "moa_profile_end", "moa_profile_phases",
+           "moa_paged_evict", "moa_token_record", "moa_logit_rules", "moa_verify_greedy_rules", "moa_page_plan", "moa_qk_norm_rope", "moa_paged8_append",
+           "moa_paged8_workspace_bytes", "moa_paged8_attention", "moa_paged8_commit", "moa_paged8_read", "moa_state_status", "moa_profile_begin", "moa_profile_end", "moa_profile_phases",
            "moa_launch_count", "moa_trace_begin", "moa_trace_end"]
 
 
@@ -73,6 +74,24 @@ class MoaPagedCache(C.Structure):
     _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("page_stride", C.c_int64)] + [
         (n, C.c_void_p) for n in ("page_table", "len", "weight", "pos", "seen")] + [
         (n, C.c_int32) for n in ("batch", "max_pages", "n_pages", "page_size", "hkv", "head_dim", "dtype")]
+
+
+class MoaPagePool(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("page_table", "held", "free_pages", "free_count")] + [
+        (n, C.c_int32) for n in ("batch", "max_pages", "n_pages", "page_size")]
+
+
+class MoaQkNormRopeArgs(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("k", C.c_void_p), ("v", C.c_void_p), ("q_stride", C.c_int64), ("kv_stride", C.c_int64)] + [
+        (n, C.c_void_p) for n in ("q_gain", "k_gain", "pos", "freq", "q_out")] + [("q_out_stride", C.c_int64), ("k_out", C.c_void_p),
+        ("k_out_stride", C.c_int64), ("cache", C.c_void_p), ("slot", C.c_void_p)] + [
+        (n, C.c_int32) for n in ("rows", "hq", "hkv", "head_dim", "rot_dim", "interleaved", "dtype")] + [("eps", C.c_float)]
+
+
+class MoaPagedCache8(C.Structure):
+    _fields_ = [("pages", C.c_void_p), ("page_stride", C.c_int64)] + [
+        (n, C.c_void_p) for n in ("k_ring", "v_ring", "page_table", "len", "seen")] + [
+        (n, C.c_int32) for n in ("batch", "max_pages", "n_pages", "page_size", "hkv", "head_dim")]
 
 
 class MoaLogitRuleSet(C.Structure):
@@ -137,6 +156,13 @@ def load_library(rebuild_if_stale: bool = True) -> C.CDLL:
     lib.moa_paged_commit.argtypes = [vp, i32, vp, vp, i32, i32, vp]
     lib.moa_paged_evict_workspace_bytes.argtypes = [vp, i32, C.POINTER(sz)]
     lib.moa_paged_evict.argtypes = [vp, i32, i32, i32, vp, vp, vp, vp, sz, vp]
+    lib.moa_page_plan.argtypes = [vp] * 10 + [i32, vp]
+    lib.moa_qk_norm_rope.argtypes = [vp, vp]
+    lib.moa_paged8_append.argtypes = [vp, vp, vp, C.c_int64, i32, vp, i32, vp]
+    lib.moa_paged8_workspace_bytes.argtypes = [vp, i32, i32, C.POINTER(sz)]
+    lib.moa_paged8_attention.argtypes = [vp, vp, C.c_int64, vp, vp, C.c_int64, i32, i32, i32, vp, C.c_float, vp, vp, sz, vp]
+    lib.moa_paged8_commit.argtypes = [vp, i32, vp, vp, i32, i32, vp]
+    lib.moa_paged8_read.argtypes = [vp, i32, vp, vp, vp, vp, i32, vp]
     lib.moa_token_record.argtypes = [vp, vp, i32, i32, vp, vp, i32, vp]
     lib.moa_logit_rules.argtypes = [vp, vp, vp, i32, i32, vp, i32, i32, vp, vp, vp]
     lib.moa_verify_greedy_rules.argtypes = [vp, vp, vp, i32, i32, vp, i32, i32, i32, vp, vp, vp, vp, vp, vp]
@@ -277,6 +303,18 @@ def _made(make, stream):
         t = make()
     t.record_stream(torch.cuda.current_stream(t.device))       # where a result is read afterwards
     return t
+
+
+def _made_all(make, stream):
+    """_made for a tuple of tensors, or None among them."""
+    if stream is None:
+        return make()
+    with torch.cuda.stream(stream):
+        made = make()
+    for t in made:
+        if t is not None:
+            t.record_stream(torch.cuda.current_stream(t.device))
+    return made
 
 
 def _is(t: torch.Tensor, dtype, index: int) -> bool:
@@ -423,6 +461,228 @@ def moa_paged_evict(cache: PagedCache, budget: int, sink: int = 4, recent: int =
     ws = cache._own_scratch(ws, lambda: cache.evict_workspace(budget), stream)
     _serving_call(at, stream, load_library().moa_paged_evict, "moa_paged_evict", cache._ref, budget, sink, recent, w.data_ptr(), p.data_ptr(),
                   None if n is None else n.data_ptr(), ws.data_ptr(), ws.numel())
+
+
+class PagePool:
+    """The pages of a pool and who holds them (moa_page_pool of include/moa.h). page_table: cuda int32 [batch, max_pages]; held: int32
+    [batch]; free_pages: int32 [n_pages]; free_count: int32 [1]. The tensors are held, not copied."""
+
+    def __init__(self, page_table, held, free_pages, free_count, page_size: int):
+        assert page_table.is_cuda and page_table.dim() == 2, "page_table: cuda int32 [batch, max_pages]"
+        at, (batch, per) = page_table.get_device(), page_table.shape
+        assert _is(page_table, torch.int32, at) and per >= 1, "page_table: cuda int32 [batch, max_pages]"
+        assert _is(held, torch.int32, at) and held.shape == (batch,), "held: int32 [batch]"
+        assert _is(free_pages, torch.int32, at) and free_pages.dim() == 1 and free_pages.numel() >= 1, "free_pages: int32 [n_pages]"
+        assert _is(free_count, torch.int32, at) and free_count.numel() == 1, "free_count: int32 [1]"
+        self.page_table, self.held, self.free_pages, self.free_count = page_table, held, free_pages, free_count
+        self.index, self.device, self.batch, self.page_size = at, page_table.device, batch, page_size
+        self.shape = (batch, per, free_pages.numel(), page_size)
+        self.c = MoaPagePool(page_table.data_ptr(), held.data_ptr(), free_pages.data_ptr(), free_count.data_ptr(), *self.shape)
+        self._ref = C.addressof(self.c)
+
+    @classmethod
+    def make(cls, batch: int, max_pages: int, n_pages: int, page_size: int, device="cuda"):
+        """A pool of which nobody holds a page yet; page 0 is the first that is given."""
+        i32 = dict(dtype=torch.int32, device=device)
+        return cls(torch.full((batch, max_pages), -1, **i32), torch.zeros(batch, **i32), torch.arange(n_pages - 1, -1, -1, **i32),
+                   torch.full((1,), n_pages, **i32), page_size)
+
+
+def moa_page_plan(pool: PagePool, length: torch.Tensor, n_new=None, max_rows: int = 0, seen=None, pool_out=None, maps=None, stream=None):
+    """Gives the sequences the pages of their length[b] committed (< 0: not in use) and n_new[b] new rows (None: one each) and lays
+    the new rows out as one packed batch (see include/moa.h). pool_out: a pool of the same shape that gets the result; None: the
+    pool itself. Returns maps: (rows int32 [batch], row_start int32 [batch + 1], row_seq int32, row_pos int32, slot int64, each
+    [max_rows]); without max_rows the last three are None and the rows have no bound."""
+    at, b = pool.index, pool.batch
+    assert _is(length, torch.int32, at) and length.shape == (b,), "length: int32 [batch]"
+    assert n_new is None or (_is(n_new, torch.int32, at) and n_new.shape == (b,)), "n_new: int32 [batch]"
+    assert seen is None or (_is(seen, torch.int32, at) and seen.shape == (b,)), "seen: int32 [batch]"
+    assert pool_out is None or (pool_out.index == at and pool_out.shape == pool.shape), "pool_out: a pool of the same shape"
+    if maps is None:
+        new = lambda n, dt=torch.int32: torch.empty(n, dtype=dt, device=pool.device)  # noqa: E731
+        maps = _made_all(lambda: (new(b), new(b + 1)) + ((new(max_rows), new(max_rows), new(max_rows, torch.int64)) if max_rows > 0 else (None,) * 3), stream)
+    rows, start, seq, pos, slot = maps
+    assert _is(rows, torch.int32, at) and rows.shape == (b,) and _is(start, torch.int32, at) and start.shape == (b + 1,), "rows, row_start: int32 [batch], [batch + 1]"
+    n = 0
+    if slot is not None:
+        n = slot.numel()
+        assert _is(slot, torch.int64, at) and max_rows in (0, n), "slot: int64 [max_rows]"
+        assert _is(seq, torch.int32, at) and seq.numel() == n and _is(pos, torch.int32, at) and pos.numel() == n, "row_seq, row_pos: int32 [max_rows]"
+    else:
+        assert seq is None and pos is None and max_rows == 0, "row_seq, row_pos and slot come together"
+    p = lambda t: None if t is None else t.data_ptr()  # noqa: E731
+    _serving_call(at, stream, load_library().moa_page_plan, "moa_page_plan", pool._ref, None if pool_out is None else pool_out._ref, length.data_ptr(),
+                  p(n_new), p(seen), rows.data_ptr(), start.data_ptr(), p(seq), p(pos), p(slot), n)
+    return maps
+
+
+def _flat_rows(t: torch.Tensor, rows, heads, head_dim, dtype, index: int, what: str) -> int:
+    """Checks rows [rows, heads, head_dim] whose heads are contiguous; returns the elements between two rows."""
+    assert t.dim() == 3 and t.dtype is dtype and t.get_device() == index and t.shape == (rows, heads, head_dim), what
+    s0, s1, s2 = t.stride()
+    assert s2 == 1 and (s1 == head_dim or heads == 1), what + ": heads must be contiguous"
+    return s0 if rows > 1 else heads * head_dim
+
+
+def moa_qk_norm_rope(q: torch.Tensor, k: torch.Tensor, pos: torch.Tensor, freq=None, q_gain=None, k_gain=None, eps: float = 1e-5,
+                     interleaved: bool = False, q_out=None, k_out=None, cache=None, slot=None, v=None, stream=None):
+    """Norm (with gains [head_dim]) and rotation of q [rows, hq, head_dim] and k [rows, hkv, head_dim], parts of a fused projection as a
+    rule. pos: int32 [rows], < 0 for padding; freq: float64 [rot_dim / 2], radians per position (None: no rotation). The results
+    go to q_out and k_out (which may be q and k; None: new ones), or, with a PagedCache and slot int64 [rows] (moa_page_plan), keys
+    and values v to the cache's pages. Returns (q_out, k_out), k_out None with a cache."""
+    assert q.is_cuda and q.dim() == 3 and q.dtype in (torch.float32, torch.bfloat16), "q: cuda [rows, hq, head_dim]"
+    at, dt, (rows, hq, dh) = q.get_device(), q.dtype, q.shape
+    assert k.dim() == 3 and rows >= 1, "k: [rows, hkv, head_dim]"
+    hkv = k.shape[1]
+    qs, ks = _flat_rows(q, rows, hq, dh, dt, at, "q"), _flat_rows(k, rows, hkv, dh, dt, at, "k")
+    assert _is(pos, torch.int32, at) and pos.shape == (rows,), "pos: int32 [rows]"
+    assert freq is None or (_is(freq, torch.float64, at) and freq.dim() == 1), "freq: float64 [rot_dim / 2]"
+    assert (q_gain is None) == (k_gain is None), "q_gain and k_gain come together"
+    for g in (q_gain, k_gain):
+        assert g is None or (_is(g, dt, at) and g.shape == (dh,)), "gains: as the rows, [head_dim]"
+    # with padding some rows of a new tensor are not written
+    if q_out is None:
+        q_out = _made(lambda: torch.zeros((rows, hq, dh), dtype=dt, device=q.device), stream)
+    qo, ko, vp, sp, cp = _flat_rows(q_out, rows, hq, dh, dt, at, "q_out"), 0, None, None, None
+    if cache is None:
+        assert slot is None and v is None, "slot and v belong to a cache"
+        if k_out is None:
+            k_out = _made(lambda: torch.zeros((rows, hkv, dh), dtype=dt, device=q.device), stream)
+        ko = _flat_rows(k_out, rows, hkv, dh, dt, at, "k_out")
+    else:
+        assert k_out is None and v is not None and slot is not None, "a cache needs v and slot, and takes the place of k_out"
+        assert cache.index == at and cache.dtype is dt and cache.hkv == hkv and cache.head_dim == dh, "the cache is of another kind of rows"
+        assert _flat_rows(v, rows, hkv, dh, dt, at, "v") == ks, "v must be laid out as k"
+        assert _is(slot, torch.int64, at) and slot.shape == (rows,), "slot: int64 [rows]"
+        vp, sp, cp = v.data_ptr(), slot.data_ptr(), cache._ref
+    a = MoaQkNormRopeArgs(q.data_ptr(), k.data_ptr(), vp, qs, ks, None if q_gain is None else q_gain.data_ptr(),
+                          None if k_gain is None else k_gain.data_ptr(), pos.data_ptr(), None if freq is None else freq.data_ptr(), q_out.data_ptr(), qo,
+                          None if k_out is None else k_out.data_ptr(), ko, cp, sp, rows, hq, hkv, dh, 0 if freq is None else 2 * freq.numel(),
+                          1 if interleaved else 0, 0 if dt is torch.float32 else 1, eps)
+    _serving_call(at, stream, load_library().moa_qk_norm_rope, "moa_qk_norm_rope", C.addressof(a))
+    return q_out, k_out
+
+
+PAGED8_BLOCK, PAGED8_RING = 16, 80
+
+
+class PagedCache8:
+    """A paged key / value cache in 8 bits for bf16 rows (moa_paged_cache8 of include/moa.h). pages: cuda uint8 [n_pages, hkv,
+    page_size / 16, 32 * head_dim + 16], contiguous within a page; k_ring, v_ring: bfloat16 [batch, 80, hkv, head_dim]; page_table:
+    int32 [batch, max_pages]; length: int32 [batch], committed slots, < 0 for a sequence not in use; seen: int32 [batch], advanced
+    with length, or None. The tensors are held, not copied; the caller (or moa_page_plan) fills the table."""
+
+    def __init__(self, pages, k_ring, v_ring, page_table, length, page_size: int, seen=None):
+        assert pages.is_cuda and pages.dim() == 4 and pages.dtype is torch.uint8, "pages: cuda uint8 [n_pages, hkv, page_size / 16, 32 * head_dim + 16]"
+        at, (n_pages, hkv, blocks, rec) = pages.get_device(), pages.shape
+        assert k_ring.dim() == 4 and _is(k_ring, torch.bfloat16, at), "k_ring: bfloat16 [batch, 80, hkv, head_dim]"
+        batch, dh = k_ring.shape[0], k_ring.shape[3]
+        assert k_ring.shape == (batch, PAGED8_RING, hkv, dh) and _is(v_ring, torch.bfloat16, at) and v_ring.shape == k_ring.shape, "k_ring, v_ring: bfloat16 [batch, 80, hkv, head_dim]"
+        assert rec == 32 * dh + 16 and blocks * PAGED8_BLOCK == page_size, "pages: cuda uint8 [n_pages, hkv, page_size / 16, 32 * head_dim + 16]"
+        assert pages[0].is_contiguous(), "a page must be contiguous"
+        assert _is(page_table, torch.int32, at) and page_table.dim() == 2 and page_table.shape[0] == batch and page_table.shape[1] >= 1, "page_table: int32 [batch, max_pages]"
+        for t in (length, seen):
+            assert t is None or (_is(t, torch.int32, at) and t.shape == (batch,)), "length, seen: int32 [batch]"
+        per = page_table.shape[1]
+        self.pages, self.k_ring, self.v_ring, self.page_table, self.len, self.seen = pages, k_ring, v_ring, page_table, length, seen
+        self.device, self.index, self.batch, self.hkv, self.head_dim, self.slots = pages.device, at, batch, hkv, dh, per * page_size
+        self.c = MoaPagedCache8(pages.data_ptr(), pages.stride(0) if n_pages > 1 else hkv * blocks * rec, k_ring.data_ptr(), v_ring.data_ptr(),
+                                page_table.data_ptr(), length.data_ptr(), None if seen is None else seen.data_ptr(), batch, per, n_pages, page_size, hkv, dh)
+        self._ref = C.addressof(self.c)
+
+    @classmethod
+    def make(cls, page_table, length, n_pages: int, page_size: int, hkv: int, head_dim: int, seen=None):
+        """An empty cache over a page table."""
+        dev = page_table.device
+        ring = lambda: torch.zeros((page_table.shape[0], PAGED8_RING, hkv, head_dim), dtype=torch.bfloat16, device=dev)  # noqa: E731
+        return cls(torch.empty((n_pages, hkv, page_size // PAGED8_BLOCK, 32 * head_dim + 16), dtype=torch.uint8, device=dev), ring(), ring(), page_table,
+                   length, page_size, seen)
+
+    def workspace(self, n: int, hq: int) -> torch.Tensor:
+        """Scratch for moa_paged8_attention with n rows per sequence and hq query heads (zeroed, as its first call needs it)."""
+        size, lib = C.c_size_t(), load_library()
+        with torch.cuda.device(self.device):
+            _check(lib.moa_paged8_workspace_bytes(self._ref, n, hq, C.byref(size)), "moa_paged8_workspace_bytes")
+            return torch.zeros(size.value, dtype=torch.uint8, device=self.device)
+
+
+def _new_rows8(cache: PagedCache8, k_new, v_new):
+    at, b, hkv, dh = cache.index, cache.batch, cache.hkv, cache.head_dim
+    n, step = _rows(k_new, b, hkv, dh, torch.bfloat16, at, "k_new")
+    assert _rows(v_new, b, hkv, dh, torch.bfloat16, at, "v_new") == (n, step), "v_new must be laid out as k_new"
+    return n, step
+
+
+def moa_paged8_append(cache: PagedCache8, k_new: torch.Tensor, v_new: torch.Tensor, n_new=None, advance: bool = True, stream=None):
+    """Appends rows bfloat16 [batch, n, hkv, head_dim] (the first n_new[b] of each sequence) as committed rows, closing the blocks
+    that become whole; cache.len (and seen) grow when asked to."""
+    at = cache.index
+    n, step = _new_rows8(cache, k_new, v_new)
+    assert n_new is None or (_is(n_new, torch.int32, at) and n_new.shape == (cache.batch,)), "n_new: int32 [batch]"
+    _serving_call(at, stream, load_library().moa_paged8_append, "moa_paged8_append", cache._ref, k_new.data_ptr(), v_new.data_ptr(), step, n,
+                  None if n_new is None else n_new.data_ptr(), 1 if advance else 0)
+
+
+def moa_paged8_attention(cache: PagedCache8, q: torch.Tensor, k_new=None, v_new=None, mask=None, scale: float = 0.0, new_rows: bool = True,
+                         out=None, ws=None, stream=None) -> torch.Tensor:
+    """moa_paged_attention over an 8-bit cache: q [batch, n, hq, head_dim], k_new, v_new [batch, n, hkv, head_dim] (kept in the ring by
+    the call; None: they are there already; new_rows=False: there are none), mask int64 [batch, n], None: causal. Returns out."""
+    at, b, hkv, dh, dt = cache.index, cache.batch, cache.hkv, cache.head_dim, torch.bfloat16
+    assert q.dim() == 4, "q: [batch, n, hq, head_dim]"
+    hq = q.shape[2]
+    n, q_step = _rows(q, b, hq, dh, dt, at, "q")
+    kp = vp = mp = None
+    new_step = 0
+    assert (k_new is None) == (v_new is None), "k_new and v_new come together"
+    if k_new is not None:
+        assert new_rows, "k_new and v_new are new rows"
+        m, new_step = _new_rows8(cache, k_new, v_new)
+        assert m == n, "k_new: with q's rows"
+        kp, vp = k_new.data_ptr(), v_new.data_ptr()
+    if mask is not None:
+        assert (_is(mask, torch.int64, at) or _is(mask, torch.uint64, at)) and mask.numel() == b * n, "mask: int64 [batch, n]"
+        mp = mask.data_ptr()
+    if out is None:
+        out = _made(lambda: torch.empty((b, n, hq, dh), dtype=dt, device=cache.device), stream)
+    else:
+        assert _is(out, dt, at) and out.shape == q.shape, "out: [batch, n, hq, head_dim]"
+    if ws is None:
+        ws = _made(lambda: cache.workspace(n, hq), stream)
+    assert _is(ws, torch.uint8, at), "ws: cuda uint8, contiguous"
+    _serving_call(at, stream, load_library().moa_paged8_attention, "moa_paged8_attention", cache._ref, q.data_ptr(), q_step, kp, vp, new_step, n,
+                  n if new_rows else 0, hq, mp, scale, out.data_ptr(), ws.data_ptr(), ws.numel())
+    return out
+
+
+def moa_paged8_commit(cache: PagedCache8, n: int, acc_slot=None, acc_len=None, advance: bool = True, stream=None):
+    """Keeps the accepted path (acc_slot [batch, cap], acc_len [batch] of moa_verify_greedy) of n uncommitted rows, or the first
+    acc_len (or all) of them, closes the blocks that become whole and advances cache.len (and seen) when asked to."""
+    at, cap = cache.index, 0
+    assert acc_len is None or (_is(acc_len, torch.int32, at) and acc_len.shape == (cache.batch,)), "acc_len: int32 [batch]"
+    if acc_slot is not None:
+        assert acc_len is not None and _is(acc_slot, torch.int32, at) and acc_slot.dim() == 2, "acc_slot: int32 [batch, cap]"
+        b, cap = acc_slot.shape
+        assert b == cache.batch, "acc_slot: int32 [batch, cap]"
+    _serving_call(at, stream, load_library().moa_paged8_commit, "moa_paged8_commit", cache._ref, n, None if acc_slot is None else acc_slot.data_ptr(),
+                  None if acc_len is None else acc_len.data_ptr(), cap, 1 if advance else 0)
+
+
+def moa_paged8_read(cache: PagedCache8, n: int, first=None, length=None, dtype=torch.bfloat16, out=None, stream=None):
+    """Rows of slots first[b] .. first[b] + n - 1 (first None: from 0) as they stand for; zeros where no row is. length: int32 [batch],
+    committed rows, None: cache.len. Returns (k, v) [batch, n, hkv, head_dim] of dtype (or of out's)."""
+    at, shape = cache.index, (cache.batch, n, cache.hkv, cache.head_dim)
+    for t in (first, length):
+        assert t is None or (_is(t, torch.int32, at) and t.shape == (cache.batch,)), "first, length: int32 [batch]"
+    if out is None:
+        # rows of a sequence that is not in use are not written
+        out = _made_all(lambda: tuple(torch.zeros(shape, dtype=dtype, device=cache.device) for _ in range(2)), stream)
+    k, v = out
+    assert k.dtype in (torch.float32, torch.bfloat16), "out: float32 or bfloat16"
+    for t in out:
+        assert _is(t, k.dtype, at) and t.shape == shape, "out: [batch, n, hkv, head_dim], both of a type"
+    _serving_call(at, stream, load_library().moa_paged8_read, "moa_paged8_read", cache._ref, n, None if first is None else first.data_ptr(),
+                  None if length is None else length.data_ptr(), k.data_ptr(), v.data_ptr(), 0 if k.dtype is torch.float32 else 1)
+    return k, v
 
 
 class LogitRules:
