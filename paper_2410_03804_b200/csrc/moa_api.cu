@@ -17,6 +17,7 @@
 #include "moa_evict.cuh"
 #include "moa_paged.cuh"
 #include "moa_paged8.cuh"
+#include "moa_paged8_tc.cuh"
 #include "moa_paged_tc.cuh"
 #include "moa_phases.cuh"
 #include "moa_plan.cuh"

@@ -45,6 +45,7 @@ struct Paged8 {
   PagedAttn a;                               // a.c.k, a.c.v: the rings, bf16 [batch, P8_RING, hkv, DH]; its pages and weights are not used
   const uint8_t* pages;                      // [n_pages, hkv, page_size / 16] records, pages page_bytes apart
   long long page_bytes;
+  uint8_t* open;                             // open blocks as the tree kernel wants them (moa_paged8_tc.cuh)
 };
 
 // The record of block blk of (sequence, head), or null where the table has no such page.
@@ -183,31 +184,6 @@ __global__ void __launch_bounds__(256) paged8_append_kernel(const PagedView C, u
         reinterpret_cast<uint4*>((bf16*)(kv ? C.v : C.k) + p8_ring_row(C, b, slot, h, DH))[p] = x;
       }
     }
-  }
-}
-
-// New rows to their places in the ring, without closing anything; with mask [batch, n] only those that some row sees.
-template <int DH>
-__global__ void __launch_bounds__(256) paged8_ring_kernel(const PagedView C, const bf16* k_new, const bf16* v_new, long long row_stride, int n,
-                                                          const unsigned long long* mask) {
-  pdl_trigger();
-  pdl_wait(KID_APPEND);
-  constexpr int PIECES = DH / 8;
-  const int b = blockIdx.y, per = C.hkv * PIECES;
-  const int len = C.len[b];
-  if (len < 0) return;
-  unsigned long long any = ~0ull;
-  if (mask) {                                                        // n <= 64
-    any = 0ull;
-    for (int i = 0; i < n; ++i) any |= mask[(size_t)b * n + i];
-  }
-  for (int i = blockIdx.x * blockDim.x + threadIdx.x; i < n * per; i += gridDim.x * blockDim.x) {
-    const int r = i / per, c = i - r * per;
-    if (!((any >> r) & 1ull) || (long long)len + r >= C.cap()) continue;
-    const size_t to = p8_ring_row(C, b, len + r, 0, DH) / 8 + c;
-    const long long from = ((long long)b * n + r) * row_stride;
-    reinterpret_cast<uint4*>(C.k)[to] = __ldcg(reinterpret_cast<const uint4*>(k_new + from) + c);
-    reinterpret_cast<uint4*>(C.v)[to] = __ldcg(reinterpret_cast<const uint4*>(v_new + from) + c);
   }
 }
 

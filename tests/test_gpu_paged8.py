@@ -269,9 +269,11 @@ def test_one_token(dh, hq, hkv, page, lens):
     (64, 4, 4, 16, [5], 2), (128, 8, 2, 16, [100, 15], 3), (128, 8, 4, 32, [16, -1, 47, 0], 17), (128, 16, 4, 16, [333, 40], 61),
     (64, 8, 1, 64, [1000], 64), (128, 8, 1, 128, [1, 255, 511], 64), (128, 64, 8, 64, [600], 61), (64, 6, 2, 16, [79, 80, 81], 33)])
 @pytest.mark.parametrize("masked", [False, True])
-def test_rows_of_trees(dh, hq, hkv, page, lens, n, masked):
+@pytest.mark.parametrize("room", [64, 20000])
+def test_rows_of_trees(dh, hq, hkv, page, lens, n, masked, room):
+    """room: slots behind the longest sequence. The kernel is chosen by the size of the cache, so both are met at all lengths."""
     rng = np.random.default_rng(n + dh + hq)
-    m = Model(rng, lens, hkv, dh, page)
+    m = Model(rng, lens, hkv, dh, page, extra=room)
     mask = _tree(rng, m.batch, n, empty=n // 5) if masked else None
     q, k, v = _new_rows(m, n, hq)
     if masked:                                                               # rows that nobody sees may hold anything
@@ -294,7 +296,7 @@ def test_rows_of_trees(dh, hq, hkv, page, lens, n, masked):
 
 
 def test_committed_slots_only():
-    m = Model(np.random.default_rng(8), [0, 40, 300], 2, 128, 32)
+    m = Model(np.random.default_rng(8), [0, 40, 300], 2, 128, 32, extra=10000)
     for n in (1, 5, 61):
         q = _new_rows(m, n, 8)[0]
         out = _moa().moa_paged8_attention(m.c, q, new_rows=False)
@@ -303,7 +305,7 @@ def test_committed_slots_only():
 
 @pytest.mark.parametrize("n", [1, 40])
 def test_missing_pages_are_left_out(n):
-    m = Model(np.random.default_rng(9), [400, 250], 2, 128, 32)
+    m = Model(np.random.default_rng(9), [400, 250], 2, 128, 32, extra=10000)
     m.c.page_table[0, 3], m.c.page_table[0, 0], m.c.page_table[1, 1] = -1, m.c.pages.shape[0], 1 << 30
     missing = [(0, 6), (0, 7), (0, 0), (0, 1), (1, 2), (1, 3)]
     q, k, v = _new_rows(m, n, 16)
@@ -317,9 +319,10 @@ def test_missing_pages_are_left_out(n):
 @pytest.mark.parametrize("n", [1, 61])
 def test_slots_end_with_the_table(n):
     """New rows behind the last slot are neither kept nor seen."""
-    m = Model(np.random.default_rng(10), [94, 96], 2, 64, 32, extra=0)
+    hkv = 2 if n == 1 else 8
+    m = Model(np.random.default_rng(10), [94, 96], hkv, 64, 32, extra=0)
     assert m.c.slots == 96
-    q, k, v = _new_rows(m, n, 32)
+    q, k, v = _new_rows(m, n, 16 * hkv)
     out = _moa().moa_paged8_attention(m.c, q, k, v)
     _check_attention(m, q, k, v, None, out, n)
     _moa().moa_paged8_commit(m.c, n)
@@ -331,7 +334,7 @@ def test_slots_end_with_the_table(n):
 @pytest.mark.parametrize("n", [1, 61])
 @pytest.mark.parametrize("size,scale", [(60.0, None), (1e-3, 4.0), (1.0, 1e-6), (3e4, 1e-3), (1e30, 1e-30), (1e-30, 1e30)])
 def test_steep_flat_large_and_small_scores(n, size, scale):
-    m = Model(np.random.default_rng(11), [700, 33], 2, 128, 16)
+    m = Model(np.random.default_rng(11), [700, 33], 2, 128, 16, extra=64 if n == 1 else 9000)
     q, k, v = _new_rows(m, n, 16, scale=size)
     out = _moa().moa_paged8_attention(m.c, q, k, v, scale=scale or 0.0)
     _check_attention(m, q, k, v, None, out, n, scale=scale)
@@ -339,7 +342,7 @@ def test_steep_flat_large_and_small_scores(n, size, scale):
 
 @pytest.mark.parametrize("n", [1, 61])
 def test_blocks_of_very_different_scales(n):
-    m = Model(np.random.default_rng(12), [0], 2, 128, 16, extra=600)
+    m = Model(np.random.default_rng(12), [0], 2, 128, 16, extra=600 if n == 1 else 9000)
     k, v = m.fresh(400), m.fresh(400)
     for j in range(0, 400, 16):
         v[0, j:j + 16] *= 2.0 ** float(m.rng.integers(-30, 30))
@@ -357,7 +360,7 @@ def test_blocks_of_very_different_scales(n):
 @pytest.mark.parametrize("size", [2.0**-60, 2.0**60])
 @pytest.mark.parametrize("n", [1, 61])
 def test_values_far_from_one(n, size):
-    m = Model(np.random.default_rng(13), [0, 0], 1, 64, 16, extra=600)
+    m = Model(np.random.default_rng(13), [0, 0], 1, 64, 16, extra=600 if n == 1 else 9000)
     m.append(m.fresh(300), m.fresh(300, size), [300, 170])
     q, kn, vn = _new_rows(m, n, 8)
     vn *= size
@@ -365,11 +368,11 @@ def test_values_far_from_one(n, size):
     _check_attention(m, q, kn, vn, None, out, n)
 
 
-@pytest.mark.parametrize("hq", [2, 16])
-def test_unfinite_new_values_reach_only_the_rows_that_see_them(hq):
+@pytest.mark.parametrize("hq,room", [(2, 64), (16, 64), (16, 9000)])
+def test_unfinite_new_values_reach_only_the_rows_that_see_them(hq, room):
     rng = np.random.default_rng(14)
     n = 40
-    m = Model(rng, [200, 31], 2, 128, 16)
+    m = Model(rng, [200, 31], 2, 128, 16, extra=room)
     mask = _tree(rng, 2, n)
     q, k, v = _new_rows(m, n, hq)
     v[0, 20, 1, 3], v[1, 7, 0, 100], k[1, 11, 1, 0] = float("inf"), NAN, NAN
@@ -400,8 +403,9 @@ def test_unfinite_new_values_reach_only_the_rows_that_see_them(hq):
     assert torch.equal(torch.where(same, fresh, seen), fresh)
 
 
-def test_a_closed_block_with_a_nan_is_nan_for_its_head_only():
-    m = Model(np.random.default_rng(15), [0], 2, 64, 16)
+@pytest.mark.parametrize("room", [128, 40000])
+def test_a_closed_block_with_a_nan_is_nan_for_its_head_only(room):
+    m = Model(np.random.default_rng(15), [0], 2, 64, 16, extra=room)
     k, v = m.fresh(64), m.fresh(64)
     v[0, 20, 1, 0] = NAN
     m.append(k, v, [64])
@@ -417,8 +421,9 @@ def test_a_closed_block_with_a_nan_is_nan_for_its_head_only():
             assert not out[:, n - 1].any()                                   # sees nothing
 
 
-def test_a_query_that_is_not_finite_spoils_its_own_row_only():
-    m = Model(np.random.default_rng(16), [200], 2, 128, 16)
+@pytest.mark.parametrize("room", [128, 40000])
+def test_a_query_that_is_not_finite_spoils_its_own_row_only(room):
+    m = Model(np.random.default_rng(16), [200], 2, 128, 16, extra=room)
     for n in (1, 61):
         q, k, v = _new_rows(m, n, 8)
         q[0, 0, 1, 5] = float("inf")
@@ -432,7 +437,7 @@ def test_a_query_that_is_not_finite_spoils_its_own_row_only():
 @pytest.mark.parametrize("dh,hq,hkv,page,lens,n", [(128, 8, 2, 16, [10, 77, -1, 0], 13), (64, 16, 2, 32, [64, 15], 61), (128, 32, 8, 64, [200, 201], 64)])
 def test_draft_verify_commit_cycles(dh, hq, hkv, page, lens, n):
     rng = np.random.default_rng(n)
-    m = Model(rng, lens, hkv, dh, page, extra=400)
+    m = Model(rng, lens, hkv, dh, page, extra=400 if n < 60 else 6000)
     ws = m.c.workspace(n, hq)
     for cycle in range(5):
         mask = _tree(rng, m.batch, n)
@@ -491,7 +496,7 @@ def test_captured_decode_follows_the_lengths():
 
 
 def test_calls_on_a_stream_of_their_own():
-    m = Model(np.random.default_rng(19), [300], 2, 128, 16)
+    m = Model(np.random.default_rng(19), [300], 2, 128, 16, extra=9000)
     n = 40
     q, k, v = _new_rows(m, n, 16)
     want = _moa().moa_paged8_attention(m.c, q, k, v)
