@@ -16,12 +16,12 @@
 // multiply-add, and of the maximum of the 16 scores; the values' scale, relative to a power of two above all that the item has met,
 // is a term of its addend, 2^(x + log2 r) = r 2^x, and is divided out of the 16 probabilities' sum again.
 // The probabilities are rounded once to fp16 (2^-11 of themselves), a quarter of the outputs' own rounding to bf16.
-// Measured: 16 sequences x 61 rows x 64 heads over 4090 positions, with the commit: 279 us (the row kernel: 1466); 61 rows x 32 heads over
-// 2045: 42.8 us. A block takes some 5300 cycles: 650 for the maxima, 1700 for the probabilities, 850 until a tile's four warps have
-// them, 1900 for the two products that follow and the other tile's between them. What it took to get there: the
-// masks out of the softmax's loop (350 from 380 us), the operands' work without spills and with addresses that
-// are constants apart (7000 to 2000 cycles), the open slots' work in a kernel of its own (420 to 300 us: here it ran cold, once per
-// item, for 100000 cycles), the queries' scaling in a loop (20000 to 9000 cycles a start).
+// A tile's first 64 probabilities are handed over while the other 64 are made, so half of their product is done when those come.
+// Measured: 16 sequences x 61 rows x 64 heads over 4090 positions: 208 us, with the commit 216 (the row kernel: 1466); 61 rows x 32 heads
+// over 2045: 31.7 and 36.4. What it took to get there, us of the large case: the masks out of the softmax's loop (380 to 350), operands' addresses that are constants apart and their registers
+// not live across a call (to 300 with the next), the open slots' work in a kernel of its own (here it ran cold, once per item, for
+// 100000 cycles), loops in place of unrolled halves (263 to 210: a quarter of the instruction cache's requests had missed; 8 % do now,
+// the rest of the kernel's 98 KB), probabilities in two halves (212 to 208).
 // Every wait is bounded; a CTA whose wait ran out writes NaN to its rows (the serving calls have no status word).
 #pragma once
 #include "moa_paged8.cuh"
@@ -30,6 +30,7 @@
 namespace moa {
 
 constexpr int P8T_THREADS = 512;
+constexpr int P8T_AT = 32;                   // scores that the softmax's loops take at a time: 32 or 64
 constexpr int P8T_TABLE_WARP = 9, P8T_CONV_WARP = 10;
 
 struct P8Table {                             // of one block of 128 positions: per 16 of them
@@ -46,18 +47,38 @@ template <int DH> struct P8tCfg {
   static constexpr int QCHUNK = 128 * 128, KCHUNK = PT_KB * 128, VCHUNK = DH * 128;          // 64 columns: of queries, of keys; 64 positions of values
   static constexpr int REC = P8Cfg<DH>::REC;
   static constexpr int O_K = 2 * QTILE, O_V = O_K + 2 * KTILE, O_TAB = O_V + 2 * KTILE;          // two of keys, two of values
-  static constexpr int O_DOWN = O_TAB + 4 * (int)sizeof(P8Table), O_BAR = O_DOWN + 256 * 4;
+  static constexpr int O_BAR = O_TAB + 4 * (int)sizeof(P8Table);
   static constexpr int SMEM = O_BAR + 256 + 1024;
 };
 
 __host__ __device__ constexpr uint32_t umma_idesc_f16(int m, int n) { return (1u << 4) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24); }
 
+// 32 consecutive columns of this thread's lane in one instruction
+__device__ __forceinline__ void tc_ld32(uint32_t taddr, float* v) {
+  uint32_t r[32];
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
+        "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]),
+        "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]),
+        "=r"(r[31])
+      : "r"(taddr));
+  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+  for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
+}
 // Four codes (plus 128) of a word as fp16, in order.
 __device__ __forceinline__ uint2 p8_codes_in_order(uint32_t w) {
   const uint32_t a = __byte_perm(w, 0x64646464u, 0x4140), b = __byte_perm(w, 0x64646464u, 0x4342);
   const __half2 bias = __half2half2(__ushort_as_half(0x6480));
   const __half2 x = __hsub2(*reinterpret_cast<const __half2*>(&a), bias), y = __hsub2(*reinterpret_cast<const __half2*>(&b), bias);
   return make_uint2(*reinterpret_cast<const uint32_t*>(&x), *reinterpret_cast<const uint32_t*>(&y));
+}
+template <int N>
+__device__ __forceinline__ void p8t_ld(uint32_t taddr, float* v) {
+  if constexpr (N == 64) tc_ld64(taddr, v); else tc_ld32(taddr, v);
 }
 // Barrier over three converting warps that also ORs a flag: who gives up takes all of them along.
 template <int ID>
@@ -139,13 +160,13 @@ struct P8Convert {
       else store_keys(to + (r >> 1) * C::KCHUNK + j * 2048, to_keys(r & 1, 0), to_keys(r & 1, 1), c[r]);
     }
   }
-  // block j from an open block's record, or zeros without one
+  // block j from an open block's record
   template <bool VALUES>
   static __device__ __forceinline__ void copy(uint8_t* to, int j, const uint8_t* open) {
     uint4 c[DH / 16];
 #pragma unroll
     for (int u = 0; u < DH / 16; ++u)
-      c[u] = open ? __ldcg(reinterpret_cast<const uint4*>(open + (VALUES ? 32 * DH : 0)) + u * 32 + (threadIdx.x & 31)) : make_uint4(0u, 0u, 0u, 0u);
+      c[u] = __ldcg(reinterpret_cast<const uint4*>(open + (VALUES ? 32 * DH : 0)) + u * 32 + (threadIdx.x & 31));
 #pragma unroll
     for (int u = 0; u < DH / 16; ++u) {
       const int i = u * 32 + (threadIdx.x & 31);
@@ -253,20 +274,22 @@ __global__ void __launch_bounds__(64) paged8_open_kernel(const Paged8 PP, uint8_
   }
 }
 
-// The operand of a block of 128 positions with blocks of 16 that are open, behind the end, or on pages that the table does not have.
+// The operand of a block of 128 positions with blocks of 16 that are open, behind the end, or on pages that the table does not have. The
+// latter two keep what was there: their scores are masked, and zero times a finite value is zero.
 template <int DH, bool VALUES>
-__device__ __noinline__ void p8t_ragged(const Paged8& PP, int b, int h, int blk0, unsigned there, int len, int keys, uint8_t* to, int cw) {
+__device__ __noinline__ void p8t_ragged(const Paged8& PP, int b, int h, int blk0, const uint8_t* rec, int len, int keys, uint8_t* to, int cw) {
   using X = P8Convert<DH>;
   const PagedAttn& P = PP.a;
 #pragma unroll 1
   for (int j = cw; j < 8; j += 3) {
     const int blk = blk0 + j, i = blk - (len >> 4);
-    if ((there >> j) & 1u) {
+    const uint8_t* from = (const uint8_t*)__shfl_sync(0xffffffffu, (unsigned long long)rec, j);
+    if (from) {
       uint4 c[X::UNITS];
-      X::template load<VALUES>(c, p8_record<DH>(P.c, PP.pages, PP.page_bytes, b, h, blk));
+      X::template load<VALUES>(c, from);
       X::template store<VALUES>(to, j, c);
-    } else {
-      X::template copy<VALUES>(to, j, i >= 0 && blk * 16 < keys ? P8Open<DH>::at(PP.open, P.c, b, h, i) : nullptr);
+    } else if (i >= 0 && blk * 16 < keys) {
+      X::template copy<VALUES>(to, j, P8Open<DH>::at(PP.open, P.c, b, h, i));
     }
   }
 }
@@ -349,7 +372,7 @@ __device__ __forceinline__ void p8t_operands(const Paged8& PP, const PagedLine& 
     const int len = min(L.len[W.b], cap), keys = min(len + P.n_new, cap), shut = len >> 4;
     uint4 c[3][X::UNITS];                    // blocks cw, cw + 3 and cw + 6 of 16 positions
     unsigned there = 0u;
-    const uint8_t* rec = nullptr;            // a record per lane, looked up a block ahead of its loads
+    const uint8_t *rec = nullptr, *last = nullptr;                   // a record per lane, looked up a block ahead of its loads; the loaded block's
     if (lane < 8 && W.t0 * 8 + lane < shut) rec = p8_record<DH>(P.c, PP.pages, PP.page_bytes, W.b, W.h, W.t0 * 8 + lane);
 #pragma unroll 1
     for (int t = -1; t < W.nb; ++t) {
@@ -358,11 +381,14 @@ __device__ __forceinline__ void p8t_operands(const Paged8& PP, const PagedLine& 
         const bool good = __all_sync(0xffffffffu, mbar_wait(empty + 8u * (g & 1u), ((g >> 1) & 1u) ^ 1u, abort_flag));
         if (good) {
           if (there == 0xffu) {
+#pragma unroll 1
+            for (int j = cw; j < 8; j += 3) {
+              X::template store<VALUES>(at, j, c[0]);
 #pragma unroll
-            for (int i = 0; i < 3; ++i)
-              if (i < 2 || cw < 2) X::template store<VALUES>(at, cw + 3 * i, c[i]);
+              for (int r = 0; r < X::UNITS; ++r) { c[0][r] = c[1][r]; c[1][r] = c[2][r]; }
+            }
           } else {
-            p8t_ragged<DH, VALUES>(PP, W.b, W.h, (W.t0 + t) * 8, there, len, keys, at, cw);
+            p8t_ragged<DH, VALUES>(PP, W.b, W.h, (W.t0 + t) * 8, last, len, keys, at, cw);
           }
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         }
@@ -371,6 +397,7 @@ __device__ __forceinline__ void p8t_operands(const Paged8& PP, const PagedLine& 
         ++g;
       }
       there = __ballot_sync(0xffffffffu, rec != nullptr);
+      last = rec;
       if (there == 0xffu) {
 #pragma unroll
         for (int i = 0; i < 3; ++i) {
@@ -404,11 +431,11 @@ __global__ void __launch_bounds__(P8T_THREADS, 1) paged8_tree_kernel(const __gri
   auto full_bar = [&](int kv, uint32_t blk) { return bar0 + 64u + 16u * kv + 8u * (blk & 1u); };
   auto empty_bar = [&](int kv, uint32_t blk) { return bar0 + 96u + 16u * kv + 8u * (blk & 1u); };
   auto table_bar = [&](uint32_t blk) { return bar0 + 128u + 8u * (blk & 3u); };
-  uint32_t* tmem_slot = (uint32_t*)(bp + C::O_BAR + 160);
+  auto h_bar = [&](int i) { return bar0 + 160u + 8u * i; };
+  uint32_t* tmem_slot = (uint32_t*)(bp + C::O_BAR + 176);
   volatile int* abort_flag = (volatile int*)(tmem_slot + 1);
   volatile int* odd_flag = abort_flag + 1;   // an open slot's value that is not finite was met
   P8Table* const tabs = (P8Table*)(bp + C::O_TAB);
-  float* const s_down = (float*)(bp + C::O_DOWN);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int R = P.n * P.group, cap = (int)P.c.cap();
   pdl_trigger();
@@ -417,6 +444,7 @@ __global__ void __launch_bounds__(P8T_THREADS, 1) paged8_tree_kernel(const __gri
       mbar_init(q_bar(i), 128);
       mbar_init(s_bar(i), 1);
       mbar_init(p_bar(i), 128);
+      mbar_init(h_bar(i), 128);
       mbar_init(o_bar(i), 1);
     }
     for (uint32_t i = 0; i < 4; ++i) mbar_init(table_bar(i), 1);
@@ -429,6 +457,8 @@ __global__ void __launch_bounds__(P8T_THREADS, 1) paged8_tree_kernel(const __gri
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(512u) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
+  for (int i = threadIdx.x; i < 2 * C::KTILE / 16; i += P8T_THREADS) reinterpret_cast<uint4*>(bp + C::O_V)[i] = make_uint4(0u, 0u, 0u, 0u);      // (finite)
+  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   pdl_wait(KID_ATTN);
   paged_line(L, P, PT_KB);                   // ends with a barrier
   tc_fence_before();
@@ -438,8 +468,6 @@ __global__ void __launch_bounds__(P8T_THREADS, 1) paged8_tree_kernel(const __gri
   const bool idle = L.x_begin == L.x_end;
 
   if (warp >= 8) {
-    // 128 registers a thread at the launch become 160 for the softmax warps and 96 for these: 512 * 128 = 256 * (160 + 96)
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 96;");
     if (idle) {
       if (threadIdx.x == 256) P.joins[blockIdx.x * 8] = 0;
     } else if (warp == P8T_TABLE_WARP) {
@@ -544,7 +572,7 @@ __global__ void __launch_bounds__(P8T_THREADS, 1) paged8_tree_kernel(const __gri
         }
         for (int t = 0; t < W.nb && ok; ++t, ++g) {
           for (int i = 0; i < tiles && ok; ++i) {
-            ok = mbar_wait(p_bar(i), c[i]++ & 1u, abort_flag);
+            ok = mbar_wait(h_bar(i), c[i] & 1u, abort_flag);
             if (ok && i == 0) ok = mbar_wait(full_bar(1, g), (g >> 1) & 1u, abort_flag);
             ok = __all_sync(0xffffffffu, ok);
             if (!ok) break;
@@ -553,8 +581,17 @@ __global__ void __launch_bounds__(P8T_THREADS, 1) paged8_tree_kernel(const __gri
             const uint64_t vd = umma_desc_sw128(base + C::O_V + (g & 1u) * C::KTILE);
             if (leader) {
 #pragma unroll
-              for (int ks = 0; ks < PT_KB / 16; ++ks)
+              for (int ks = 0; ks < PT_KB / 32; ++ks)
                 tc_mma_bf16_ta(d, pa + ks * 8, vd + (uint64_t)((ks >> 2) * (C::VCHUNK / 16) + 2 * (ks & 3)), IDESC_O, (t > 0 || ks > 0) ? 1u : 0u);
+            }
+            __syncwarp();
+            ok = __all_sync(0xffffffffu, mbar_wait(p_bar(i), c[i]++ & 1u, abort_flag));
+            if (!ok) break;
+            tc_fence_after();
+            if (leader) {
+#pragma unroll
+              for (int ks = PT_KB / 32; ks < PT_KB / 16; ++ks)
+                tc_mma_bf16_ta(d, pa + ks * 8, vd + (uint64_t)((ks >> 2) * (C::VCHUNK / 16) + 2 * (ks & 3)), IDESC_O, 1u);
               tc_commit(o_bar(i));
               if (i == tiles - 1) tc_commit(empty_bar(1, g));
             }
@@ -565,7 +602,6 @@ __global__ void __launch_bounds__(P8T_THREADS, 1) paged8_tree_kernel(const __gri
       }
     }
   } else {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 160;");
     // ------------------------------ softmax ------------------------------
     const int i = warp >> 2, quad = warp & 3, row = quad * 32 + lane;
     const uint32_t lane_addr = (uint32_t)(quad * 32) << 16;
@@ -586,42 +622,33 @@ __global__ void __launch_bounds__(P8T_THREADS, 1) paged8_tree_kernel(const __gri
       // are worked on, but not written
       constexpr int PIECES = DH / 8, RPI = 32 / PIECES;
       const int piece = lane % PIECES;
+      float down;                            // what this row's queries were divided by
       {
         const long long off = ((long long)W.b * P.n + qi) * P.q_stride + (long long)(W.h * P.group + hd) * DH;
-        // four rows a lane at a time, the next four under way (all at once the code was long, and cold once per item)
-        uint4 x[4], y[4];
-        auto fetch = [&](uint4* z, int u0) {
-#pragma unroll
-          for (int u = 0; u < 4; ++u)
-            z[u] = __ldcg(reinterpret_cast<const uint4*>((const bf16*)P.q + __shfl_sync(0xffffffffu, off, (u0 + u) * RPI + lane / PIECES)) + piece);
-        };
-        fetch(y, 0);
 #pragma unroll 1
-        for (int u0 = 0; u0 < PIECES; u0 += 4) {
-#pragma unroll
-          for (int u = 0; u < 4; ++u) x[u] = y[u];
-          if (u0 + 4 < PIECES) fetch(y, u0 + 4);
-#pragma unroll
-          for (int u = 0; u < 4; ++u) {
-            uint32_t top = abs2_max(0u, x[u]);
-            top = max(top & 0xffffu, top >> 16);
-#pragma unroll
-            for (int o = PIECES / 2; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
-            float up, down, f[8];
-            p8_range(__uint_as_float(top << 16), up, down);
-            bf16x8_to_float(x[u], f);
-            const int r = quad * 32 + (u0 + u) * RPI + lane / PIECES;
-            *reinterpret_cast<uint4*>(bp + i * C::QTILE + pt_q_off(r, piece)) =
-                make_uint4(pack_f16(f[0] * up, f[1] * up), pack_f16(f[2] * up, f[3] * up), pack_f16(f[4] * up, f[5] * up), pack_f16(f[6] * up, f[7] * up));
-            if (piece == 0) s_down[i * 128 + r] = down;
-          }
+        for (int u = 0; u < PIECES; ++u)
+          cp_async16(base + i * C::QTILE + pt_q_off(quad * 32 + u * RPI + lane / PIECES, piece),
+                     reinterpret_cast<const uint4*>((const bf16*)P.q + __shfl_sync(0xffffffffu, off, u * RPI + lane / PIECES)) + piece, true);
+        cp_async_commit();
+        cp_async_wait<0>();
+        __syncwarp();
+        // this thread's own row, in place
+        uint32_t top = 0u;
+#pragma unroll 4
+        for (int c8 = 0; c8 < PIECES; ++c8) top = abs2_max(top, *reinterpret_cast<const uint4*>(bp + i * C::QTILE + pt_q_off(row, c8)));
+        float up;
+        p8_range(__uint_as_float(max(top & 0xffffu, top >> 16) << 16), up, down);
+#pragma unroll 2
+        for (int c8 = 0; c8 < PIECES; ++c8) {
+          uint4* at = reinterpret_cast<uint4*>(bp + i * C::QTILE + pt_q_off(row, c8));
+          float f[8];
+          bf16x8_to_float(*at, f);
+          *at = make_uint4(pack_f16(f[0] * up, f[1] * up), pack_f16(f[2] * up, f[3] * up), pack_f16(f[4] * up, f[5] * up), pack_f16(f[6] * up, f[7] * up));
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         tc_fence_before();
         mbar_arrive(q_bar(i));
-        __syncwarp();
       }
-      const float down = s_down[i * 128 + row];
       if (!valid) word = 0ull;
       float m_ref = -INFINITY, l_run = 0.f, vref = 1.f;
       for (int t = 0; t < W.nb; ++t, ++g, ++c) {
@@ -638,19 +665,21 @@ __global__ void __launch_bounds__(P8T_THREADS, 1) paged8_tree_kernel(const __gri
           vis[1] = row_bits(word, k0 + 64, len, keys) & ((unsigned long long)lv.w << 32 | lv.z);
         }
         vref = tab->vref;
-        // The block's scores in two halves of 64, so that they stay in registers: the upper half for its maximum, the lower
-        // half for its maximum and its probabilities, the upper half again (the probabilities, two to a column, lie over
-        // the lower half's scores).
-        float s[64];
+        // The block's scores in halves of 64, so that they stay in registers: for their maximum, and again for their probabilities, which
+        // lie, two to a column, over the lower half's scores. The halves are a loop: unrolled, the kernel's code was more than the
+        // instruction cache holds (a quarter of its requests missed, and warps waited for instructions as long as for data).
+        constexpr int AT = P8T_AT;           // scores at a time
+        float s[AT];
         float m_blk = -INFINITY, widest = 0.f;
         const bool zero = masked && p8t_mask(tS, tab, vis[0], vis[1], down * P.scale_log2);
+#pragma unroll 1
+        for (int part = 0; part < PT_KB / AT; ++part) {
+          p8t_ld<AT>(tS + part * AT, s);
+          float ks[AT / 16];
 #pragma unroll
-        for (int half = 1; half >= 0; --half) {
-          tc_ld64(tS + half * 64, s);
-          const float4 k4 = *reinterpret_cast<const float4*>(tab->ks + half * 4);
-          const float ks[4] = {k4.x, k4.y, k4.z, k4.w};
+          for (int b = 0; b < AT / 16; ++b) ks[b] = tab->ks[part * (AT / 16) + b];
 #pragma unroll
-          for (int b = 0; b < 4; ++b) {
+          for (int b = 0; b < AT / 16; ++b) {
             const float* x = s + 16 * b;
             const float m0 = max3_nan(x[0], x[1], x[2]), m1 = max3_nan(x[3], x[4], x[5]), m2 = max3_nan(x[6], x[7], x[8]), m3 = max3_nan(x[9], x[10], x[11]);
             const float mx = max3_nan(max3_nan(m0, m1, m2), max3_nan(x[12], x[13], x[14]), max3_nan(m3, x[15], x[15]));
@@ -689,16 +718,19 @@ __global__ void __launch_bounds__(P8T_THREADS, 1) paged8_tree_kernel(const __gri
         const float scaled = __fmul_rn(sub, P.scale_log2);
         if (__any_sync(0xffffffffu, fabsf(scaled) >= 16777216.f || !(widest * P.scale_log2 < 1e30f) || zero)) {
           l_run += p8t_slow(tS, tab, down, sub, P.scale_log2);
+          asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+          tc_fence_before();
+          mbar_arrive(h_bar(i));
         } else {
           const float dsc = down * P.scale_log2;
+#pragma unroll 1
+          for (int part = 0; part < PT_KB / AT; ++part) {
+            p8t_ld<AT>(tS + part * AT, s);
+            float ks[AT / 16], lr[AT / 16], ir[AT / 16];
 #pragma unroll
-          for (int half = 0; half < 2; ++half) {
-            if (half) tc_ld64(tS + 64, s);
-            const float4 k4 = *reinterpret_cast<const float4*>(tab->ks + half * 4), r4 = *reinterpret_cast<const float4*>(tab->lr + half * 4),
-                         i4 = *reinterpret_cast<const float4*>(tab->ir + half * 4);
-            const float ks[4] = {k4.x, k4.y, k4.z, k4.w}, lr[4] = {r4.x, r4.y, r4.z, r4.w}, ir[4] = {i4.x, i4.y, i4.z, i4.w};
+            for (int b = 0; b < AT / 16; ++b) { ks[b] = tab->ks[part * (AT / 16) + b]; lr[b] = tab->lr[part * (AT / 16) + b]; ir[b] = tab->ir[part * (AT / 16) + b]; }
 #pragma unroll
-            for (int b = 0; b < 4; ++b) {
+            for (int b = 0; b < AT / 16; ++b) {
               const float cs = ks[b] * dsc, off = lr[b] - scaled;
               const uint64_t cs2 = f2_pack(cs, cs), off2 = f2_pack(off, off);
               uint64_t l2 = 0ull;
@@ -712,10 +744,15 @@ __global__ void __launch_bounds__(P8T_THREADS, 1) paged8_tree_kernel(const __gri
                 l2 = f2_add(l2, f2_pack(p0, p1));
                 w8[u] = pack_f16(p0, p1);
               }
-              tc_st8(tS + (uint32_t)(half * 32 + b * 8), w8);
+              tc_st8(tS + (uint32_t)(part * (AT / 2) + b * 8), w8);
               float a0, a1;
               f2_unpack(l2, a0, a1);
               l_run = fmaf(a0 + a1, ir[b], l_run);
+            }
+            if (part == PT_KB / AT / 2 - 1) {
+              asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+              tc_fence_before();
+              mbar_arrive(h_bar(i));
             }
           }
         }
@@ -758,7 +795,7 @@ __global__ void __launch_bounds__(P8T_THREADS, 1) paged8_tree_kernel(const __gri
       if (W.whole) {                         // coalesced, as the queries came
         const long long off = valid ? (((long long)W.b * P.n + qi) * P.hq + W.h * P.group + hd) * DH : -1ll;
         __syncwarp();
-#pragma unroll
+#pragma unroll 2
         for (int u = 0; u < PIECES; ++u) {
           const long long o = __shfl_sync(0xffffffffu, off, u * RPI + lane / PIECES);
           if (o >= 0)
