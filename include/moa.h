@@ -438,7 +438,7 @@ typedef struct {
   const void *q, *k, *v;        /* T [rows, hq or hkv, head_dim], rows q_stride / kv_stride elements apart (parts of a fused projection); v: with cache only */
   int64_t q_stride, kv_stride;  /* multiples of 16 bytes, as the other strides */
   const void *q_gain, *k_gain;  /* T [head_dim], both or neither (then no norm) */
-  const int32_t *pos;           /* device int32 [rows]; a row with pos < 0 is padding: nothing of it is read or written */
+  const int32_t *pos;           /* device int32 [rows]; a row with pos < 0 is padding: nothing of it is written */
   const double *freq;           /* device double [rot_dim / 2], radians per position */
   void *q_out;                  /* T [rows, hq, head_dim], rows q_out_stride apart; may be q */
   int64_t q_out_stride;

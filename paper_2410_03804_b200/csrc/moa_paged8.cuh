@@ -13,12 +13,13 @@
 // them, so that a lane's 16 bytes are loaded whole, without bank conflicts, and become operand registers by byte masks:
 //   keys    (token % 2, dim / 64, token / 2, dim % 64): 16 dims of a token are 16 bytes
 //   values  (dim / 32, dim % 8, token / 4, dim / 8 % 4, token % 4): 4 tokens of a dim are a word
-// 8-bit codes become fp16 by placing the byte under the exponent of 1024 and subtracting 1152: two instructions for two codes,
-// exact. Queries are scaled by a power of two per row into fp16's range (exact for what lies within 2^28 of the row's largest).
+// 8-bit codes become fp16, exactly, by placing the byte under the exponent of 1024 and subtracting 1152: two instructions for two codes.
+// (A byte with zeros above it is (code + 128) * 2^-24 already, but taking the 128 off the sums afterwards -- from scores by the query's
+// sum, from outputs by one more product of a constant per block -- cost precision where sums cancel and gained nothing.) Queries are
+// scaled by a power of two per row into fp16's range (exact for what lies within 2^28 of the row's largest).
 //
 // What bounds it: one token reads a byte and 1/16 of a scale per cached value once, so the cache's stream from HBM does. 256 bytes
-// per position and head leave 175 cycles of an SM per 16 positions and head; the 64 conversions per lane of them are the largest
-// part of the 240 instructions that they cost, of 700 that can be issued.
+// per position and head leave 175 cycles of an SM per 16 positions and head, 700 instructions.
 #pragma once
 #include <cuda_fp16.h>
 
@@ -277,7 +278,8 @@ __global__ void __launch_bounds__(256) paged8_read_kernel(const PagedView C, con
         reinterpret_cast<float4*>(to)[1] = make_float4(x[4], x[5], x[6], x[7]);
       }
     };
-    auto byte = [](uint32_t w4, int e) { return (float)((int)((w4 >> (8 * e)) & 0xffu) - 128); };
+    // a byte under the exponent of 2^23, less that and 128 (conversions of integers run at a quarter of this rate)
+    auto byte = [](uint32_t w4, int e) { return __uint_as_float(__byte_perm(w4, 0x4b000000u, 0x7540 | e)) - 8388736.f; };
     const int gq = lane >> 2, tq = lane & 3;
     if (rec) {
 #pragma unroll
@@ -337,13 +339,16 @@ __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
   const __half2 v = __floats2half2_rn(lo, hi);
   return *reinterpret_cast<const uint32_t*>(&v);
 }
-// Four codes (plus 128) of a word as fp16: bytes 0 and 2, bytes 1 and 3.
+// Two codes (plus 128), each under the exponent of fp16's 1024, as what they stand for.
+__device__ __forceinline__ uint32_t p8_less_bias(uint32_t w) {
+  uint32_t r;
+  asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(w), "r"(0x64806480u));          // 1024 + 128
+  return r;
+}
+// Four codes (plus 128) of a word as what they stand for: bytes 0 and 2, bytes 1 and 3.
 __device__ __forceinline__ void p8_codes(uint32_t w, uint32_t& even, uint32_t& odd) {
-  const uint32_t e = (w & 0x00ff00ffu) | 0x64006400u, o = __byte_perm(w, 0x64646464u, 0x4341);
-  const __half2 bias = __half2half2(__ushort_as_half(0x6480));       // 1152
-  const __half2 x = __hsub2(*reinterpret_cast<const __half2*>(&e), bias), y = __hsub2(*reinterpret_cast<const __half2*>(&o), bias);
-  even = *reinterpret_cast<const uint32_t*>(&x);
-  odd = *reinterpret_cast<const uint32_t*>(&y);
+  even = p8_less_bias((w & 0x00ff00ffu) | 0x64006400u);
+  odd = p8_less_bias(__byte_perm(w, 0x64646464u, 0x4341));
 }
 // Power of two that brings a row whose largest |x| is m to at most 2^15, and its inverse; 1 for a row without a finite largest.
 __device__ __forceinline__ void p8_range(float m, float& up, float& down) {
@@ -397,8 +402,6 @@ struct Paged8Warp {
     top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
     float up, down;
     p8_range(__uint_as_float(top << 16), up, down);
-    qd[0] = __shfl_sync(0xffffffffu, down, 8 * tq);
-    qd[1] = __shfl_sync(0xffffffffu, down, 8 * tq + 4);
 #pragma unroll
     for (int c = 0; c < DH / 64; ++c) {
       float f[16];
@@ -410,6 +413,8 @@ struct Paged8Warp {
         qf[c * 4 + j][1] = pack_f16(f[4 * j + 1] * up, f[4 * j + 3] * up);
       }
     }
+    qd[0] = __shfl_sync(0xffffffffu, down, 8 * tq);
+    qd[1] = __shfl_sync(0xffffffffu, down, 8 * tq + 4);
 #pragma unroll
     for (int i = 0; i < DH / 16; ++i) { o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f; }
     m[0] = m[1] = -INFINITY;
@@ -502,58 +507,53 @@ struct Paged8Warp {
     }
   }
 
-  // 16 slots of the ring from slot s0 on; V: this warp's scratch. Rows of slots from len on come from the call's new rows when it
-  // has them, and go to the ring with them (store).
+  // 16 slots of the ring from slot s0 on, a multiple of 16; V: this warp's scratch. Rows of slots from len on come from the call's new
+  // rows when it has them, and go to the ring with them (store). One warp of an item comes here while the others wait for it
+  // at the item's end, so addresses are made once and stepped.
   __device__ __forceinline__ void open(const Paged8& PP, int b, int h, int mt, int s0, int len, int keys, unsigned long long any, bool store, uint8_t* V) {
     const PagedAttn& P = PP.a;
-    const int lane = threadIdx.x & 31, R = P.n * P.group;
-    auto exists = [&](int j) { return s0 + j < keys && (s0 + j < len || ((any >> (s0 + j - len)) & 1ull) != 0ull); };
-    auto row = [&](int kv, int j) -> const uint4* {
-      const int slot = s0 + j;
-      if (slot >= len && P.k_new) return reinterpret_cast<const uint4*>((const bf16*)(kv ? P.v_new : P.k_new) + ((long long)b * P.n + (slot - len)) * P.new_stride + (long long)h * DH);
-      return reinterpret_cast<const uint4*>((const bf16*)(kv ? P.c.v : P.c.k) + p8_ring_row(P.c, b, slot, h, DH));
-    };
+    const int lane = threadIdx.x & 31, R = P.n * P.group, old = max(0, min(16, len - s0));       // rows that are committed
+    const int slot = s0 + (lane & 15);
+    const uint32_t live = __ballot_sync(0xffffffffu, slot < keys && (slot < len || ((any >> (slot - len)) & 1ull) != 0ull)) & 0xffffu;
     auto sees = [&](unsigned long long w, int j) -> bool {
-      if (!exists(j)) return false;
-      return s0 + j < len ? w != 0ull : ((w >> (s0 + j - len)) & 1ull) != 0ull;
+      return ((live >> j) & 1u) != 0u && (j < old ? w != 0ull : ((w >> (s0 + j - len)) & 1ull) != 0ull);
     };
-    constexpr int NP = DH / 32, NV = DH / 16;                        // pieces of 8 elements per lane: of a key row, of all values
-    const uint4* q = reinterpret_cast<const uint4*>(q_row(P, b, h, mt, gq));
-    uint4 kx[2][NP], vx[NV], qx[NP];
+    constexpr int NP = DH / 32, NV = DH / 16, CH = DH / 8;           // pieces of 8 elements: per lane of a key row and of all values; of a row
+    const size_t ring_at = p8_ring_row(P.c, b, s0, h, DH);           // (a block does not wrap)
+    const long long ring_ld = (long long)P.c.hkv * DH, new_at = ((long long)b * P.n + (s0 - len)) * P.new_stride + (long long)h * DH;
+    auto row = [&](int kv, int j) -> const bf16* {
+      return j >= old && P.k_new ? (const bf16*)(kv ? P.v_new : P.k_new) + new_at + j * P.new_stride : (const bf16*)(kv ? P.c.v : P.c.k) + ring_at + j * ring_ld;
+    };
+    // the values by copies, past the registers that the queries' and outputs' states leave
+#pragma unroll 2
+    for (int j = lane / CH; j < 16; j += 32 / CH)
+      cp_async16(smem_u32(V) + tile_off<DH>(j, lane % CH), row(1, j) + (lane % CH) * 8, ((live >> j) & 1u) != 0u);
+    cp_async_commit();
+    uint4 kx[2][NP], qx[NP], fresh[2];
 #pragma unroll
-    for (int p = 0; p < 2; ++p)
+    for (int p = 0; p < 2; ++p) {
+      const bool there = (live >> (gq + 8 * p)) & 1u;
+      const uint4* from = reinterpret_cast<const uint4*>(row(0, gq + 8 * p)) + tq;
 #pragma unroll
-      for (int i = 0; i < NP; ++i) kx[p][i] = exists(gq + 8 * p) ? __ldcg(row(0, gq + 8 * p) + tq + 4 * i) : make_uint4(0u, 0u, 0u, 0u);
-#pragma unroll
-    for (int u = 0; u < NV; ++u) {
-      const int j = (u * 32 + lane) / (DH / 8), c = (u * 32 + lane) % (DH / 8);
-      vx[u] = exists(j) ? __ldcg(row(1, j) + c) : make_uint4(0u, 0u, 0u, 0u);
+      for (int i = 0; i < NP; ++i) kx[p][i] = there ? __ldcg(from + 4 * i) : make_uint4(0u, 0u, 0u, 0u);
     }
+    const uint4* q = reinterpret_cast<const uint4*>(q_row(P, b, h, mt, gq)) + tq;
 #pragma unroll
-    for (int i = 0; i < NP; ++i) qx[i] = __ldcg(q + tq + 4 * i);
-    if (store) {
+    for (int i = 0; i < NP; ++i) qx[i] = __ldcg(q + 4 * i);
+    // the first new row, for the ring: its keys and values
+    uint32_t todo = store ? live & ~((1u << old) - 1u) : 0u;
+    const int first = __ffs(todo) - 1;
+    if (todo != 0u && lane < CH) {
 #pragma unroll
-      for (int p = 0; p < 2; ++p)
-#pragma unroll
-        for (int i = 0; i < NP; ++i)
-          if (exists(gq + 8 * p) && s0 + gq + 8 * p >= len)
-            reinterpret_cast<uint4*>((bf16*)P.c.k + p8_ring_row(P.c, b, s0 + gq + 8 * p, h, DH))[tq + 4 * i] = kx[p][i];
-#pragma unroll
-      for (int u = 0; u < NV; ++u) {
-        const int j = (u * 32 + lane) / (DH / 8), c = (u * 32 + lane) % (DH / 8);
-        if (exists(j) && s0 + j >= len) reinterpret_cast<uint4*>((bf16*)P.c.v + p8_ring_row(P.c, b, s0 + j, h, DH))[c] = vx[u];
-      }
+      for (int kv = 0; kv < 2; ++kv) fresh[kv] = __ldcg(reinterpret_cast<const uint4*>(row(kv, first)) + lane);
     }
+    cp_async_wait<0>();
+    __syncwarp();
     // values that are not finite go by themselves to the rows that see them; zeros stand for them in the product
     bool odd = false;
-#pragma unroll
-    for (int u = 0; u < NV; ++u) {
-      const int j = (u * 32 + lane) / (DH / 8), c = (u * 32 + lane) % (DH / 8);
-      odd = odd || odd_any(vx[u]);
-      *reinterpret_cast<uint4*>(V + tile_off<DH>(j, c)) = vx[u];
-    }
-    odd = __any_sync(0xffffffffu, odd);      // (a barrier of the warp, too)
-    __syncwarp();
+#pragma unroll 4
+    for (int u = 0; u < NV; ++u) odd = odd || odd_any(reinterpret_cast<const uint4*>(V)[u * 32 + lane]);
+    odd = __any_sync(0xffffffffu, odd);
     float s[2][4];
 #pragma unroll
     for (int c = 0; c < 2; ++c) s[c][0] = s[c][1] = s[c][2] = s[c][3] = 0.f;
@@ -606,30 +606,54 @@ struct Paged8Warp {
       mma_bf16_16816(o[d], v, hi[0], hi[1]);
       mma_bf16_16816(o[d], v, lo[0], lo[1]);
     }
+    if (lane < CH) {
+#pragma unroll 1
+      for (bool again = false; todo != 0u; todo &= todo - 1u, again = true) {
+        const int j = __ffs(todo) - 1;
+        uint4* const to = reinterpret_cast<uint4*>((bf16*)P.c.k + ring_at + j * ring_ld) + lane;
+        uint4* const to_v = reinterpret_cast<uint4*>((bf16*)P.c.v + ring_at + j * ring_ld) + lane;
+        *to = again ? __ldcg(reinterpret_cast<const uint4*>(row(0, j)) + lane) : fresh[0];
+        *to_v = again ? __ldcg(reinterpret_cast<const uint4*>(row(1, j)) + lane) : fresh[1];
+      }
+    }
     __syncwarp();
   }
 
-  // Leaves (max, sum) and the output of the tile's first `rows` queries in shared memory, as PagedWarp does.
-  __device__ __forceinline__ void finish(float* so, float* sml, int rows) {
+  // Leaves (max, sum) of every query in sml [8][2] and the outputs in so [DH][8].
+  __device__ __forceinline__ void finish(float* so, float* sml) {
     const float unit = vref * 0x1p-7f;
+    float f[2];
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       float t = l[u];
       t += __shfl_xor_sync(0xffffffffu, t, 4);
       t += __shfl_xor_sync(0xffffffffu, t, 8);
       t += __shfl_xor_sync(0xffffffffu, t, 16);
-      const int r = 2 * tq + u;
-      if (r >= rows) continue;
       const bool blind = word[u] == 0ull;    // a row that sees nothing, not even the closed blocks
-      if (gq == 0) { sml[r * 2] = blind ? -INFINITY : m[u]; sml[r * 2 + 1] = blind ? 0.f : t * 0x1p-7f; }
+      f[u] = blind || vref == 0.f ? 0.f : unit;
+      if (gq == 0) { sml[(2 * tq + u) * 2] = blind ? -INFINITY : m[u]; sml[(2 * tq + u) * 2 + 1] = blind ? 0.f : t * 0x1p-7f; }
+      if (f[u] == 0.f) {                     // (what is there may not be finite)
 #pragma unroll
-      for (int i = 0; i < DH / 16; ++i) {
-        so[pg_at<DH>(r, i * 16) + gq] = blind || vref == 0.f ? 0.f : o[i][u] * unit;
-        so[pg_at<DH>(r, i * 16 + 8) + gq] = blind || vref == 0.f ? 0.f : o[i][2 + u] * unit;
+        for (int i = 0; i < DH / 16; ++i) o[i][u] = o[i][2 + u] = 0.f;
       }
+    }
+    float* at = so + gq * 8 + 2 * tq;
+#pragma unroll
+    for (int i = 0; i < DH / 16; ++i) {
+      *reinterpret_cast<float2*>(at + i * 128) = make_float2(o[i][0] * f[0], o[i][1] * f[1]);
+      *reinterpret_cast<float2*>(at + i * 128 + 64) = make_float2(o[i][2] * f[0], o[i][3] * f[1]);
     }
   }
 };
+
+// Columns 4 c .. of row r of (sequence, head): a / Z, zeros for a row that sees nothing; a NaN stays one.
+template <int DH>
+__device__ __forceinline__ void p8_write(const PagedAttn& P, int b, int h, int r, int c, float Z, float4 a) {
+  const float inv = Z == 0.f ? 0.f : 1.f / Z;
+  if (Z == 0.f) a = make_float4(0.f, 0.f, 0.f, 0.f);
+  const int i = r / P.group;
+  store4((bf16*)P.out + (((size_t)b * P.n + i) * P.hq + h * P.group + (r - i * P.group)) * DH + c * 4, make_float4(a.x * inv, a.y * inv, a.z * inv, a.w * inv));
+}
 
 template <int DH>
 __global__ void __launch_bounds__(PG_THREADS, 2) paged8_rows_kernel(const Paged8 PP) {
@@ -661,33 +685,40 @@ __global__ void __launch_bounds__(PG_THREADS, 2) paged8_rows_kernel(const Paged8
   const int cap = (int)P.c.cap();
 
   // ---- copies: the next closed block of this warp ----
+  const int per = P.c.shift - 4;
   PagedPlace F = L.first;
   int f_x = x_begin, f_blk = min(L.len[F.b], cap) >> 4;              // closed blocks of F's sequence
+  const int* f_table = P.c.table + (size_t)F.b * P.c.max_pages;
   unsigned live = 0u;                        // bit per stage: a copy is under way (not, where the table does not have the block)
-  const uint8_t* next = nullptr;
+  int next = -1, page = -1;                  // the next block, its page
   bool more = false;
+  const uint8_t* from = nullptr;             // block 0 of its page 0, its head
+  const uint8_t* f_head = PP.pages + (long long)(F.h << per) * C::REC;
   auto look = [&]() {                        // finds the next closed block, a step ahead of its copy
     more = false;
     while (f_x < x_end && !more) {
-      const int blk = F.t * PG_WARPS + warp;
-      if (blk < f_blk) {
-        next = p8_record<DH>(P.c, PP.pages, PP.page_bytes, F.b, F.h, blk);
+      next = F.t * PG_WARPS + warp;
+      if (next < f_blk) {
+        page = f_table[next >> per];
+        from = f_head;
         more = true;
       }
       ++f_x;
       if (++F.t == F.T_b && f_x < x_end) {
         F.at(L, P, f_x);
         f_blk = min(L.len[F.b], cap) >> 4;
+        f_table = P.c.table + (size_t)F.b * P.c.max_pages;
+        f_head = PP.pages + (long long)(F.h << per) * C::REC;
       }
     }
   };
   auto issue = [&](int st) {
     if (!more) return;
-    if (next) {
+    if (page >= 0 && page < P.c.n_pages) {
       live |= 1u << st;
       if (lane == 0) {
         mbar_expect_tx(bar_s + 8u * st, C::REC);
-        bulk_load(ring_s + st * C::REC, next, C::REC, bar_s + 8u * st);
+        bulk_load(ring_s + st * C::REC, from + page * PP.page_bytes + (long long)((next & ((1 << per) - 1)) * C::REC), C::REC, bar_s + 8u * st);
       }
     }
     look();
@@ -708,11 +739,14 @@ __global__ void __launch_bounds__(PG_THREADS, 2) paged8_rows_kernel(const Paged8
     W.begin(P, b, h, mt);
     const bool whole = t0 == 0 && t1 == S.T_b;
     const int place = x == x_begin ? 0 : 1;
-    if (!whole && threadIdx.x == PG_THREADS - 32) {                  // (while the first copies are on their way)
+    if (!whole && lane == 0 && (warp == 2 || warp == 5)) {           // (while the first copies are on their way)
       int* j = s_join[place];
-      j[0] = x0; j[1] = b; j[2] = h; j[3] = mt;
-      j[4] = place ? (int)blockIdx.x : line_owner(L, x0);
-      j[5] = line_owner(L, x0 + S.T_b - 1);
+      if (warp == 2) {
+        j[0] = x0; j[1] = b; j[2] = h; j[3] = mt;
+        j[4] = place ? (int)blockIdx.x : line_owner(L, x0);
+      } else {
+        j[5] = line_owner(L, x0 + S.T_b - 1);
+      }
     }
     // the open slots first, at most five blocks and so one of this warp: their loads' latency passes while the copies fly
     {
@@ -732,42 +766,44 @@ __global__ void __launch_bounds__(PG_THREADS, 2) paged8_rows_kernel(const Paged8
       issue(st);
       st = st + 1 == P8_STAGES ? 0 : st + 1;
     }
-    // ---- merge of the warps ----
+    // ---- merge of the warps: a thread takes four columns of a row. (Code that runs once per item comes cold from memory, so loops here
+    // stay loops.) ----
     const int rows = min(PG_ROWS, R - mt * PG_ROWS), xn = x + (t1 - t0);
-    W.finish(reinterpret_cast<float*>(scratch), &sml[warp][0][0], rows);
-    if (dead && lane < rows) sml[warp][lane][1] = __int_as_float(0x7fffffff);
+    W.finish(reinterpret_cast<float*>(scratch), &sml[warp][0][0]);
+    if (dead && lane < PG_ROWS) sml[warp][lane][1] = __int_as_float(0x7fffffff);
     __syncthreads();
-    const size_t prow = ((size_t)blockIdx.x * 2 + place) * PG_ROWS;
-    for (int i = threadIdx.x; i < rows * (DH / 4); i += PG_THREADS) {
-      const int r = i / (DH / 4), c = i - r * (DH / 4), rr = mt * PG_ROWS + r;
+    const size_t piece0 = (size_t)blockIdx.x * 2 + place;
+    const int mr = threadIdx.x & 7, mc = threadIdx.x >> 3;           // row, columns 4 mc ...
+    if (mr < rows && mc < DH / 4) {
+      const float* so = reinterpret_cast<const float*>(pg_smem + PG_WARPS * P8_STAGES * C::REC) + mc * 32 + mr;
       float M = -INFINITY;
 #pragma unroll
-      for (int w = 0; w < PG_WARPS; ++w) M = fmaxf(M, sml[w][r][0]);
+      for (int w = 0; w < PG_WARPS; ++w) M = fmaxf(M, sml[w][mr][0]);
       const float ref = M == -INFINITY ? 0.f : M;
       float Z = 0.f;
       float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
+#pragma unroll 4
       for (int w = 0; w < PG_WARPS; ++w) {
-        const float f = exp2f((sml[w][r][0] - ref) * P.scale_log2);
-        Z = fmaf(f, sml[w][r][1], Z);
-        const float4 y = *reinterpret_cast<const float4*>(pg_smem + PG_WARPS * P8_STAGES * C::REC + w * C::SCRATCH + pg_at<DH>(r, c * 4) * 4);
-        a.x = fmaf(f, y.x, a.x); a.y = fmaf(f, y.y, a.y); a.z = fmaf(f, y.z, a.z); a.w = fmaf(f, y.w, a.w);
+        const float f = ex2_approx((sml[w][mr][0] - ref) * P.scale_log2);
+        const float* y = so + w * (C::SCRATCH / 4);
+        Z = fmaf(f, sml[w][mr][1], Z);
+        a.x = fmaf(f, y[0], a.x); a.y = fmaf(f, y[8], a.y); a.z = fmaf(f, y[16], a.z); a.w = fmaf(f, y[24], a.w);
       }
       if (whole) {
-        const float inv = Z == 0.f ? 0.f : 1.f / Z;                  // a row that sees nothing; a NaN stays one
-        if (Z == 0.f) a = make_float4(0.f, 0.f, 0.f, 0.f);
-        store4((bf16*)P.out + (((size_t)b * P.n + rr / P.group) * P.hq + h * P.group + rr % P.group) * DH + c * 4,
-               make_float4(a.x * inv, a.y * inv, a.z * inv, a.w * inv));
+        p8_write<DH>(P, b, h, mt * PG_ROWS + mr, mc, Z, a);
       } else {
-        __stcg(reinterpret_cast<float4*>(P.part_o + (prow + r) * DH + c * 4), a);
-        if (c == 0) __stcg(reinterpret_cast<float2*>(P.part_ml + (prow + r) * 2), make_float2(M, Z));
+        __stcg(reinterpret_cast<float4*>(P.part_o) + (piece0 * (DH / 4) + mc) * PG_ROWS + mr, a);
+        if (mc == 0) __stcg(reinterpret_cast<float2*>(P.part_ml) + piece0 * PG_ROWS + mr, make_float2(M, Z));
       }
     }
     __syncthreads();                                                 // the merge is read before the scratch is written again
     if (!whole && threadIdx.x == 0) {
-      const int c0 = s_join[place][4], c1 = s_join[place][5];        // as in the paged row kernel: who delivers the last piece joins them
-      __threadfence();
-      s_last[place] = atomicAdd(P.arrived + c0, 1) == c1 - c0;
+      // Who delivers the last piece joins them. The count releases this CTA's stores, which came before the barrier, and acquires the others'
+      // for the whole CTA, behind the next one.
+      const int c0 = s_join[place][4], c1 = s_join[place][5];
+      int before;
+      asm volatile("atom.acq_rel.gpu.global.add.s32 %0, [%1], 1;" : "=r"(before) : "l"(P.arrived + c0) : "memory");
+      s_last[place] = before == c1 - c0;
     }
     x = xn;
   }
@@ -777,78 +813,71 @@ __global__ void __launch_bounds__(PG_THREADS, 2) paged8_rows_kernel(const Paged8
       while (((live >> s) & 1u) && !mbar_test(bar_s + 8u * s, (phase >> s) & 1u) && clock64() < t_end) {}
   }
 
-  // ---- join: pieces in the order of their positions, a group of threads for every so many of them ----
+  // ---- join: pieces in the order of their positions, four columns of a row per thread, and as many threads for those as there are ----
   __syncthreads();
+#pragma unroll 1
   for (int place = 0; place < 2; ++place) {
     if (!s_last[place]) continue;                                    // the same for the whole CTA
     const int x0 = s_join[place][0], b = s_join[place][1], h = s_join[place][2], mt = s_join[place][3], c0 = s_join[place][4], c1 = s_join[place][5];
     if (threadIdx.x == 0) P.arrived[c0] = 0;                         // as the next call expects it
-    __threadfence();
-    const int rows = min(PG_ROWS, R - mt * PG_ROWS), units = rows * (DH / 4), np = c1 - c0 + 1;
-    const int fp = first_place(L, c0, x0);
-    const int subs = max(1, min(PG_THREADS / units, (np + 7) / 8)), each = (np + subs - 1) / subs;
-    float* sub_o = reinterpret_cast<float*>(pg_smem + PG_WARPS * P8_STAGES * C::REC);          // [sub][unit][6]: 6 KB of the scratch
-    for (int u0 = 0; u0 < units; u0 += PG_THREADS) {
-      const int sub = threadIdx.x / units, unit = subs > 1 ? threadIdx.x - sub * units : u0 + threadIdx.x;
-      const bool work = sub < subs && unit < units;
-      const int r = unit / (DH / 4), c = unit - r * (DH / 4), rr = mt * PG_ROWS + r;
-      float M = -INFINITY, Z = 0.f;
-      float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
-      auto add = [&](float m, float z, const float4& o, float ref) {
-        const float f = exp2f((m - ref) * P.scale_log2);
-        Z = fmaf(f, z, Z);
-        a.x = fmaf(f, o.x, a.x); a.y = fmaf(f, o.y, a.y); a.z = fmaf(f, o.z, a.z); a.w = fmaf(f, o.w, a.w);
-      };
-      auto move = [&](float mx) {                                    // to a new reference
-        const float g = exp2f((M - (mx == -INFINITY ? 0.f : mx)) * P.scale_log2);
-        Z *= g;
-        a.x *= g; a.y *= g; a.z *= g; a.w *= g;
-        M = mx;
-      };
-      if (work) {
-        const int p_end = min(c1 + 1, c0 + (sub + 1) * each);
-        for (int p0 = c0 + sub * each; p0 < p_end; p0 += 8) {        // eight loads under way
-          float2 ml[8];
-          float4 o[8];
+    const int rows = min(PG_ROWS, R - mt * PG_ROWS), np = c1 - c0 + 1, fp = first_place(L, c0, x0);
+    int shift = 3;                                                   // rows as a power of two
+    while (shift > 0 && (1 << (shift - 1)) >= rows) --shift;
+    const int units = (DH / 4) << shift, subs = PG_THREADS / units, each = (np + subs - 1) / subs;
+    const int sub = threadIdx.x / units, unit = threadIdx.x - sub * units, r = unit & ((1 << shift) - 1), c = unit >> shift;
+    constexpr int JOIN = 8;                  // pieces under way
+    float M = -INFINITY, Z = 0.f;
+    float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+    auto add = [&](float m, float z, const float4& o, float ref) {
+      const float f = ex2_approx((m - ref) * P.scale_log2);
+      Z = fmaf(f, z, Z);
+      a.x = fmaf(f, o.x, a.x); a.y = fmaf(f, o.y, a.y); a.z = fmaf(f, o.z, a.z); a.w = fmaf(f, o.w, a.w);
+    };
+    auto move = [&](float mx) {                                      // to a new reference
+      const float g = ex2_approx((M - (mx == -INFINITY ? 0.f : mx)) * P.scale_log2);
+      Z *= g;
+      a.x *= g; a.y *= g; a.z *= g; a.w *= g;
+      M = mx;
+    };
+    const float4* po = reinterpret_cast<const float4*>(P.part_o) + c * PG_ROWS + r;
+    const float2* pm = reinterpret_cast<const float2*>(P.part_ml) + r;
+    const int end = min(np, (sub + 1) * each);
+#pragma unroll 1
+    for (int i = sub * each; i < end; i += JOIN) {
+      float2 ml[JOIN];
+      float4 o[JOIN];
 #pragma unroll
-          for (int u = 0; u < 8; ++u) {
-            const size_t at = (size_t)piece_of(min(p0 + u, p_end - 1), c0, fp) * PG_ROWS + r;
-            ml[u] = __ldcg(reinterpret_cast<const float2*>(P.part_ml + at * 2));
-            o[u] = __ldcg(reinterpret_cast<const float4*>(P.part_o + at * DH + c * 4));
-          }
-          float mx = M;
+      for (int u = 0; u < JOIN; ++u) {
+        const int k = min(i + u, end - 1), piece = (c0 + k) * 2 + (k == 0 ? fp : 0);
+        ml[u] = __ldcg(pm + (size_t)piece * PG_ROWS);
+        o[u] = __ldcg(po + (size_t)piece * (DH / 4) * PG_ROWS);
+      }
+      float mx = M;
 #pragma unroll
-          for (int u = 0; u < 8; ++u) mx = fmaxf(mx, ml[u].x);
-          move(mx);
-          const float ref = mx == -INFINITY ? 0.f : mx;
+      for (int u = 0; u < JOIN; ++u) mx = fmaxf(mx, ml[u].x);
+      move(mx);
+      const float ref = mx == -INFINITY ? 0.f : mx;
 #pragma unroll
-          for (int u = 0; u < 8; ++u)
-            if (p0 + u < p_end) add(ml[u].x, ml[u].y, o[u], ref);
-        }
-      }
-      if (subs > 1) {                                                // units <= the CTA's threads: one round
-        float* t = sub_o + (sub * units + unit) * 6;
-        if (work && sub > 0) { t[0] = M; t[1] = Z; t[2] = a.x; t[3] = a.y; t[4] = a.z; t[5] = a.w; }
-        __syncthreads();
-        if (work && sub == 0) {
-          float mx = M;
-          for (int q = 1; q < subs; ++q) mx = fmaxf(mx, sub_o[(q * units + unit) * 6]);
-          move(mx);
-          const float ref = mx == -INFINITY ? 0.f : mx;
-          for (int q = 1; q < subs; ++q) {
-            const float* y = sub_o + (q * units + unit) * 6;
-            add(y[0], y[1], make_float4(y[2], y[3], y[4], y[5]), ref);
-          }
-        }
-        __syncthreads();
-      }
-      if (work && sub == 0) {
-        const float inv = Z == 0.f ? 0.f : 1.f / Z;
-        if (Z == 0.f) a = make_float4(0.f, 0.f, 0.f, 0.f);
-        store4((bf16*)P.out + (((size_t)b * P.n + rr / P.group) * P.hq + h * P.group + rr % P.group) * DH + c * 4,
-               make_float4(a.x * inv, a.y * inv, a.z * inv, a.w * inv));
-      }
+      for (int u = 0; u < JOIN; ++u)
+        if (i + u < end) add(ml[u].x, ml[u].y, o[u], ref);
     }
+    if (subs > 1) {
+      float* t = reinterpret_cast<float*>(pg_smem) + threadIdx.x;    // [6][256]; the rings are empty
+      t[0] = M; t[256] = Z; t[512] = a.x; t[768] = a.y; t[1024] = a.z; t[1280] = a.w;
+      __syncthreads();
+      if (sub == 0) {
+        float mx = M;
+        for (int k = 1; k < subs; ++k) mx = fmaxf(mx, t[k * units]);
+        move(mx);
+        const float ref = mx == -INFINITY ? 0.f : mx;
+        for (int k = 1; k < subs; ++k) {
+          const float* y = t + k * units;
+          add(y[0], y[256], make_float4(y[512], y[768], y[1024], y[1280]), ref);
+        }
+      }
+      __syncthreads();
+    }
+    if (sub == 0 && r < rows) p8_write<DH>(P, b, h, mt * PG_ROWS + r, c, Z, a);
   }
 }
 

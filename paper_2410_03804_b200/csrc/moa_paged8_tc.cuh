@@ -71,10 +71,7 @@ __device__ __forceinline__ void tc_ld32(uint32_t taddr, float* v) {
 }
 // Four codes (plus 128) of a word as fp16, in order.
 __device__ __forceinline__ uint2 p8_codes_in_order(uint32_t w) {
-  const uint32_t a = __byte_perm(w, 0x64646464u, 0x4140), b = __byte_perm(w, 0x64646464u, 0x4342);
-  const __half2 bias = __half2half2(__ushort_as_half(0x6480));
-  const __half2 x = __hsub2(*reinterpret_cast<const __half2*>(&a), bias), y = __hsub2(*reinterpret_cast<const __half2*>(&b), bias);
-  return make_uint2(*reinterpret_cast<const uint32_t*>(&x), *reinterpret_cast<const uint32_t*>(&y));
+  return make_uint2(p8_less_bias(__byte_perm(w, 0x64646464u, 0x4140)), p8_less_bias(__byte_perm(w, 0x64646464u, 0x4342)));
 }
 template <int N>
 __device__ __forceinline__ void p8t_ld(uint32_t taddr, float* v) {

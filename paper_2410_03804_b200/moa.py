@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 
 import torch
 
@@ -516,12 +517,16 @@ def moa_page_plan(pool: PagePool, length: torch.Tensor, n_new=None, max_rows: in
     return maps
 
 
-def _flat_rows(t: torch.Tensor, rows, heads, head_dim, dtype, index: int, what: str) -> int:
+def _flat_rows(t: torch.Tensor, shape, dtype, index: int, what: str) -> int:
     """Checks rows [rows, heads, head_dim] whose heads are contiguous; returns the elements between two rows."""
-    assert t.dim() == 3 and t.dtype is dtype and t.get_device() == index and t.shape == (rows, heads, head_dim), what
+    assert t.shape == shape and t.dtype is dtype and t.get_device() == index, what
     s0, s1, s2 = t.stride()
-    assert s2 == 1 and (s1 == head_dim or heads == 1), what + ": heads must be contiguous"
-    return s0 if rows > 1 else heads * head_dim
+    assert s2 == 1 and (s1 == shape[2] or shape[1] == 1), what + ": heads must be contiguous"
+    return s0 if shape[0] > 1 else shape[1] * shape[2]
+
+
+_QN_ARGS = struct.Struct("@3P2q5Pq1Pq2P7if")                  # moa_qk_norm_rope_args
+assert _QN_ARGS.size == C.sizeof(MoaQkNormRopeArgs)
 
 
 def moa_qk_norm_rope(q: torch.Tensor, k: torch.Tensor, pos: torch.Tensor, freq=None, q_gain=None, k_gain=None, eps: float = 1e-5,
@@ -530,36 +535,40 @@ def moa_qk_norm_rope(q: torch.Tensor, k: torch.Tensor, pos: torch.Tensor, freq=N
     rule. pos: int32 [rows], < 0 for padding; freq: float64 [rot_dim / 2], radians per position (None: no rotation). The results
     go to q_out and k_out (which may be q and k; None: new ones), or, with a PagedCache and slot int64 [rows] (moa_page_plan), keys
     and values v to the cache's pages. Returns (q_out, k_out), k_out None with a cache."""
-    assert q.is_cuda and q.dim() == 3 and q.dtype in (torch.float32, torch.bfloat16), "q: cuda [rows, hq, head_dim]"
-    at, dt, (rows, hq, dh) = q.get_device(), q.dtype, q.shape
+    at, dt, shape = q.get_device(), q.dtype, q.shape
+    assert at >= 0 and len(shape) == 3 and dt in (torch.float32, torch.bfloat16), "q: cuda [rows, hq, head_dim]"
+    rows, hq, dh = shape
     assert k.dim() == 3 and rows >= 1, "k: [rows, hkv, head_dim]"
     hkv = k.shape[1]
-    qs, ks = _flat_rows(q, rows, hq, dh, dt, at, "q"), _flat_rows(k, rows, hkv, dh, dt, at, "k")
+    kv_shape = (rows, hkv, dh)
+    qs, ks = _flat_rows(q, shape, dt, at, "q"), _flat_rows(k, kv_shape, dt, at, "k")
     assert _is(pos, torch.int32, at) and pos.shape == (rows,), "pos: int32 [rows]"
-    assert freq is None or (_is(freq, torch.float64, at) and freq.dim() == 1), "freq: float64 [rot_dim / 2]"
+    fp = gp = hp = rot = 0
+    if freq is not None:
+        assert _is(freq, torch.float64, at) and freq.dim() == 1, "freq: float64 [rot_dim / 2]"
+        fp, rot = freq.data_ptr(), 2 * freq.numel()
     assert (q_gain is None) == (k_gain is None), "q_gain and k_gain come together"
-    for g in (q_gain, k_gain):
-        assert g is None or (_is(g, dt, at) and g.shape == (dh,)), "gains: as the rows, [head_dim]"
+    if q_gain is not None:
+        assert _is(q_gain, dt, at) and q_gain.shape == (dh,) and _is(k_gain, dt, at) and k_gain.shape == (dh,), "gains: as the rows, [head_dim]"
+        gp, hp = q_gain.data_ptr(), k_gain.data_ptr()
     # with padding some rows of a new tensor are not written
     if q_out is None:
-        q_out = _made(lambda: torch.zeros((rows, hq, dh), dtype=dt, device=q.device), stream)
-    qo, ko, vp, sp, cp = _flat_rows(q_out, rows, hq, dh, dt, at, "q_out"), 0, None, None, None
+        q_out = _made(lambda: torch.zeros(shape, dtype=dt, device=q.device), stream)
+    qo, ko, kp, vp, sp, cp = _flat_rows(q_out, shape, dt, at, "q_out"), 0, 0, 0, 0, 0
     if cache is None:
         assert slot is None and v is None, "slot and v belong to a cache"
         if k_out is None:
-            k_out = _made(lambda: torch.zeros((rows, hkv, dh), dtype=dt, device=q.device), stream)
-        ko = _flat_rows(k_out, rows, hkv, dh, dt, at, "k_out")
+            k_out = _made(lambda: torch.zeros(kv_shape, dtype=dt, device=q.device), stream)
+        ko, kp = _flat_rows(k_out, kv_shape, dt, at, "k_out"), k_out.data_ptr()
     else:
         assert k_out is None and v is not None and slot is not None, "a cache needs v and slot, and takes the place of k_out"
         assert cache.index == at and cache.dtype is dt and cache.hkv == hkv and cache.head_dim == dh, "the cache is of another kind of rows"
-        assert _flat_rows(v, rows, hkv, dh, dt, at, "v") == ks, "v must be laid out as k"
+        assert _flat_rows(v, kv_shape, dt, at, "v") == ks, "v must be laid out as k"
         assert _is(slot, torch.int64, at) and slot.shape == (rows,), "slot: int64 [rows]"
         vp, sp, cp = v.data_ptr(), slot.data_ptr(), cache._ref
-    a = MoaQkNormRopeArgs(q.data_ptr(), k.data_ptr(), vp, qs, ks, None if q_gain is None else q_gain.data_ptr(),
-                          None if k_gain is None else k_gain.data_ptr(), pos.data_ptr(), None if freq is None else freq.data_ptr(), q_out.data_ptr(), qo,
-                          None if k_out is None else k_out.data_ptr(), ko, cp, sp, rows, hq, hkv, dh, 0 if freq is None else 2 * freq.numel(),
-                          1 if interleaved else 0, 0 if dt is torch.float32 else 1, eps)
-    _serving_call(at, stream, load_library().moa_qk_norm_rope, "moa_qk_norm_rope", C.addressof(a))
+    a = _QN_ARGS.pack(q.data_ptr(), k.data_ptr(), vp, qs, ks, gp, hp, pos.data_ptr(), fp, q_out.data_ptr(), qo, kp, ko, cp, sp, rows, hq, hkv, dh, rot,
+                      1 if interleaved else 0, 0 if dt is torch.float32 else 1, eps)
+    _serving_call(at, stream, load_library().moa_qk_norm_rope, "moa_qk_norm_rope", a)
     return q_out, k_out
 
 
