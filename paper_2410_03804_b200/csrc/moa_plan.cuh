@@ -153,11 +153,15 @@ __global__ void __launch_bounds__(1024) page_plan_kernel(const PlanArgs A) {
       A.table_out[(size_t)b * A.max_pages + S.held[b] + (i - S.take0[b])] = taken(i);
     }
   } else {
-    const long long all = (long long)A.batch * A.max_pages;
-    for (long long x = tid; x < all; x += nt) {
-      const int b = (int)(x / A.max_pages), j = (int)(x - (long long)b * A.max_pages), i = j - S.held[b];
-      const int n = S.take0[b + 1] - S.take0[b];
-      A.table_out[x] = j < S.keep[b] ? A.table[x] : i >= 0 && i < n ? taken(S.take0[b] + i) : -1;
+    // a sequence's entries by as many warps as there are for each
+    const int warps = nt >> 5, warp = tid >> 5, parts = max(1, warps / A.batch);
+    for (int b = warp % A.batch, part = warp / A.batch; b < A.batch && part < parts; b += warps) {
+      const int keep = S.keep[b], held = S.held[b], take0 = S.take0[b], n = S.take0[b + 1] - take0;
+      const int *in = A.table + (size_t)b * A.max_pages;
+      int* out = A.table_out + (size_t)b * A.max_pages;
+#pragma unroll 4
+      for (int j = part * 32 + (tid & 31); j < A.max_pages; j += parts * 32)
+        out[j] = j < keep ? in[j] : j >= held && j - held < n ? taken(take0 + j - held) : -1;
     }
   }
   if (blockIdx.x == 0) {
