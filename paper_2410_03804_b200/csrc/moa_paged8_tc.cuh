@@ -17,11 +17,11 @@
 // is a term of its addend, 2^(x + log2 r) = r 2^x, and is divided out of the 16 probabilities' sum again.
 // The probabilities are rounded once to fp16 (2^-11 of themselves), a quarter of the outputs' own rounding to bf16.
 // A tile's first 64 probabilities are handed over while the other 64 are made, so half of their product is done when those come.
-// Measured: 16 sequences x 61 rows x 64 heads over 4090 positions: 208 us, with the commit 216 (the row kernel: 1466); 61 rows x 32 heads
-// over 2045: 31.7 and 36.4. What it took to get there, us of the large case: the masks out of the softmax's loop (380 to 350), operands' addresses that are constants apart and their registers
-// not live across a call (to 300 with the next), the open slots' work in a kernel of its own (here it ran cold, once per item, for
-// 100000 cycles), loops in place of unrolled halves (263 to 210: a quarter of the instruction cache's requests had missed; 8 % do now,
-// the rest of the kernel's 98 KB), probabilities in two halves (212 to 208).
+// Measured: 16 sequences x 61 rows x 64 heads over 4090 positions: 208 us, with the commit 216 (the row kernel: 1466); 61 rows x 32
+// heads over 2045: 31.7 and 36.4. What it took to get there, us of the large case: the masks out of the softmax's loop (380 to 350),
+// operands' addresses that are constants apart, their registers not live across a call, and the open slots' work in a kernel of its
+// own (here it ran cold, once per item, for 100000 cycles; together to 263), loops in place of unrolled halves (to 212: a quarter of
+// the instruction cache's requests had missed, 8 % do now), probabilities in two halves (to 208).
 // Every wait is bounded; a CTA whose wait ran out writes NaN to its rows (the serving calls have no status word).
 #pragma once
 #include "moa_paged8.cuh"
@@ -30,7 +30,7 @@
 namespace moa {
 
 constexpr int P8T_THREADS = 512;
-constexpr int P8T_AT = 32;                   // scores that the softmax's loops take at a time: 32 or 64
+constexpr int P8T_AT = 32;                   // scores that the softmax's loops take at a time
 constexpr int P8T_TABLE_WARP = 9, P8T_CONV_WARP = 10;
 
 struct P8Table {                             // of one block of 128 positions: per 16 of them
@@ -72,10 +72,6 @@ __device__ __forceinline__ void tc_ld32(uint32_t taddr, float* v) {
 // Four codes (plus 128) of a word as fp16, in order.
 __device__ __forceinline__ uint2 p8_codes_in_order(uint32_t w) {
   return make_uint2(p8_less_bias(__byte_perm(w, 0x64646464u, 0x4140)), p8_less_bias(__byte_perm(w, 0x64646464u, 0x4342)));
-}
-template <int N>
-__device__ __forceinline__ void p8t_ld(uint32_t taddr, float* v) {
-  if constexpr (N == 64) tc_ld64(taddr, v); else tc_ld32(taddr, v);
 }
 // Barrier over three converting warps that also ORs a flag: who gives up takes all of them along.
 template <int ID>
@@ -662,16 +658,16 @@ __global__ void __launch_bounds__(P8T_THREADS, 1) paged8_tree_kernel(const __gri
           vis[1] = row_bits(word, k0 + 64, len, keys) & ((unsigned long long)lv.w << 32 | lv.z);
         }
         vref = tab->vref;
-        // The block's scores in halves of 64, so that they stay in registers: for their maximum, and again for their probabilities, which
-        // lie, two to a column, over the lower half's scores. The halves are a loop: unrolled, the kernel's code was more than the
-        // instruction cache holds (a quarter of its requests missed, and warps waited for instructions as long as for data).
+        // The block's scores in quarters of 32, so that they stay in registers: for their maximum, and again for their probabilities,
+        // which lie, two to a column, over the lower half's scores. The quarters are a loop: unrolled, the kernel's code was more than
+        // the instruction cache holds (a quarter of its requests missed, and warps waited for instructions as long as for data).
         constexpr int AT = P8T_AT;           // scores at a time
         float s[AT];
         float m_blk = -INFINITY, widest = 0.f;
         const bool zero = masked && p8t_mask(tS, tab, vis[0], vis[1], down * P.scale_log2);
 #pragma unroll 1
         for (int part = 0; part < PT_KB / AT; ++part) {
-          p8t_ld<AT>(tS + part * AT, s);
+          tc_ld32(tS + part * AT, s);
           float ks[AT / 16];
 #pragma unroll
           for (int b = 0; b < AT / 16; ++b) ks[b] = tab->ks[part * (AT / 16) + b];
@@ -722,7 +718,7 @@ __global__ void __launch_bounds__(P8T_THREADS, 1) paged8_tree_kernel(const __gri
           const float dsc = down * P.scale_log2;
 #pragma unroll 1
           for (int part = 0; part < PT_KB / AT; ++part) {
-            p8t_ld<AT>(tS + part * AT, s);
+            tc_ld32(tS + part * AT, s);
             float ks[AT / 16], lr[AT / 16], ir[AT / 16];
 #pragma unroll
             for (int b = 0; b < AT / 16; ++b) { ks[b] = tab->ks[part * (AT / 16) + b]; lr[b] = tab->lr[part * (AT / 16) + b]; ir[b] = tab->ir[part * (AT / 16) + b]; }

@@ -522,3 +522,15 @@ def test_two_caches_of_one_table_on_two_streams():
             _moa().moa_paged8_attention(m.c, q, out=o, ws=w, stream=s)
     torch.cuda.synchronize()
     assert all(torch.equal(o, want) for o in outs)
+
+
+@pytest.mark.parametrize("hq,hkv,lens", [(16, 2, [3000, 90, 1500]), (64, 32, [2500])])
+def test_a_workspace_serves_fewer_rows_and_both_kernels_in_turn(hq, hkv, lens):
+    m = Model(np.random.default_rng(21), lens, hkv, 128, 64, extra=9000)
+    ws = m.c.workspace(61, hq)
+    for n in (61, 1, 5, 40, 61, 1, 2):
+        assert m.c.workspace(n, hq).numel() <= ws.numel()
+        q, k, v = _new_rows(m, n, hq)
+        want = _moa().moa_paged8_attention(m.c, q, k, v)
+        out = torch.full_like(want, NAN)
+        assert torch.equal(_moa().moa_paged8_attention(m.c, q, k, v, out=out, ws=ws), want), n
