@@ -487,7 +487,12 @@ moa_status moa_paged8_append(const moa_paged_cache8 *cache, const void *k_new, c
                              const int32_t *n_new, int32_t advance, void *stream);
 /* moa_paged_attention over the 8-bit cache, without weights: the new rows are kept in the ring. Scores, statistics and sums are fp32. The
  * codes enter the products exactly, the probabilities times the values' scales rounded once to fp16: each off by at most 2^-11 of itself,
- * or, where that is less, 2^-29 of the largest probability times the largest scale. */
+ * or, where that is less, 2^-29 of the largest probability times the largest scale.
+ *   n_new       n, with k_new and v_new or with rows that a call before has put into the ring; 0: committed slots only
+ *   ws          moa_paged8_workspace_bytes bytes, zeroed once; enough for calls of fewer rows of the same cache and heads, too
+ * Calls of many query rows over much room (n > 1, by the table's size and not by the lengths) run on tensor memory; a wait there that
+ * runs out (about 2 s; it means a fault of the device) leaves NaN in the rows concerned. hq / hkv <= 128; batch * hkv * (n * hq / hkv
+ * / 8, rounded up) * (max_pages * page_size / 64, rounded up) <= 2^30. */
 moa_status moa_paged8_workspace_bytes(const moa_paged_cache8 *cache, int32_t n, int32_t hq, size_t *bytes);
 moa_status moa_paged8_attention(const moa_paged_cache8 *cache, const void *q, int64_t q_stride, const void *k_new, const void *v_new,
                                 int64_t new_stride, int32_t n, int32_t n_new, int32_t hq, const uint64_t *mask, float scale, void *out,

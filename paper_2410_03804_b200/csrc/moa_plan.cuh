@@ -9,8 +9,8 @@
 // warp make the sums, the threads then take pages and rows by searching those sums. Large tables take a cluster of eight CTAs,
 // each of which makes the sums for itself (the barriers between reading and writing are the cluster's); the maps of many rows
 // take a second kernel over the whole GPU.
-// A warp takes a sequence's entries together, so that who they belong to is searched once (6.7 to 5.0 us, 16.6 to 14.6 below).
-// Measured, calls in a graph: a decode step of 64 sequences 5.0 us; 64 prompts of up to 32768 rows (18.4 MB of maps) 14.6 us.
+// A warp takes a sequence's entries together, so that who they belong to is searched once (6.7 to 5.0 us, 16.6 to 15.1 below).
+// Measured, calls in a graph: a decode step of 64 sequences 5.0 us; 64 prompts of up to 32768 rows (18.4 MB of maps) 15.1 us.
 #pragma once
 #include "moa_paged.cuh"
 
@@ -122,7 +122,7 @@ __device__ __forceinline__ void plan_row(const PlanArgs& A, const int* row0, int
 }
 
 template <int CL>
-__global__ void __launch_bounds__(1024) page_plan_kernel(const PlanArgs A) {
+__global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(1024) page_plan_kernel(const PlanArgs A) {
   __shared__ PlanSums S;
   pdl_trigger();
   pdl_wait();

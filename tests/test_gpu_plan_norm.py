@@ -108,6 +108,20 @@ def test_plans_of_a_changing_batch(batch, per, n_pages, page, max_rows, seed):
         lens = [L + n if L >= 0 else L for L, n in zip(lens, want[0])]
 
 
+@pytest.mark.parametrize("per", [100, 1000])
+def test_pages_that_come_back_are_taken_in_the_same_call(per):
+    """Half of the batch gives all of its pages to the other half, over and over: every page is read, put back and taken at once."""
+    batch, page = 64, 8
+    ref, p = Pool(batch, per, batch // 2 * per, page), _moa().PagePool.make(batch, per, batch // 2 * per, page)
+    for step in range(20):
+        lens = [-1 if (b + step) % 2 else 0 for b in range(batch)]
+        new = [per * page] * batch
+        want = ref.plan(lens, new)
+        _moa().moa_page_plan(p, _i32(lens), _i32(new))
+        _check_pool(p, ref)
+        assert want[0] == [0 if L < 0 else per * page for L in lens]
+
+
 def test_plan_without_counts_gives_a_row_each():
     p = _moa().PagePool.make(3, 4, 12, 16)
     ref = Pool(3, 4, 12, 16)
