@@ -5,18 +5,22 @@
 //   free pages; who needs more takes them from its top, in the order of the sequences, none overtaking one that waits.
 //
 // What bounds it: the latency of a chain -- lengths, sums over the sequences, table, rows -- at a decode step's sizes; the stores
-// of the maps (16 bytes per row) when whole prompts come in. So one kernel does it all for a step: two sequences per lane of a
-// warp make the sums, the threads then take pages and rows by searching those sums. Large tables take a cluster of eight CTAs,
-// each of which makes the sums for itself (the barriers between reading and writing are the cluster's); the maps of many rows
-// take a second kernel over the whole GPU.
-// A warp takes a sequence's entries together, so that who they belong to is searched once (6.7 to 5.0 us, 16.6 to 15.1 below).
-// Measured, calls in a graph: a decode step of 64 sequences 5.0 us; 64 prompts of up to 32768 rows (18.4 MB of maps) 15.1 us.
+// of the maps (16 bytes per row) when whole prompts come in. Two sequences per lane of a warp make the sums; the threads then take
+// pages and rows by searching those sums.
+// A plan into a second pool overwrites nothing that it reads, so every CTA makes the sums for itself and no two depend on one another:
+// one launch over as much of the GPU as there is work for. A page that comes back and is taken at once is read where it was.
+// A plan in place has to put pages back before any are taken, and to read before it writes: one CTA, or for large tables a cluster of
+// eight, each CTA with its own sums and the cluster's barriers between; the maps of many rows take a second kernel then.
+// Measured, calls in a graph, to a second pool: a decode step of 64 sequences 4.1 us (in place 2.9 to 4.3); 64 prompts of up to 32768
+// rows (18.4 MB of maps) 7.7 us, where one cluster and a second kernel took 15.1.
 #pragma once
 #include "moa_paged.cuh"
 
 namespace moa {
 
 constexpr int PL_CLUSTER = 8;
+constexpr int PL_THREADS = 512;              // of a plan into a second pool
+constexpr int PL_PIECE = 256;
 
 struct PlanArgs {
   const int *table, *held, *free_pages, *free_count;         // [batch, max_pages], [batch], [n_pages] (a stack), [1]
@@ -25,7 +29,7 @@ struct PlanArgs {
   int *rows, *row_start, *row_seq, *row_pos;                 // [batch], [batch + 1], [max_rows] twice
   long long* slot;                                           // [max_rows], or null: no maps
   int batch, max_pages, n_pages, shift, max_rows;
-  int same, maps_here;                                       // the pool's own arrays are written; the maps are this kernel's
+  int maps_here;                                             // in place: the first kernel's
 };
 
 struct PlanSums {
@@ -121,6 +125,52 @@ __device__ __forceinline__ void plan_row(const PlanArgs& A, const int* row0, int
   A.slot[r] = at;
 }
 
+__device__ __forceinline__ void plan_counts(const PlanSums& S, const PlanArgs& A, int left) {
+  const int b = threadIdx.x;
+  if (b < A.batch) {
+    A.held_out[b] = S.keep[b] + S.take0[b + 1] - S.take0[b];
+    A.rows[b] = S.row0[b + 1] - S.row0[b];
+  }
+  if (b <= A.batch) A.row_start[b] = S.row0[b];
+  if (b == 0) *A.count_out = left;
+}
+
+// To a second pool.
+__global__ void __launch_bounds__(PL_THREADS) page_plan_other_kernel(const PlanArgs A) {
+  __shared__ PlanSums S;
+  pdl_trigger();
+  pdl_wait();
+  if (threadIdx.x < 32) plan_sums(S, A);
+  __syncthreads();
+  const int nt = gridDim.x * blockDim.x, tid = blockIdx.x * blockDim.x + threadIdx.x, left = S.have - S.take0[PG_MAX_SEQ];
+  // page i of the stack with the pages that come back on it
+  auto stack = [&](int i) {
+    if (i < S.count) return A.free_pages[i];
+    const int b = plan_find(S.back0, i - S.count);
+    return A.table[(size_t)b * A.max_pages + S.keep[b] + (i - S.count - S.back0[b])];
+  };
+  auto taken = [&](int i) { return stack(S.have - 1 - i); };         // the i-th of all that are taken
+  if (A.slot)
+#pragma unroll 4
+    for (int r = tid; r < A.max_rows; r += nt)
+      plan_row(A, S.row0, r, [&](int b, int j) {
+        return j < S.keep[b] ? A.table[(size_t)b * A.max_pages + j] : taken(S.take0[b] + j - S.held[b]);
+      });
+  for (int i = tid; i < left; i += nt) A.free_out[i] = stack(i);
+  // a warp per PL_PIECE entries of a sequence's table
+  const int pieces = (A.max_pages + PL_PIECE - 1) / PL_PIECE;
+  for (long long w = tid >> 5; w < (long long)pieces * A.batch; w += nt >> 5) {
+    const int b = (int)(w / pieces), j0 = (int)(w - (long long)b * pieces) * PL_PIECE, end = min(j0 + PL_PIECE, A.max_pages);
+    const int keep = S.keep[b], held = S.held[b], take0 = S.take0[b], n = S.take0[b + 1] - take0;
+    const int* in = A.table + (size_t)b * A.max_pages;
+    int* out = A.table_out + (size_t)b * A.max_pages;
+#pragma unroll 4
+    for (int j = j0 + (tid & 31); j < end; j += 32) out[j] = j < keep ? in[j] : j >= held && j - held < n ? taken(take0 + j - held) : -1;
+  }
+  if (blockIdx.x == 0) plan_counts(S, A, left);
+}
+
+// In place.
 template <int CL>
 __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(1024) page_plan_kernel(const PlanArgs A) {
   __shared__ PlanSums S;
@@ -139,41 +189,18 @@ __global__ void __cluster_dims__(CL, 1, 1) __launch_bounds__(1024) page_plan_ker
     const int b = plan_find(S.back0, i), to = S.count + i;
     if (to < A.n_pages) A.free_out[to] = __ldcg(A.table + (size_t)b * A.max_pages + S.keep[b] + (i - S.back0[b]));
   }
-  if (!A.same)
-    for (int i = tid; i < S.count; i += nt) A.free_out[i] = A.free_pages[i];
-  if (CL > 1 || n_back > 0 || !A.same) barrier();
+  if (CL > 1 || n_back > 0) barrier();
   // ---- pages that are taken, from its top: the i-th of all ----
   auto taken = [&](int i) { return __ldcg((const int*)A.free_out + (S.have - 1 - i)); };
-  if (A.same) {
-    for (int i = tid; i < n_back; i += nt) {
-      const int b = plan_find(S.back0, i);
-      A.table_out[(size_t)b * A.max_pages + S.keep[b] + (i - S.back0[b])] = -1;
-    }
-    for (int i = tid; i < n_take; i += nt) {
-      const int b = plan_find(S.take0, i);
-      A.table_out[(size_t)b * A.max_pages + S.held[b] + (i - S.take0[b])] = taken(i);
-    }
-  } else {
-    // a sequence's entries by as many warps as there are for each
-    const int warps = nt >> 5, warp = tid >> 5, parts = max(1, warps / A.batch);
-    for (int b = warp % A.batch, part = warp / A.batch; b < A.batch && part < parts; b += warps) {
-      const int keep = S.keep[b], held = S.held[b], take0 = S.take0[b], n = S.take0[b + 1] - take0;
-      const int *in = A.table + (size_t)b * A.max_pages;
-      int* out = A.table_out + (size_t)b * A.max_pages;
-#pragma unroll 4
-      for (int j = part * 32 + (tid & 31); j < A.max_pages; j += parts * 32)
-        out[j] = j < keep ? in[j] : j >= held && j - held < n ? taken(take0 + j - held) : -1;
-    }
+  for (int i = tid; i < n_back; i += nt) {
+    const int b = plan_find(S.back0, i);
+    A.table_out[(size_t)b * A.max_pages + S.keep[b] + (i - S.back0[b])] = -1;
   }
-  if (blockIdx.x == 0) {
-    const int b = threadIdx.x;
-    if (b < A.batch) {
-      A.held_out[b] = S.keep[b] + S.take0[b + 1] - S.take0[b];
-      A.rows[b] = S.row0[b + 1] - S.row0[b];
-    }
-    if (b <= A.batch) A.row_start[b] = S.row0[b];
-    if (b == 0) *A.count_out = S.have - n_take;
+  for (int i = tid; i < n_take; i += nt) {
+    const int b = plan_find(S.take0, i);
+    A.table_out[(size_t)b * A.max_pages + S.held[b] + (i - S.take0[b])] = taken(i);
   }
+  if (blockIdx.x == 0) plan_counts(S, A, S.have - n_take);
   if (!A.slot || !A.maps_here) return;
   for (int r = tid; r < A.max_rows; r += nt)
     plan_row(A, S.row0, r, [&](int b, int j) {                       // a page that the sequence keeps or one that it takes now

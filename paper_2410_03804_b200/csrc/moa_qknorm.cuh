@@ -13,7 +13,7 @@
 // the loads ahead: 197 us for the large case below, 14 of 24 warps of an SM there on average.)
 // Angles: position * frequency in 64 bits, reduced to a fraction of a turn there (a position of 100000 leaves fp32 no more than
 // 7 bits behind the turn), then cosine and sine in fp32. A warp's lanes form two each and pass them round.
-// Measured, calls in a graph: 32768 rows of 32 + 2 x 8 heads of 128, bf16 (0.81 GB): 144 us, 5.6 TB/s, a copy's rate; 16 x 61 rows of
+// Measured, calls in a graph: 32768 rows of 32 + 2 x 8 heads of 128, bf16 (0.81 GB): 144 us, 5.6 TB/s, 0.85 of a copy's; 16 x 61 rows of
 // 64 + 2 x 8 heads (40 MB, which L2 holds): 11.0 us; 33 rows of 4 + 4 heads of 64, fp32: 3.0 us, the chain of loads and a launch.
 #pragma once
 #include "moa_paged_tc.cuh"

@@ -75,7 +75,7 @@ def _check_maps(maps, want):
 
 @pytest.mark.parametrize("batch,per,n_pages,page,max_rows,seed", [
     (1, 1, 1, 16, 1, 0), (3, 4, 7, 1, 9, 1), (64, 40, 900, 16, 300, 2), (17, 100, 1000, 32, 20000, 3), (64, 700, 30000, 16, 9000, 4), (5, 9, 20, 1024, None, 5),
-    (64, 300, 17000, 8, None, 6)])
+    (64, 300, 17000, 8, None, 6), (64, 100, 3000, 16, 2500, 7), (2, 9, 9, 4, 60, 8)])
 def test_plans_of_a_changing_batch(batch, per, n_pages, page, max_rows, seed):
     """Requests come, grow, shrink and end; some do not fit. In place, and to a second pool, alternately."""
     rng = np.random.default_rng(seed)
@@ -109,15 +109,18 @@ def test_plans_of_a_changing_batch(batch, per, n_pages, page, max_rows, seed):
 
 
 @pytest.mark.parametrize("per", [100, 1000])
-def test_pages_that_come_back_are_taken_in_the_same_call(per):
+@pytest.mark.parametrize("second", [False, True])
+def test_pages_that_come_back_are_taken_in_the_same_call(per, second):
     """Half of the batch gives all of its pages to the other half, over and over: every page is read, put back and taken at once."""
     batch, page = 64, 8
-    ref, p = Pool(batch, per, batch // 2 * per, page), _moa().PagePool.make(batch, per, batch // 2 * per, page)
+    ref, p, other = Pool(batch, per, batch // 2 * per, page), *(_moa().PagePool.make(batch, per, batch // 2 * per, page) for _ in range(2))
     for step in range(20):
         lens = [-1 if (b + step) % 2 else 0 for b in range(batch)]
         new = [per * page] * batch
         want = ref.plan(lens, new)
-        _moa().moa_page_plan(p, _i32(lens), _i32(new))
+        _moa().moa_page_plan(p, _i32(lens), _i32(new), pool_out=other if second else None)
+        if second:
+            p, other = other, p
         _check_pool(p, ref)
         assert want[0] == [0 if L < 0 else per * page for L in lens]
 
