@@ -74,6 +74,7 @@ struct PagedAttn {
   int min_tiles;                             // ... and the least tiles of one
 };
 
+constexpr int PG_JOIN = 10;                  // pieces whose join takes as long as a tile
 struct PagedLine;
 // A place on the line: tile t of item (b, h, mt).
 struct PagedPlace {
@@ -96,7 +97,8 @@ struct PagedLine {
   PagedPlace first;
 };
 
-// Every thread of the CTA calls it; ends with a barrier.
+// Every thread of the CTA calls it; ends with a barrier. LONG: an item of T tiles is cut into pieces of sqrt(T / PG_JOIN) tiles or more.
+template <bool LONG = false>
 __device__ __forceinline__ void paged_line(PagedLine& L, const PagedAttn& P, int tile) {
   if (threadIdx.x < 32) {
     const int lane = threadIdx.x;
@@ -120,7 +122,9 @@ __device__ __forceinline__ void paged_line(PagedLine& L, const PagedAttn& P, int
     L.pre[lane * 2] = inc - sum;
     L.pre[lane * 2 + 1] = inc - sum + own[0];
     const int all = __shfl_sync(0xffffffffu, inc, 31), total = all * hm_n;
-    const int ctas = max(1, min(P.ctas, (total + P.min_tiles - 1) / P.min_tiles));
+    int least = P.min_tiles;
+    if constexpr (LONG) least = max(least, (int)sqrtf((float)__reduce_max_sync(0xffffffffu, max(own[0], own[1])) * (1.f / PG_JOIN)));
+    const int ctas = max(1, min(P.ctas, (total + least - 1) / least));
     // Whole items: an item's share of the CTAs, rounded down. A stretch that ends inside an item costs its CTA a merge and a
     // new start, about two tiles' time, so they are taken when the longest stretch is at most two tiles longer.
     int n[2], count = 0, worst = 0;

@@ -332,6 +332,9 @@ __global__ void __launch_bounds__(256) paged8_read_kernel(const PagedView C, con
 // ---------------------------------------------------------------------------------------------
 // Attention of a few query rows. Work split, pieces and their join are those of the paged row kernel (moa_paged.cuh), with two CTAs per
 // SM: while one merges its warps at the end of an item, the other's copies go on.
+// A long axis is cut into no more pieces than pay for their join: it costs the CTA that makes it about a tenth of a tile's time each, so
+// pieces of sqrt(T / 10) tiles balance both. One head over 30000 positions 17.0 us (26.0 with pieces of one tile, 18.9 and 18.5 with
+// sqrt(T / 5) and sqrt(T / 20)), over 100000 25.2 (32.6); where the heads fill the GPU nothing changes (8 over 32767: 21.3).
 // ---------------------------------------------------------------------------------------------
 __device__ __forceinline__ void mma_f16_16816(float* c, const uint32_t* a, uint32_t b0, uint32_t b1) {
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
@@ -680,7 +683,7 @@ __global__ void __launch_bounds__(PG_THREADS, 2) paged8_rows_kernel(const Paged8
   }
   asm volatile("fence.mbarrier_init.release.cluster;\n\tfence.proxy.async.shared::cta;" ::: "memory");
   pdl_wait(KID_ATTN);
-  paged_line(L, P, PG_WARPS * P8_BLOCK);     // ends with a barrier
+  paged_line<true>(L, P, PG_WARPS * P8_BLOCK);          // ends with a barrier
   const int x_begin = L.x_begin, x_end = L.x_end;
   if (x_begin == x_end) return;
   asm volatile("fence.proxy.async.global;" ::: "memory");            // records that earlier kernels' stores wrote are read by copies

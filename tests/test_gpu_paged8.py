@@ -245,7 +245,7 @@ def test_pages_beyond_four_gigabytes():
 # ------------------------------------------------------------------------------------------------------- attention
 @pytest.mark.parametrize("dh,hq,hkv,page,lens", [
     (64, 4, 4, 16, [0]), (64, 4, 2, 16, [1, 15, 16, 17]), (128, 8, 1, 32, [31, -1, 0, 33]), (128, 32, 8, 16, [2048]), (128, 7, 7, 64, [500, 3]),
-    (128, 40, 4, 16, [129, 700]), (64, 128, 1, 128, [300]), (128, 16, 2, 1024, [4000, 1, 127, 128])])
+    (128, 40, 4, 16, [129, 700]), (64, 128, 1, 128, [300]), (128, 16, 2, 1024, [4000, 1, 127, 128]), (64, 5, 1, 16, [25000, 1300])])
 def test_one_token(dh, hq, hkv, page, lens):
     m = Model(np.random.default_rng(dh + hq + page), lens, hkv, dh, page)
     ws = m.c.workspace(1, hq)
