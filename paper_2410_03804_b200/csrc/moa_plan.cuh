@@ -156,7 +156,7 @@ __global__ void __launch_bounds__(PL_THREADS) page_plan_other_kernel(const PlanA
       plan_row(A, S.row0, r, [&](int b, int j) {
         return j < S.keep[b] ? A.table[(size_t)b * A.max_pages + j] : taken(S.take0[b] + j - S.held[b]);
       });
-  for (int i = tid; i < left; i += nt) A.free_out[i] = stack(i);
+  for (int i = tid; i < S.have; i += nt) A.free_out[i] = stack(i);
   // a warp per PL_PIECE entries of a sequence's table
   const int pieces = (A.max_pages + PL_PIECE - 1) / PL_PIECE;
   for (long long w = tid >> 5; w < (long long)pieces * A.batch; w += nt >> 5) {

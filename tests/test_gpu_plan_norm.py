@@ -123,6 +123,7 @@ def test_pages_that_come_back_are_taken_in_the_same_call(per, second):
             p, other = other, p
         _check_pool(p, ref)
         assert want[0] == [0 if L < 0 else per * page for L in lens]
+        assert sorted(p.free_pages.tolist()) == list(range(batch // 2 * per))       # what was taken is still there, behind the count
 
 
 def test_plan_without_counts_gives_a_row_each():
