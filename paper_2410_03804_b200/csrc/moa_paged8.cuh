@@ -36,6 +36,8 @@ constexpr int P8_RING = 80;                  // rows of the 16-bit ring: 15 of a
 constexpr int P8_STAGES = 2;
 constexpr float P8_BIAS = 7.f;               // probabilities enter their fp16 product times 2^7: a row's maximum may pass the
 constexpr float P8_LAZY = 8.f;               // reference by 2^8 before the sums move to a new one, and 2^15 fits fp16
+constexpr int P8_OPEN = 100;                 // log2 of the open rows' values over the unit of the outputs, at most
+constexpr int P8_LEAST = -105;               // log2 of the least unit: scales are 0 or above 2^-107, units 4 to 8 times those
 
 template <int DH> struct P8Cfg {
   static constexpr int CODES = P8_BLOCK * DH;                   // of the keys, and of the values
@@ -68,6 +70,13 @@ __device__ __forceinline__ size_t p8_ring_row(const PagedView& c, int b, int slo
 // ---------------------------------------------------------------------------------------------
 __device__ __forceinline__ uint32_t abs2_max(uint32_t m, uint32_t w) { return __vmaxu2(m, w & 0x7fff7fffu); }
 __device__ __forceinline__ uint32_t abs2_max(uint32_t m, const uint4& x) { return abs2_max(abs2_max(abs2_max(abs2_max(m, x.x), x.y), x.z), x.w); }
+
+// Largest finite |x| of packed bf16 patterns, kept packed.
+__device__ __forceinline__ uint32_t finite2_max(uint32_t m, uint32_t w) {
+  w = odd_cleared(w) & 0x7fff7fffu;
+  return __vmaxu2(m, w);
+}
+__device__ __forceinline__ uint32_t finite2_max(uint32_t m, const uint4& x) { return finite2_max(finite2_max(finite2_max(finite2_max(m, x.x), x.y), x.z), x.w); }
 
 struct P8Scale {
   float scale, inv;                          // of the record, and codes per unit
@@ -370,7 +379,10 @@ __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_
 }
 
 // One warp's running state over 8 query rows. Maxima are of unscaled scores; sums and outputs are times 2^P8_BIAS, outputs in
-// units of vref, a power of two above the scales of the values that it has met.
+// units of vref, a power of two that only rises: above the scales of the closed blocks that it has met, so that their probabilities
+// times scales fit fp16, and at most 2^P8_OPEN below the open rows' values, which enter as bf16, so that no sum leaves fp32: up
+// to 2^8 (P8_LAZY) * 2^7 * 16 rows * 2^P8_OPEN. It lies that far below them so that open values take no bits off closed blocks of
+// much smaller ones, which rows that do not see the open values still want to the last.
 template <int DH>
 struct Paged8Warp {
   static constexpr int KS = DH / 16;
@@ -378,7 +390,6 @@ struct Paged8Warp {
   float o[DH / 16][4];                       // columns 16 d + gq and + 8 of queries 2 tq and 2 tq + 1
   float m[2], l[2], qd[2];                   // queries 2 tq, 2 tq + 1: reference, sum over this lane's positions, scale of its fp16 form
   float vref, inv_vref;
-  bool ranged;                               // vref comes from a block's scale
   unsigned long long word[2];                // their mask words
   int gq, tq;
 
@@ -426,7 +437,6 @@ struct Paged8Warp {
     m[0] = m[1] = -INFINITY;
     l[0] = l[1] = 0.f;
     vref = inv_vref = 0.f;                   // none yet
-    ranged = false;
   }
 
   // References that the scores z [position][query] have outgrown move up. Rare.
@@ -448,12 +458,14 @@ struct Paged8Warp {
 #pragma unroll
     for (int i = 0; i < DH / 16; ++i) { o[i][0] *= f[0]; o[i][1] *= f[1]; o[i][2] *= f[0]; o[i][3] *= f[1]; }
   }
-  // Outputs move to units of `ref`, a power of two.
+  // Outputs move to units of `ref`, a power of two. (The factor may be below fp32's least, and infinity times zero is no number.)
   __device__ __forceinline__ void rescale(float ref, float inv) {
     if (vref != 0.f) {
-      const float f = vref * inv;
 #pragma unroll
-      for (int i = 0; i < DH / 16; ++i) { o[i][0] *= f; o[i][1] *= f; o[i][2] *= f; o[i][3] *= f; }
+      for (int i = 0; i < DH / 16; ++i) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[i][e] = __fmul_rn(__fmul_rn(o[i][e], vref), inv);
+      }
     }
     vref = ref;
     inv_vref = inv;
@@ -484,10 +496,9 @@ struct Paged8Warp {
 #pragma unroll
     for (int e = 0; e < 4; ++e) z[e >> 1][e & 1] = (s[0][e] + s[1][e]) * (e & 1 ? t1 : t0);
     refer(P, z);
-    if (scale.y != 0.f && (!(scale.y <= vref) || !ranged)) {         // the same for the whole warp; 4 to 8 times the scale, so that it is rarely passed
+    if (!(scale.y <= vref)) {                // the same for the whole warp; 4 to 8 times the scale, so that it is rarely passed
       const uint32_t e = scale.y > 0.f ? (__float_as_uint(scale.y) >> 23) + 3u : 127u;         // (a scale may be NaN)
       rescale(__uint_as_float(e << 23), __uint_as_float((254u - e) << 23));
-      ranged = true;
     }
     const float ratio = scale.y * inv_vref;
     const float sub0 = m[0] == -INFINITY ? 0.f : m[0], sub1 = m[1] == -INFINITY ? 0.f : m[1];
@@ -557,9 +568,15 @@ struct Paged8Warp {
     __syncwarp();
     // values that are not finite go by themselves to the rows that see them; zeros stand for them in the product
     bool odd = false;
+    uint32_t top = 0u;                       // largest finite |v|
 #pragma unroll 4
-    for (int u = 0; u < NV; ++u) odd = odd || odd_any(reinterpret_cast<const uint4*>(V)[u * 32 + lane]);
+    for (int u = 0; u < NV; ++u) {
+      const uint4 x = reinterpret_cast<const uint4*>(V)[u * 32 + lane];
+      odd = odd || odd_any(x);
+      top = finite2_max(top, x);
+    }
     odd = __any_sync(0xffffffffu, odd);
+    top = __reduce_max_sync(0xffffffffu, max(top & 0xffffu, top >> 16)) >> 7;          // its biased exponent
     float s[2][4];
 #pragma unroll
     for (int c = 0; c < 2; ++c) s[c][0] = s[c][1] = s[c][2] = s[c][3] = 0.f;
@@ -573,7 +590,11 @@ struct Paged8Warp {
 #pragma unroll
     for (int e = 0; e < 4; ++e) z[e >> 1][e & 1] = sees(word[e & 1], gq + 8 * (e >> 1)) ? s[0][e] + s[1][e] : -INFINITY;
     refer(P, z);
-    if (vref == 0.f) { vref = 1.f; inv_vref = 1.f; }
+    {                                        // (the first of the item's blocks: no unit is set yet)
+      const uint32_t e = max(top, (uint32_t)(127 + P8_LEAST) + P8_OPEN) - P8_OPEN;
+      vref = __uint_as_float(e << 23);
+      inv_vref = __uint_as_float((254u - e) << 23);
+    }
     if (odd) {                               // (rare)
 #pragma unroll 1
       for (int j = 0; j < 16; ++j) {

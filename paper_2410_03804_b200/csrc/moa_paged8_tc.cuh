@@ -91,12 +91,6 @@ __device__ __forceinline__ void p8_range_to(float m, int t, float& up, float& do
   up = fit ? __uint_as_float((uint32_t)(254 + t - e) << 23) : 1.f;
   down = fit ? __uint_as_float((uint32_t)(e - t) << 23) : 1.f;
 }
-// Largest finite |x| of packed bf16 patterns, kept packed.
-__device__ __forceinline__ uint32_t finite2_max(uint32_t m, uint32_t w) {
-  w = odd_cleared(w) & 0x7fff7fffu;
-  return __vmaxu2(m, w);
-}
-__device__ __forceinline__ uint32_t finite2_max(uint32_t m, const uint4& x) { return finite2_max(finite2_max(finite2_max(finite2_max(m, x.x), x.y), x.z), x.w); }
 __device__ __forceinline__ float warp_top(uint32_t top) { return __uint_as_float(__reduce_max_sync(0xffffffffu, max(top & 0xffffu, top >> 16)) << 16); }
 
 // One unit of work of a converting warp: 16 positions of keys, or of values.

@@ -1,0 +1,58 @@
+"""Edges of the 8-bit paged cache on the GPU: values far apart, against the definition in 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+from tests.test_gpu_paged8 import Model, _attend, _bound, _moa, _new_rows, _tree, _word
+
+pytestmark = pytest.mark.gpu
+
+
+def _check_rows(m, q, k_new, v_new, mask, out, per_row=False):
+    """out [batch, n, hq, dh] against the definition. per_row: "the largest scale" of the bound is that of the slots that the row sees."""
+    batch, n, hq, dh = q.shape
+    G = hq // m.hkv
+    o, qd = out.double().cpu().numpy(), q.double().cpu().numpy()
+    assert np.isfinite(o).all()
+    for b in range(batch):
+        K, V = (np.concatenate([x.astype(np.float64), y[b].double().cpu().numpy()]) for x, y in zip(m.held(b), (k_new, v_new)))
+        L = len(K) - n
+        for i in range(n):
+            see = np.ones(len(K), bool)
+            see[L:] = [(_word(mask, b, i) >> j) & 1 for j in range(n)]
+            most = np.abs(V[see] if per_row else V).max()
+            for h in range(hq):
+                ref, mass, spread = _attend(qd[b, i, h], K[:, h // G], V[:, h // G], see, dh**-0.5)
+                tol = _bound(dh, len(K), spread, mass, ref, most)
+                assert np.all(np.abs(o[b, i, h] - ref) <= tol), (b, i, h, np.max(np.abs(o[b, i, h] - ref) - tol), np.abs(ref).max())
+
+
+# ------------------------------------------------------------------------------------------------------- values far apart
+# A long sequence is cut into pieces of two tiles of 128 positions: the open block's warp has a closed block in hand, too. (n, hq): few rows
+# and rows of trees, by the room's size.
+@pytest.mark.parametrize("n,hq", [(1, 8), (40, 4), (61, 8)])
+@pytest.mark.parametrize("dh", [64, 128])
+@pytest.mark.parametrize("large,small", [(2.0**19, 2.0**-99), (1e20, 1e-16), (2.0**110, 2.0**-90), (1.0, 2.0**-98), (2.0**-60, 2.0**-99), (1e-16, 1e20)])
+def test_open_values_far_from_the_closed_ones(n, hq, dh, large, small):
+    """New rows' values, and those of two committed rows of the open block, of one size behind closed blocks of another."""
+    m = Model(np.random.default_rng(n + dh), [0, 0], 2, dh, 16, extra=5392)
+    k, v = m.fresh(5314), m.fresh(5314, small)
+    v[:, 5312:] = m.fresh(2, large)
+    m.append(k, v, [5314, 194])
+    q, kn, vn = _new_rows(m, n, hq)
+    vn *= large
+    mask = _tree(m.rng, 2, n)
+    out = _moa().moa_paged8_attention(m.c, q, kn, vn, mask=mask)
+    _check_rows(m, q, kn, vn, mask, out)
+
+
+@pytest.mark.parametrize("dh", [64, 128])
+def test_few_rows_keep_their_bits_beside_large_open_values(dh):
+    """A tree slot with values 2^60 times the others' takes nothing off the rows that do not see it, where few rows are attended."""
+    m = Model(np.random.default_rng(dh), [5309], 2, dh, 16, extra=70)
+    n, large = 3, 2.0**60
+    q, kn, vn = _new_rows(m, n, 8)
+    vn[0, 1] *= large
+    mask = torch.tensor([[0b001, 0b011, 0b101]], dtype=torch.int64, device="cuda")
+    out = _moa().moa_paged8_attention(m.c, q, kn, vn, mask=mask)
+    _check_rows(m, q, kn, vn, mask, out, per_row=True)
