@@ -36,6 +36,9 @@ constexpr int P8_RING = 80;                  // rows of the 16-bit ring: 15 of a
 constexpr int P8_STAGES = 2;
 constexpr float P8_BIAS = 7.f;               // probabilities enter their fp16 product times 2^7: a row's maximum may pass the
 constexpr float P8_LAZY = 8.f;               // reference by 2^8 before the sums move to a new one, and 2^15 fits fp16
+// Sums and outputs of a piece are handed on times 2^-32 beside that: probabilities times values are divided at the very end only, and
+// 2^24 positions at 2^8 above their reference may have bf16's largest values. (What is below 2^-117 goes, far under a record's least.)
+constexpr float P8_PIECE = 0x1p-39f;         // 2^-P8_BIAS * 2^-32
 constexpr int P8_OPEN = 100;                 // log2 of the open rows' values over the unit of the outputs, at most
 constexpr int P8_LEAST = -105;               // log2 of the least unit: scales are 0 or above 2^-107, units 4 to 8 times those
 
@@ -458,13 +461,16 @@ struct Paged8Warp {
 #pragma unroll
     for (int i = 0; i < DH / 16; ++i) { o[i][0] *= f[0]; o[i][1] *= f[1]; o[i][2] *= f[0]; o[i][3] *= f[1]; }
   }
-  // Outputs move to units of `ref`, a power of two. (The factor may be below fp32's least, and infinity times zero is no number.)
+  // Outputs move to units of `ref`, a power of two. (A factor below fp32's least goes in two steps: infinity times zero is no number.)
   __device__ __forceinline__ void rescale(float ref, float inv) {
     if (vref != 0.f) {
+      const float f = vref * inv;
+      const bool deep = f < 0x1p-126f;
+      const float f1 = deep ? inv : f, f2 = deep ? vref : 1.f;
 #pragma unroll
       for (int i = 0; i < DH / 16; ++i) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) o[i][e] = __fmul_rn(__fmul_rn(o[i][e], vref), inv);
+        for (int e = 0; e < 4; ++e) o[i][e] = __fmul_rn(__fmul_rn(o[i][e], f1), f2);
       }
     }
     vref = ref;
@@ -648,7 +654,7 @@ struct Paged8Warp {
 
   // Leaves (max, sum) of every query in sml [8][2] and the outputs in so [DH][8].
   __device__ __forceinline__ void finish(float* so, float* sml) {
-    const float unit = vref * 0x1p-7f;
+    const float unit = vref * P8_PIECE;
     float f[2];
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
@@ -658,7 +664,7 @@ struct Paged8Warp {
       t += __shfl_xor_sync(0xffffffffu, t, 16);
       const bool blind = word[u] == 0ull;    // a row that sees nothing, not even the closed blocks
       f[u] = blind || vref == 0.f ? 0.f : unit;
-      if (gq == 0) { sml[(2 * tq + u) * 2] = blind ? -INFINITY : m[u]; sml[(2 * tq + u) * 2 + 1] = blind ? 0.f : t * 0x1p-7f; }
+      if (gq == 0) { sml[(2 * tq + u) * 2] = blind ? -INFINITY : m[u]; sml[(2 * tq + u) * 2 + 1] = blind ? 0.f : t * P8_PIECE; }
       if (f[u] == 0.f) {                     // (what is there may not be finite)
 #pragma unroll
         for (int i = 0; i < DH / 16; ++i) o[i][u] = o[i][2 + u] = 0.f;

@@ -772,7 +772,7 @@ __global__ void __launch_bounds__(P8T_THREADS, 1) paged8_tree_kernel(const __gri
           *reinterpret_cast<uint4*>(q + pt_q_off(row, d / 8)) = make_uint4(w8[0], w8[1], w8[2], w8[3]);
           *reinterpret_cast<uint4*>(q + pt_q_off(row, d / 8 + 1)) = make_uint4(w8[4], w8[5], w8[6], w8[7]);
         } else {                             // columns outside, rows inside: neighbouring threads write neighbouring 16 bytes
-          const float unit = none ? 0.f : vref;
+          const float unit = none ? 0.f : vref * P8_PIECE;
 #pragma unroll
           for (int e = 0; e < 16; e += 4)
             *reinterpret_cast<float4*>(P.part_o + ((piece_at * (DH / 4) + (d + e) / 4) * PT_ROWS + i * 128 + row) * 4) =
@@ -793,7 +793,7 @@ __global__ void __launch_bounds__(P8T_THREADS, 1) paged8_tree_kernel(const __gri
       }
       if (!W.whole && valid) {
         P.part_ml[prow * 2] = none ? -INFINITY : m_ref;
-        P.part_ml[prow * 2 + 1] = dead ? __int_as_float(0x7fffffff) : none ? 0.f : l_run;
+        P.part_ml[prow * 2 + 1] = dead ? __int_as_float(0x7fffffff) : none ? 0.f : l_run * P8_PIECE;
       }
       tc_fence_before();
     }

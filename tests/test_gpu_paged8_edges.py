@@ -35,6 +35,18 @@ def _check_rows(m, q, k_new, v_new, mask, out, per_row=False):
 @pytest.mark.parametrize("large,small", [(2.0**19, 2.0**-99), (1e20, 1e-16), (2.0**110, 2.0**-90), (1.0, 2.0**-98), (2.0**-60, 2.0**-99), (1e-16, 1e20)])
 def test_open_values_far_from_the_closed_ones(n, hq, dh, large, small):
     """New rows' values, and those of two committed rows of the open block, of one size behind closed blocks of another."""
+    _far_apart(n, hq, dh, large, small)
+
+
+@pytest.mark.parametrize("n,hq", [(1, 8), (40, 4), (61, 8)])
+@pytest.mark.parametrize("dh", [64, 128])
+@pytest.mark.parametrize("large,small", [(2.0**122, 1.0), (2.0**122, 2.0**122), (1.0, 2.0**122)])
+def test_values_near_the_largest(n, hq, dh, large, small):
+    """Sums of probabilities times values are divided at the end; values of up to 2^125 still do not leave fp32 on the way."""
+    _far_apart(n, hq, dh, large, small)
+
+
+def _far_apart(n, hq, dh, large, small):
     m = Model(np.random.default_rng(n + dh), [0, 0], 2, dh, 16, extra=5392)
     k, v = m.fresh(5314), m.fresh(5314, small)
     v[:, 5312:] = m.fresh(2, large)
@@ -56,3 +68,16 @@ def test_few_rows_keep_their_bits_beside_large_open_values(dh):
     mask = torch.tensor([[0b001, 0b011, 0b101]], dtype=torch.int64, device="cuda")
     out = _moa().moa_paged8_attention(m.c, q, kn, vn, mask=mask)
     _check_rows(m, q, kn, vn, mask, out, per_row=True)
+
+
+def test_infinity_among_small_open_values_before_large_closed_ones():
+    """The outputs' unit passes from the open values' to the closed blocks', a factor that is zero in fp32: infinity stays what it is."""
+    m = Model(np.random.default_rng(3), [0], 2, 64, 16, extra=5392)
+    m.append(m.fresh(5314), m.fresh(5314, 2.0**122), [5314])
+    q, kn, vn = _new_rows(m, 1, 8)
+    vn *= 2.0**-60
+    vn[0, 0, 1, 7] = float("inf")
+    out = _moa().moa_paged8_attention(m.c, q, kn, vn).float().cpu()[0, 0]
+    assert bool((out[4:, 7] == float("inf")).all())
+    out[4:, 7] = 0
+    assert bool(torch.isfinite(out).all())
