@@ -427,7 +427,8 @@ typedef struct {
  *      page outside 0 .. n_pages-1 is -1. All three may be NULL: no maps, and no bound on the rows.
  * pool_out (NULL: the pool itself) gets the pool as it is afterwards; with arrays of its own, all of them, a plan may be dropped.
  * Entries of the table behind held are then -1; the stack's places behind its count still hold the pages that were taken from them,
- * those behind may hold anything. */
+ * those behind may hold anything. rows may be n_new; beside that, and the pool itself, nothing that is written may overlap anything
+ * that is read or written (MOA_ERR_SHAPE). */
 moa_status moa_page_plan(const moa_page_pool *pool, const moa_page_pool *pool_out, const int32_t *len, const int32_t *n_new, const int32_t *seen,
                          int32_t *rows, int32_t *row_start, int32_t *row_seq, int32_t *row_pos, int64_t *slot, int32_t max_rows, void *stream);
 

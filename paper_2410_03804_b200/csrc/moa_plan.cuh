@@ -30,6 +30,7 @@ struct PlanArgs {
   long long* slot;                                           // [max_rows], or null: no maps
   int batch, max_pages, n_pages, shift, max_rows;
   int maps_here;                                             // in place: the first kernel's
+  int counts_here;                                           // to a second pool: the first kernel's
 };
 
 struct PlanSums {
@@ -167,7 +168,17 @@ __global__ void __launch_bounds__(PL_THREADS) page_plan_other_kernel(const PlanA
 #pragma unroll 4
     for (int j = j0 + (tid & 31); j < end; j += 32) out[j] = j < keep ? in[j] : j >= held && j - held < n ? taken(take0 + j - held) : -1;
   }
-  if (blockIdx.x == 0) plan_counts(S, A, left);
+  if (A.counts_here && blockIdx.x == 0) plan_counts(S, A, left);
+}
+
+// Its counts alone, where they overwrite the numbers of new rows that every CTA above makes its sums from.
+__global__ void __launch_bounds__(128) page_counts_kernel(const PlanArgs A) {
+  __shared__ PlanSums S;
+  pdl_trigger();
+  pdl_wait();
+  if (threadIdx.x < 32) plan_sums(S, A);
+  __syncthreads();
+  plan_counts(S, A, S.have - S.take0[PG_MAX_SEQ]);
 }
 
 // In place.

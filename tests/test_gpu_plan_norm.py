@@ -369,3 +369,24 @@ def test_a_serving_loop(eight):
             moa.moa_paged_commit(cache, 1)
             seen += (length >= 0).int()
         assert length.tolist() == [len(rows[b]) if b in live else -1 for b in range(batch)]
+
+
+@pytest.mark.parametrize("second", [False, True])
+@pytest.mark.parametrize("batch,per,n_pages,page,max_rows", [(64, 700, 30000, 16, 9000), (64, 3000, 100000, 16, 40000), (3, 4, 7, 1, 9)])
+def test_granted_rows_over_the_numbers_asked_for(batch, per, n_pages, page, max_rows, second):
+    """rows may be n_new: every sum is made of what was asked for, whichever CTA writes first."""
+    rng = np.random.default_rng(batch + per)
+    ref, p, other = Pool(batch, per, n_pages, page), *(_moa().PagePool.make(batch, per, n_pages, page) for _ in range(2))
+    lens, new = [0] * batch, torch.zeros(batch, dtype=torch.int32, device="cuda")
+    maps = (new,) + _moa().moa_page_plan(_moa().PagePool.make(batch, per, n_pages, page), _i32(lens), _i32([0] * batch), max_rows=max_rows)[1:]
+    for step in range(20):
+        lens = [0 if L > per * page // 2 else L for L in lens]
+        ask = [int(x) for x in rng.choice([0, 1, 61, 500, per * page // 3], batch)]
+        want = ref.plan(lens, ask, max_rows)
+        new.copy_(_i32(ask))
+        _moa().moa_page_plan(p, _i32(lens), new, pool_out=other if second else None, maps=maps)
+        if second:
+            p, other = other, p
+        _check_pool(p, ref)
+        _check_maps(maps, want)
+        lens = [L + n for L, n in zip(lens, want[0])]

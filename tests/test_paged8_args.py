@@ -140,3 +140,26 @@ def test_the_other_calls_refuse():
     assert lib.moa_paged8_read(r, 1, None, None, None, P, 1, None) == NULL and lib.moa_paged8_read(r, 1, None, None, P, None, 1, None) == NULL
     assert lib.moa_paged8_read(r, 0, None, None, P, P, 1, None) == SHAPE and lib.moa_paged8_read(r, 1, None, None, P, P, 2, None) == DTYPE
     assert lib.moa_paged8_read(r, 1, None, None, P + 8, P, 1, None) == ALIGN
+
+
+def test_plan_refuses_outputs_over_inputs():
+    """Decided by address: every array of the call a page of 64 KB apart, then one output moved into another array."""
+    at = {n: P * (2 + i) for i, n in enumerate(("page_table", "held", "free_pages", "free_count", "len", "n_new", "seen", "rows", "row_start", "row_seq",
+                                                "row_pos", "slot"))}
+    pool = {n: at[n] for n in ("page_table", "held", "free_pages", "free_count")}
+    other = {n: 32 * P + at[n] for n in pool}
+    args = {n: at[n] for n in PLAN if n in at}
+    outs = ("rows", "row_start", "row_seq", "row_pos", "slot")
+    for second in (None, other):
+        call = lambda p=pool, s=second, **kw: _plan(_pool(**p), s and _pool(**s), **dict(args, **kw))  # noqa: E731
+        for o in outs:
+            for name, there in {**args, **pool, **(second or {})}.items():
+                if name != o and (o, name) != ("rows", "n_new"):
+                    assert call(**{o: there}) == SHAPE, (o, name)
+        # the end of one inside of the other: 2 sequences, 10 rows, 4 pages each
+        assert call(rows=at["len"] + 4 - 8 + 4) == SHAPE and call(row_start=at["n_new"] + 4) == SHAPE and call(rows=at["n_new"] + 4) == SHAPE
+        assert call(slot=at["row_pos"] + 32) == SHAPE and call(row_pos=at["slot"] + 76) == SHAPE and call(rows=at["page_table"] + 28) == SHAPE
+        assert call(row_start=at["free_pages"] + 32) == SHAPE
+    for n in pool:                                                   # a second pool that lies in the first one, or in an input
+        assert _plan(_pool(**pool), _pool(**dict(other, **{n: pool["page_table"] + 16})), **args) == SHAPE
+        assert _plan(_pool(**pool), _pool(**dict(other, **{n: at["seen"]})), **args) == SHAPE
