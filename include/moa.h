@@ -442,9 +442,9 @@ typedef struct {
   const void *q_gain, *k_gain;  /* T [head_dim], both or neither (then no norm) */
   const int32_t *pos;           /* device int32 [rows]; a row with pos < 0 is padding: nothing of it is written */
   const double *freq;           /* device double [rot_dim / 2], radians per position */
-  void *q_out;                  /* T [rows, hq, head_dim], rows q_out_stride apart; may be q */
+  void *q_out;                  /* T [rows, hq, head_dim], rows q_out_stride apart; may be q, of the same stride. Beside that no output may overlap a row */
   int64_t q_out_stride;
-  void *k_out;                  /* T [rows, hkv, head_dim], rows k_out_stride apart; may be k. NULL with cache */
+  void *k_out;                  /*   of q, k or v or another output. T [rows, hkv, head_dim], rows k_out_stride apart; may be k likewise. NULL with cache */
   int64_t k_out_stride;
   const moa_paged_cache *cache; /* or NULL: keys and values go to slot[r] of its pages (moa_page_plan), outside of the pool: nowhere. Its */
   const int64_t *slot;          /*   table, lengths, weights and positions are neither read nor written (so not for a cache that evicts) */

@@ -390,3 +390,18 @@ def test_granted_rows_over_the_numbers_asked_for(batch, per, n_pages, page, max_
         _check_pool(p, ref)
         _check_maps(maps, want)
         lens = [L + n for L, n in zip(lens, want[0])]
+
+
+def test_results_between_the_rows_that_are_read():
+    """Results in columns of their own of the buffer that holds the projection, and in place."""
+    rng = np.random.default_rng(40)
+    for rows in (1, 90):
+        q, k, _, gains = _rows(rng, rows, 6, 2, 64, "bf16")
+        pos = _i32(rng.integers(0, 5000, rows).tolist())
+        want = _moa().moa_qk_norm_rope(q, k, pos, _freq(64), *gains)
+        x = torch.zeros((rows, 16, 64), dtype=torch.bfloat16, device="cuda")
+        x[:, 2:8], x[:, 12:14] = q, k
+        got = _moa().moa_qk_norm_rope(x[:, 2:8], x[:, 12:14], pos, _freq(64), *gains, k_out=x[:, 14:16])
+        assert torch.equal(got[0], want[0]) and torch.equal(x[:, 14:16], want[1]) and torch.equal(x[:, 2:8], q) and torch.equal(x[:, 12:14], k)
+        _moa().moa_qk_norm_rope(x[:, 2:8], x[:, 12:14], pos, _freq(64), *gains, q_out=x[:, 2:8], k_out=x[:, :2])
+        assert torch.equal(x[:, 2:8], want[0]) and torch.equal(x[:, :2], want[1])

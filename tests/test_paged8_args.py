@@ -163,3 +163,20 @@ def test_plan_refuses_outputs_over_inputs():
     for n in pool:                                                   # a second pool that lies in the first one, or in an input
         assert _plan(_pool(**pool), _pool(**dict(other, **{n: pool["page_table"] + 16})), **args) == SHAPE
         assert _plan(_pool(**pool), _pool(**dict(other, **{n: at["seen"]})), **args) == SHAPE
+
+
+def test_norm_refuses_outputs_over_other_rows():
+    """bf16, 3 rows: q 32 heads and k 8 heads of 128. In place means the same rows; the parts of one projection may lie between each other."""
+    q, k, qo, ko, row = P, 2 * P, 3 * P, 4 * P, 1024                  # bytes between k's rows: 2048
+    base = dict(q=q, k=k, q_out=qo, k_out=ko)
+    for change in (
+            dict(q_out=q, q_out_stride=8192), dict(q_out=q, q_stride=8192),      # the same start, other rows behind it
+            dict(k_out=k, k_out_stride=2 * row), dict(q_out=q + 16), dict(k_out=k + 2048), dict(k_out=k - 16), dict(q_out=q + 8192),
+            dict(q_out=k), dict(k_out=q), dict(k_out=q + 3 * 8192 - 16), dict(q_out=ko), dict(k_out=qo), dict(rows=1, q_out=q + 16), dict(rows=1, k_out=qo + 64),
+            # one projection of 48 heads per row (12288 bytes): results that reach into the next part, or into the next row's
+            dict(k=q + 8192, q_stride=6144, kv_stride=6144, q_out=q + 4096, q_out_stride=6144),
+            dict(k=q + 8192, q_stride=6144, kv_stride=6144, k_out=q + 8192 + 1024, k_out_stride=6144),
+            dict(k=q + 8192, q_stride=6144, kv_stride=6144, k_out=q + 12288 - 16, k_out_stride=6144)):
+        assert _norm(**dict(base, **change)) == SHAPE, change
+    for change in (dict(q_out=k), dict(q_out=5 * P), dict(q_out=5 * P + 1024, q_out_stride=4096)):
+        assert _norm(cache={}, q=q, k=k, v=5 * P, slot=6 * P, **change) == SHAPE, change
