@@ -262,14 +262,34 @@ __global__ void __launch_bounds__(256) paged8_commit_kernel(const PagedView C, u
   if (rec) p8_close<DH>(rec, [&](int kv, int t) { return (const bf16*)(kv ? C.v : C.k) + p8_ring_row(C, b, ((base + warp) << 4) + t, h, DH); });
 }
 
-// Rows first[b] + i, i < n, of the cache as it is with length[b] committed rows, [batch, n, hkv, DH]: a warp per (sequence, block, head).
+// Rows t0 .. t1 - 1 of a closed block of which the first `rows` are wanted; the others, and all of a missing page's, are zeros.
+// k_out, v_out: where the block's row 0 would go, rows ld elements apart.
+template <typename T, int DH>
+__device__ __noinline__ void p8_read_part(const uint8_t* rec, int rows, int t0, int t1, T* k_out, T* v_out, int ld) {
+  const float2 scale = rec ? __ldcg(reinterpret_cast<const float2*>(rec + 2 * P8Cfg<DH>::CODES)) : make_float2(0.f, 0.f);
+  for (int t = t0; t < t1; ++t)
+    for (int d = threadIdx.x & 31; d < DH; d += 32) {
+      float x = 0.f, y = 0.f;
+      if (rec && t < rows) {
+        x = (float)(rec[((t & 1) * (DH / 64) + d / 64) * 512 + (t >> 1) * 64 + d % 64] - 128) * scale.x;
+        y = (float)(rec[P8Cfg<DH>::CODES + d / 32 * 512 + d % 8 * 64 + (t >> 2) * 16 + d / 8 % 4 * 4 + (t & 3)] - 128) * scale.y;
+      }
+      T *k = k_out + (long long)t * ld + d, *v = v_out + (long long)t * ld + d;
+      if constexpr (sizeof(T) == 2) { *k = __float2bfloat16_rn(x); *v = __float2bfloat16_rn(y); }
+      else { *k = x; *v = y; }
+    }
+}
+
+// Rows first[b] + i, i < n, of the cache's first length[b] rows, [batch, n, hkv, DH]: a warp per (sequence, block, head). A layer that has
+// not been advanced yet has more rows than its len says; with fewer, the last block may be a closed one of which only a part is wanted.
 template <typename T, int DH>
 __global__ void __launch_bounds__(256) paged8_read_kernel(const PagedView C, const uint8_t* pages, long long page_bytes, int n, const int* first,
                                                           const int* length, T* k_out, T* v_out, int blocks) {
   pdl_trigger();
   pdl_wait();
   const int b = blockIdx.y, lane = threadIdx.x & 31;
-  if (C.len[b] < 0 || length[b] < 0) return;
+  const int shut = C.len[b];
+  if (shut < 0 || length[b] < 0) return;
   const int len = (int)min((long long)length[b], C.cap());
   const long long f = first ? first[b] : 0;
   const int b0 = (int)((f >= 0 ? f : f - 15) / 16);
@@ -323,6 +343,12 @@ __global__ void __launch_bounds__(256) paged8_read_kernel(const PagedView C, con
           put(v_out, 4 * tq + t, d8 * 8, x);
         }
       }
+      continue;
+    }
+    if (open && s0 + 16 <= min((long long)shut, C.cap())) {          // (rare) a part of a block that is closed
+      const long long at = (((long long)b * n + i0) * C.hkv + h) * DH;
+      p8_read_part<T, DH>(p8_record<DH>(C, pages, page_bytes, b, h, (int)(s0 >> 4)), (int)(len - s0), (int)max(0ll, -i0), (int)min(16ll, n - i0), k_out + at, v_out + at,
+                          C.hkv * DH);
       continue;
     }
     for (int i = lane; i < 16 * (DH / 8); i += 32) {                 // the open block, or no row at all

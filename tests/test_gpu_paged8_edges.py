@@ -81,3 +81,33 @@ def test_infinity_among_small_open_values_before_large_closed_ones():
     assert bool((out[4:, 7] == float("inf")).all())
     out[4:, 7] = 0
     assert bool(torch.isfinite(out).all())
+
+
+# ------------------------------------------------------------------------------------------------------- rows read back
+@pytest.mark.parametrize("dh,hkv,lens,cut", [(64, 2, [40, 7, 160], [33, 3, 90]), (128, 3, [95, -1, 300], [16, 5, 17]), (128, 1, [64, 81, 200], [0, 80, 199])])
+def test_fewer_rows_than_are_committed(dh, hkv, lens, cut):
+    """The rows of a prefix that ends inside a closed block, as they stand for; a block with NaN behind the prefix's end leaves zeros there."""
+    m = Model(np.random.default_rng(dh + hkv), [min(L, 0) for L in lens], hkv, dh, 16, extra=320)
+    k, v = m.fresh(max(lens)), m.fresh(max(lens))
+    m.append(k, v, lens)
+    n = max(lens) + 5
+    for first in (None, [11, -3, 2]):
+        f = [0, 0, 0] if first is None else first
+        for dt in (torch.float32, torch.bfloat16):
+            got = _moa().moa_paged8_read(m.c, n, first=None if first is None else torch.tensor(first, dtype=torch.int32, device="cuda"),
+                                         length=torch.tensor(cut, dtype=torch.int32, device="cuda"), dtype=dt)
+            for b, L in enumerate(lens):
+                for x, y in zip(got, m.held(b)):
+                    want, at = torch.zeros((n, hkv, dh), dtype=dt), torch.arange(n) + f[b]
+                    ok = (at >= 0) & (at < cut[b]) & (L >= 0)
+                    want[ok] = torch.from_numpy(y)[at[ok]].to(dt)
+                    assert torch.equal(x[b].cpu(), want), (b, f[b], dt)
+
+
+def test_a_prefix_of_a_block_that_holds_a_nan():
+    m = Model(np.random.default_rng(5), [0], 2, 64, 16)
+    k, v = m.fresh(32), m.fresh(32)
+    v[0, 20, 1, 3] = float("nan")
+    m.append(k, v, [32])
+    _, got = _moa().moa_paged8_read(m.c, 32, length=torch.tensor([18], dtype=torch.int32, device="cuda"))
+    assert bool(torch.isnan(got[0, 16:18, 1]).all()) and not bool(got[0, 18:].any()) and bool(torch.isfinite(got[0, :, 0]).all())
