@@ -120,10 +120,7 @@ struct P8Convert {
     return (i >> 1) * 4 + (lane >> 4 ? 1 + (i & 1) : 3 * (i & 1));
   }
   static __device__ __forceinline__ int at_values(int k) { return P8Cfg<DH>::CODES + k * 512 + value_row() * 64 + (threadIdx.x & 3) * 16; }
-  // four tokens of a dim, 8 bytes, into the transposed values
-  static __device__ __forceinline__ void put(uint8_t* V, int j, int tq, int dim, uint2 x) {
-    *reinterpret_cast<uint2*>(V + (j >> 2) * C::VCHUNK + dim * 128 + (((2 * (j & 3) + (tq >> 1)) ^ (dim & 7)) << 4) + (tq & 1) * 8) = x;
-  }
+  // where four tokens of a dim, 8 bytes, go in the transposed values
   static __device__ __forceinline__ uint32_t to_values(int j) {
     const int row = value_row(), tq = threadIdx.x & 3;
     return (uint32_t)((j >> 2) * C::VCHUNK + row * 128 + (((2 * (j & 3) + (tq >> 1)) ^ row) << 4) + (tq & 1) * 8);
