@@ -424,7 +424,7 @@ typedef struct {
  *      row_start[b] = sum of rows before b (device int32 [batch + 1])
  *   4. per row r < max_rows: row_seq[r] its sequence, row_pos[r] its position seen[b] + i (seen NULL: len[b] + i), slot[r] its
  *      place page * page_size + row in the pool (device int32 twice, int64); -1 in all three behind the last row, and a slot on a
- *      page outside 0 .. n_pages-1 is -1. All three may be NULL: no maps, and no bound on the rows.
+ *      page outside 0 .. n_pages-1 is -1. All three may be NULL: no maps, and 2^31 - 1 for max_rows.
  * pool_out (NULL: the pool itself) gets the pool as it is afterwards; with arrays of its own, all of them, a plan may be dropped.
  * Entries of the table behind held are then -1; the stack's places behind its count still hold the pages that were taken from them,
  * those behind may hold anything. rows may be n_new; beside that, and the pool itself, nothing that is written may overlap anything

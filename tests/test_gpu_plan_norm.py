@@ -405,3 +405,37 @@ def test_results_between_the_rows_that_are_read():
         assert torch.equal(got[0], want[0]) and torch.equal(x[:, 14:16], want[1]) and torch.equal(x[:, 2:8], q) and torch.equal(x[:, 12:14], k)
         _moa().moa_qk_norm_rope(x[:, 2:8], x[:, 12:14], pos, _freq(64), *gains, q_out=x[:, 2:8], k_out=x[:, :2])
         assert torch.equal(x[:, 2:8], want[0]) and torch.equal(x[:, :2], want[1])
+
+
+@pytest.mark.parametrize("second", [False, True])
+def test_needs_that_together_pass_32_bits(second):
+    """64 sequences of which each would fit, 2^26 pages each: the sums pass 2^31 at the 33rd and come to 2^32 - 2^26 + 5 at the last.
+    There are pages for the first one's five rows only."""
+    batch, page, per, free = 64, 1, 1 << 26, 50000
+    if torch.cuda.mem_get_info()[0] < (2 if second else 1) * batch * per * 4 + (4 << 30):
+        pytest.skip("not enough memory")
+    new = lambda: _moa().PagePool(torch.full((batch, per), -1, dtype=torch.int32, device="cuda"), _i32([0] * batch),  # noqa: E731
+                                  torch.arange(free, dtype=torch.int32, device="cuda"), _i32([free]), page)
+    p, other = new(), new() if second else None
+    ask = [5] + [per] * 63
+    maps = _moa().moa_page_plan(p, _i32([0] * batch), _i32(ask), max_rows=1000, pool_out=other)
+    p = other or p
+    assert maps[0].tolist() == [5] + [0] * 63 and maps[1].tolist() == [0] + [5] * 64
+    assert p.held.tolist() == [5] + [0] * 63 and int(p.free_count) == free - 5
+    assert p.page_table[0, :6].tolist() == [free - 1 - i for i in range(5)] + [-1] and bool((p.page_table[1:, 0] == -1).all())
+
+
+@pytest.mark.parametrize("second", [False, True])
+def test_rows_that_together_pass_31_bits(second):
+    """Sequences that hold all of their pages already: without maps the rows are bounded by what row_start can hold, 2^31 - 1."""
+    batch, page, per = 6, 1024, 1 << 20
+    new = lambda: _moa().PagePool(torch.arange(batch * per, dtype=torch.int32, device="cuda").reshape(batch, per), _i32([per] * batch),  # noqa: E731
+                                  torch.arange(batch * per, dtype=torch.int32, device="cuda"), _i32([0]), page)
+    p, other = new(), new() if second else None
+    many = (1 << 30) - 1
+    maps = _moa().moa_page_plan(p, _i32([1, 0, 5, 1, 0, -1]), _i32([many, many, 1, many, many, 7]), pool_out=other)
+    # 2^31 - 2 rows, one more, and no room for any behind it; the last one is not in use and gives its pages back
+    assert maps[0].tolist() == [many, many, 1, 0, 0, 0] and maps[1].tolist() == [0, many, 2 * many] + [2 * many + 1] * 4
+    p = other or p
+    assert p.held.tolist() == [per, per, 1, per, per, 0] and int(p.free_count) == 2 * per - 1
+    assert torch.equal(p.free_pages[:2 * per - 1].long(), torch.cat([torch.arange(2 * per + 1, 3 * per), torch.arange(5 * per, 6 * per)]).cuda())
