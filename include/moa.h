@@ -464,7 +464,9 @@ moa_status moa_qk_norm_rope(const moa_qk_norm_rope_args *args, void *stream);
  * open block and the rows that are not committed lie in 16 bits in a ring, slot j in row j % MOA_PAGED8_RING. So a row is rounded once,
  * and rows that are not accepted have no part in a scale.
  * Table, len, unused sequences and missing pages are as in moa_paged_cache, with these differences: the slots of the ring need no
- * page yet, and a block that is closed on a page that the table does not have is lost. There is no eviction.
+ * page yet, and a block that is closed on a page that the table does not have is lost. There is no eviction, and a closed block is not
+ * opened again: its rows need no longer be in the ring. So len may be lowered to a multiple of 16 (0 among them) or below 0, to no
+ * other value.
  * A closed block of a head is a record of 32 * head_dim + 16 bytes, all codes plus 128: key of token t, dim d at byte
  * ((t % 2) * (head_dim / 64) + d / 64) * 512 + t / 2 * 64 + d % 64; value at 16 * head_dim + d / 32 * 512 + d % 8 * 64 + t / 4 * 16
  * + d / 8 % 4 * 4 + t % 4; then the scales of keys and values (float) and 8 bytes that are not used. moa_paged8_read gives rows. */

@@ -111,3 +111,95 @@ def test_a_prefix_of_a_block_that_holds_a_nan():
     m.append(k, v, [32])
     _, got = _moa().moa_paged8_read(m.c, 32, length=torch.tensor([18], dtype=torch.int32, device="cuda"))
     assert bool(torch.isnan(got[0, 16:18, 1]).all()) and not bool(got[0, 18:].any()) and bool(torch.isfinite(got[0, :, 0]).all())
+
+
+# ------------------------------------------------------------------------------------------------------- lengths
+@pytest.mark.parametrize("back", [0, 16, 48, 96])
+def test_a_length_lowered_to_a_multiple_of_16(back):
+    m = Model(np.random.default_rng(back), [0, 0], 2, 64, 16, extra=400)
+    m.append(m.fresh(107), m.fresh(107), [107, 99])
+    m.len.fill_(back)
+    m.rows = [tuple(x[:back] for x in r) for r in m.rows]
+    m.check_rows()
+    for n in (1, 30):
+        q, k, v = _new_rows(m, n, 8)
+        mask = _tree(m.rng, 2, n)
+        out = _moa().moa_paged8_attention(m.c, q, k, v, mask=mask)
+        _check_rows(m, q, k, v, mask, out)
+        _moa().moa_paged8_commit(m.c, n)
+        for b in range(2):
+            m.keep(b, k[b].cpu(), v[b].cpu())
+        m.check_rows()
+
+
+@pytest.mark.parametrize("dh,hkv", [(64, 3), (128, 8)])
+@pytest.mark.parametrize("lens,rows", [([5, 5, 5], [75, 78, 82]), ([15, 15, 15], [65, 79, 80]), ([1, 20, 33], [95, 60 + 16, 79]), ([79, 80, 81], [1 + 15, 80, 79])])
+def test_appended_rows_that_stay_open_where_the_open_block_lay(lens, rows, dh, hkv):
+    """The ring has 80 rows: a prompt's last rows take the places of those that the same call closes a block with."""
+    m = Model(np.random.default_rng(dh + sum(rows)), lens, hkv, dh, 16, extra=300)
+    for _ in range(2):
+        m.append(m.fresh(max(rows)), m.fresh(max(rows)), rows)
+        m.check_rows()
+        q, k, v = _new_rows(m, 1, 2 * hkv)
+        out = _moa().moa_paged8_attention(m.c, q, k, v)
+        _check_rows(m, q, k, v, None, out)
+
+
+# ------------------------------------------------------------------------------------------------------- workspaces and streams
+def _counters(ws):
+    return ws.view(torch.int32)[:2 * torch.cuda.get_device_properties(0).multi_processor_count]
+
+
+@pytest.mark.parametrize("dh,hq,hkv,lens,n", [
+    (128, 8, 8, [30000], 1), (64, 4, 1, [60000], 1), (64, 128, 1, [20000, 300], 1), (128, 16, 2, [9000, 1, 777], 1), (64, 8, 2, [3000] * 40, 1),
+    (128, 16, 4, [5000, 300], 3), (128, 16, 4, [5000, 300], 61), (64, 64, 32, [2500], 40)])
+def test_every_join_counter_is_zero_between_calls(dh, hq, hkv, lens, n):
+    m = Model(np.random.default_rng(n + hq), lens, hkv, dh, 64)
+    ws = m.c.workspace(n, hq)
+    q, k, v = _new_rows(m, n, hq)
+    want = None
+    for _ in range(3):
+        out = _moa().moa_paged8_attention(m.c, q, k, v, ws=ws)
+        assert not bool(_counters(ws).any())
+        assert want is None or torch.equal(out, want)                # the order in which pieces come in changes nothing
+        want = out
+
+
+@pytest.mark.parametrize("n", [1, 40])
+def test_two_layers_of_one_table_on_two_streams(n):
+    """Two caches of the same table and lengths, each with pages and rings of its own, appended to, attended and committed at the same time."""
+    moa, lens, hkv, dh, page, hq = _moa(), [700, 90], 4, 64, 16, 16
+    a = Model(np.random.default_rng(20), [0, 0], hkv, dh, page, extra=9000)
+    layers = [a.c] + [moa.PagedCache8(torch.zeros_like(a.c.pages), torch.zeros_like(a.c.k_ring), torch.zeros_like(a.c.v_ring), a.c.page_table, a.len, page)]
+    prompt = [tuple(x.cuda() for x in (a.fresh(700), a.fresh(700))) for _ in layers]
+    count, grown = torch.tensor(lens, dtype=torch.int32, device="cuda"), a.len.clone()
+    rows, mask = [_new_rows(a, n, hq) for _ in layers], _tree(a.rng, 2, n)
+    ws = [c.workspace(n, hq) for c in layers]
+    streams = [torch.cuda.Stream() for _ in layers]
+
+    def run(side):
+        for c in layers:
+            for t in (c.pages, c.k_ring, c.v_ring):
+                t.zero_()
+        a.len.copy_(grown)
+        torch.cuda.synchronize()
+        st = streams if side else [None, None]
+        for c, (k, v), s in zip(layers, prompt, st):
+            moa.moa_paged8_append(c, k, v, count, advance=False, stream=s)
+        torch.cuda.synchronize()
+        a.len.copy_(count)
+        torch.cuda.synchronize()
+        outs = []
+        for _ in range(5):
+            for c, (q, k, v), w, s in zip(layers, rows, ws, st):
+                outs.append(moa.moa_paged8_attention(c, q, k, v, mask=mask, ws=w, stream=s))
+        for c, s in zip(layers, st):
+            moa.moa_paged8_commit(c, n, advance=False, stream=s)
+        torch.cuda.synchronize()
+        a.len.add_(n)
+        return outs + [x for c in layers for x in moa.moa_paged8_read(c, 800)]
+
+    want, got = run(False), run(True)
+    for x, y in zip(want, got):
+        assert torch.equal(x, y)
+    assert not torch.equal(want[0], want[1])
