@@ -447,7 +447,8 @@ typedef struct {
   void *k_out;                  /*   of q, k or v or another output. T [rows, hkv, head_dim], rows k_out_stride apart; may be k likewise. NULL with cache */
   int64_t k_out_stride;
   const moa_paged_cache *cache; /* or NULL: keys and values go to slot[r] of its pages (moa_page_plan), outside of the pool: nowhere. Its */
-  const int64_t *slot;          /*   table, lengths, weights and positions are neither read nor written (so not for a cache that evicts) */
+  const int64_t *slot;          /*   table, lengths, weights and positions are neither read nor written (so not for a cache that evicts). No */
+                                /*   two rows may have the same slot */
   int32_t rows;                 /* <= 2^24 */
   int32_t hq, hkv, head_dim;    /* head_dim 64 or 128, hq and hkv <= 1024 */
   int32_t rot_dim;              /* a multiple of 16, <= head_dim; 0: no rotation */
@@ -489,9 +490,17 @@ typedef struct {
  * share len: the layers' calls without advance, the last one with it. No uncommitted rows may be held: their places may be taken. */
 moa_status moa_paged8_append(const moa_paged_cache8 *cache, const void *k_new, const void *v_new, int64_t row_stride, int32_t n,
                              const int32_t *n_new, int32_t advance, void *stream);
-/* moa_paged_attention over the 8-bit cache, without weights: the new rows are kept in the ring. Scores, statistics and sums are fp32. The
- * codes enter the products exactly, the probabilities times the values' scales rounded once to fp16: each off by at most 2^-11 of itself,
- * or, where that is less, 2^-29 of the largest probability times the largest scale.
+/* moa_paged_attention over the 8-bit cache, without weights: the new rows are kept in the ring. Scores, statistics and sums are fp32.
+ *   codes       enter the products exactly
+ *   p           times the values' scales, is rounded once to fp16: off by at most 2^-11 of itself, or, where that is more, 2^-29 of the
+ *               largest probability times the largest scale of the head (of any block that a row of the sequence sees)
+ *   queries     are held in fp16 times a power of two per row and head: exact, but for elements below 2^-31 of the row's largest, which
+ *               are off by at most 2^-39 of it (a row whose largest is below 2^-111 may count as zeros)
+ *   open rows   (not in closed blocks yet) enter as the bf16 that they are where few rows are attended, their values with probabilities of
+ *               two bf16 terms. On tensor memory they are held in fp16 times a power of two per 16 slots of a head and stand for blocks of
+ *               that scale: keys as the queries above, values exact but for elements below 2^-23 of the largest of those slots, which are
+ *               off by at most 2^-31 of it (all below 2^-100: zeros). What is largest there goes by the slots that any row sees, also
+ *               for the rows that do not see them
  *   n_new       n, with k_new and v_new or with rows that a call before has put into the ring; 0: committed slots only
  *   ws          moa_paged8_workspace_bytes bytes, zeroed once; enough for calls of fewer rows of the same cache and heads, too
  * Calls of many query rows over much room (n > 1, by the table's size and not by the lengths) run on tensor memory; a wait there that

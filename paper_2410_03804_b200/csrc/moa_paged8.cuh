@@ -16,13 +16,14 @@
 // 8-bit codes become fp16, exactly, by placing the byte under the exponent of 1024 and subtracting 1152: two instructions for two codes.
 // (A byte with zeros above it is (code + 128) * 2^-24 already, but taking the 128 off the sums afterwards -- from scores by the query's
 // sum, from outputs by one more product of a constant per block -- cost precision where sums cancel and gained nothing.) Queries are
-// scaled by a power of two per row into fp16's range (exact for what lies within 2^28 of the row's largest).
+// scaled by a power of two per row into fp16's range (exact for what lies within 2^31 of the row's largest).
 //
 // What bounds it: one token reads a byte and 1/16 of a scale per cached value once, so the cache's stream from HBM does. 256 bytes
 // per position and head leave 175 cycles of an SM per 16 positions and head, 700 instructions. A short cache is bound by the chain of
 // its steps instead: the lengths, the work's line, the first copies, the join.
 // Measured, one token of 32 heads over 8, head_dim 128: over 2047 positions 11.5 us, over 32767 24.1 us, 16 sequences of up to 8192
-// 42.8 us (the caches alone at a copy's rate: 0.6, 10.2 and 26.4). Appending 2 x 8 heads of 2048 rows and reading them back 14.6 us.
+// 42.8 us (the caches alone at a copy's rate: 0.6, 10.2 and 26.4). Appending 2 x 8 heads of 2043 rows and reading them back 14.6 us in
+// a graph, 12.6 to 13.0 among other calls.
 #pragma once
 #include <cuda_fp16.h>
 

@@ -12,7 +12,7 @@
 // A plan in place has to put pages back before any are taken, and to read before it writes: one CTA, or for large tables a cluster of
 // eight, each CTA with its own sums and the cluster's barriers between; the maps of many rows take a second kernel then.
 // Measured, calls in a graph, to a second pool: a decode step of 64 sequences 4.1 us (in place 2.9 to 4.3); 64 prompts of up to 32768
-// rows (18.4 MB of maps) 7.7 us, where one cluster and a second kernel took 15.1.
+// rows (18.4 MB of maps) 7.7 to 8.1 us, where one cluster and a second kernel took 15.1.
 #pragma once
 #include "moa_paged.cuh"
 
