@@ -37,9 +37,10 @@ constexpr int P8_RING = 80;                  // rows of the 16-bit ring: 15 of a
 constexpr int P8_STAGES = 2;
 constexpr float P8_BIAS = 7.f;               // probabilities enter their fp16 product times 2^7: a row's maximum may pass the
 constexpr float P8_LAZY = 8.f;               // reference by 2^8 before the sums move to a new one, and 2^15 fits fp16
-// Sums and outputs of a piece are handed on times 2^-32 beside that: probabilities times values are divided at the very end only, and
-// 2^24 positions at 2^8 above their reference may have bf16's largest values. (What is below 2^-117 goes, far under a record's least.)
-constexpr float P8_PIECE = 0x1p-39f;         // 2^-P8_BIAS * 2^-32
+// Sums and outputs of a piece are handed on times 2^-16 beside that: probabilities times values are divided at the very end only, and
+// values may be bf16's largest while a row's probabilities, in units of the largest, sum up to no more than 2^16 (values up to 2^106: as
+// long as there are positions). The room comes off the other end: outputs below 2^-110, far under a closed block's least, lose bits.
+constexpr float P8_PIECE = 0x1p-23f;         // 2^-P8_BIAS * 2^-16
 constexpr int P8_OPEN = 100;                 // log2 of the open rows' values over the unit of the outputs, at most
 constexpr int P8_LEAST = -105;               // log2 of the least unit: scales are 0 or above 2^-107, units 4 to 8 times those
 

@@ -83,6 +83,18 @@ def test_infinity_among_small_open_values_before_large_closed_ones():
     assert bool(torch.isfinite(out).all())
 
 
+@pytest.mark.parametrize("dh,lens,n", [(64, [5, 0], 1), (128, [5309, 13], 1), (64, [30, 2000], 3)])
+def test_tiny_open_values_keep_their_bits_where_few_rows_are_attended(dh, lens, n):
+    """Values of 2^-108 behind closed blocks that are held as zeros."""
+    m = Model(np.random.default_rng(dh + n), [0] * len(lens), 2, dh, 16, extra=max(lens) + 70)
+    if max(lens):
+        m.append(m.fresh(max(lens)), m.fresh(max(lens), 2.0**-108), lens)
+    q, kn, vn = _new_rows(m, n, 8)
+    vn *= 2.0**-108
+    out = _moa().moa_paged8_attention(m.c, q, kn, vn)
+    _check_rows(m, q, kn, vn, None, out)
+
+
 # ------------------------------------------------------------------------------------------------------- rows read back
 @pytest.mark.parametrize("dh,hkv,lens,cut", [(64, 2, [40, 7, 160], [33, 3, 90]), (128, 3, [95, -1, 300], [16, 5, 17]), (128, 1, [64, 81, 200], [0, 80, 199])])
 def test_fewer_rows_than_are_committed(dh, hkv, lens, cut):
