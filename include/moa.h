@@ -516,7 +516,8 @@ moa_status moa_paged8_commit(const moa_paged_cache8 *cache, int32_t n, const int
                              int32_t advance, void *stream);
 /* Rows of slots first[b] + i, i < n (first NULL: 0) as they stand for, to k_out, v_out [batch, n, hkv, head_dim] of dtype: code * scale
  * rounded once, or an open row; zeros where no row is (below slot 0, from length[b] on, on a missing page). length: device int32
- * [batch] rows, NULL: the cache's len; fewer than len, or, of a layer whose len has yet to be advanced, more. Rows of a sequence that is not in use (by either) stay as they were. */
+ * [batch] rows, NULL: the cache's len; fewer, or, of a layer whose len has yet to be advanced, all that it has. Rows of a sequence that
+ * is not in use (by either) stay as they were. */
 moa_status moa_paged8_read(const moa_paged_cache8 *cache, int32_t n, const int32_t *first, const int32_t *length, void *k_out, void *v_out,
                            int32_t dtype, void *stream);
 

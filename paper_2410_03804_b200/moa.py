@@ -493,7 +493,8 @@ def moa_page_plan(pool: PagePool, length: torch.Tensor, n_new=None, max_rows: in
     """Gives the sequences the pages of their length[b] committed (< 0: not in use) and n_new[b] new rows (None: one each) and lays
     the new rows out as one packed batch (see include/moa.h). pool_out: a pool of the same shape that gets the result; None: the
     pool itself. Returns maps: (rows int32 [batch], row_start int32 [batch + 1], row_seq int32, row_pos int32, slot int64, each
-    [max_rows]); without max_rows the last three are None and the rows have no bound."""
+    [max_rows]); without max_rows the last three are None and the rows are bounded by 2^31 - 1. rows may be n_new; otherwise what is
+    written overlaps nothing that is read."""
     at, b = pool.index, pool.batch
     assert _is(length, torch.int32, at) and length.shape == (b,), "length: int32 [batch]"
     assert n_new is None or (_is(n_new, torch.int32, at) and n_new.shape == (b,)), "n_new: int32 [batch]"
@@ -533,7 +534,7 @@ def moa_qk_norm_rope(q: torch.Tensor, k: torch.Tensor, pos: torch.Tensor, freq=N
                      interleaved: bool = False, q_out=None, k_out=None, cache=None, slot=None, v=None, stream=None):
     """Norm (with gains [head_dim]) and rotation of q [rows, hq, head_dim] and k [rows, hkv, head_dim], parts of a fused projection as a
     rule. pos: int32 [rows], < 0 for padding; freq: float64 [rot_dim / 2], radians per position (None: no rotation). The results
-    go to q_out and k_out (which may be q and k; None: new ones), or, with a PagedCache and slot int64 [rows] (moa_page_plan), keys
+    go to q_out and k_out (which may be q and k, and otherwise touch no row of the call; None: new ones), or, with a PagedCache and slot int64 [rows] (moa_page_plan), keys
     and values v to the cache's pages. Returns (q_out, k_out), k_out None with a cache."""
     at, dt, shape = q.get_device(), q.dtype, q.shape
     assert at >= 0 and len(shape) == 3 and dt in (torch.float32, torch.bfloat16), "q: cuda [rows, hq, head_dim]"
@@ -578,8 +579,8 @@ PAGED8_BLOCK, PAGED8_RING = 16, 80
 class PagedCache8:
     """A paged key / value cache in 8 bits for bf16 rows (moa_paged_cache8 of include/moa.h). pages: cuda uint8 [n_pages, hkv,
     page_size / 16, 32 * head_dim + 16], contiguous within a page; k_ring, v_ring: bfloat16 [batch, 80, hkv, head_dim]; page_table:
-    int32 [batch, max_pages]; length: int32 [batch], committed slots, < 0 for a sequence not in use; seen: int32 [batch], advanced
-    with length, or None. The tensors are held, not copied; the caller (or moa_page_plan) fills the table."""
+    int32 [batch, max_pages]; length: int32 [batch], committed slots, < 0 for a sequence not in use (lowered to a multiple of 16 only);
+    seen: int32 [batch], advanced with length, or None. The tensors are held, not copied; the caller (or moa_page_plan) fills the table."""
 
     def __init__(self, pages, k_ring, v_ring, page_table, length, page_size: int, seen=None):
         assert pages.is_cuda and pages.dim() == 4 and pages.dtype is torch.uint8, "pages: cuda uint8 [n_pages, hkv, page_size / 16, 32 * head_dim + 16]"
@@ -677,8 +678,8 @@ def moa_paged8_commit(cache: PagedCache8, n: int, acc_slot=None, acc_len=None, a
 
 
 def moa_paged8_read(cache: PagedCache8, n: int, first=None, length=None, dtype=torch.bfloat16, out=None, stream=None):
-    """Rows of slots first[b] .. first[b] + n - 1 (first None: from 0) as they stand for; zeros where no row is. length: int32 [batch],
-    committed rows, None: cache.len. Returns (k, v) [batch, n, hkv, head_dim] of dtype (or of out's)."""
+    """Rows of slots first[b] .. first[b] + n - 1 (first None: from 0) as they stand for; zeros where no row is. length: int32 [batch]
+    rows, None: cache.len; fewer, or, of a layer whose length has yet to be advanced, all that it has. Returns (k, v) [batch, n, hkv, head_dim] of dtype (or of out's)."""
     at, shape = cache.index, (cache.batch, n, cache.hkv, cache.head_dim)
     for t in (first, length):
         assert t is None or (_is(t, torch.int32, at) and t.shape == (cache.batch,)), "first, length: int32 [batch]"
